@@ -14,4 +14,5 @@ from .binding import (KS_DEV_RANGE, FLAG_UNIT_ROWS, FLAG_PAD_RANDOM, FLAG_TRUSTE
                       apply_weight_grad_workspace, knn_norm_backward_rows, knn_normalize_rows, full_softmax_fwd_bwd,
                       full_softmax_workspace, knn_gather_rows, knn_graph_build, knn_graph_build_plan, knn_graph_build_workspace, knn_graph_recall_plan,
                       knn_select_active, knn_select_active_static, knn_select_workspace, knn_softmax_fwd_bwd, knn_softmax_workspace,
-                      ks_version, lib, lib_path, GradTopkPlan, grad_topk_plan, grad_topk_select)
+                      ks_version, lib, lib_path, GradTopkPlan, grad_topk_plan, grad_topk_select,
+                      QUANT_CLASSES, QUANT_NORMALIZE, class_codes_bytes, class_logits_adjust, class_logits_int8, class_quantize_rows)

@@ -1,0 +1,463 @@
+// Answering with the trained layer (paper Section 3.1: W holds one row per class, Section 3.2: the fc forward): rows as 8-bit codes
+// in the order in which matrix instructions take them, logits of a batch against every class from those codes, and the
+// penalties, biases and masks that requests bring.
+#include "../../include/class_logits.h"
+#include "ks_common.h"
+
+typedef int32_t cl_i32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t cl_i32x16 __attribute__((ext_vector_type(16)));
+
+#define CL_NT 256
+#define CL_PIECE 1024 /* bytes of a piece: 32 rows x 32 codes, the operand of one 32x32x32 matrix instruction */
+#define CL_GROUP 128  /* classes whose four blocks of codes lie next to each other */
+
+// ------------------------------------------------------------------------------------------------
+// rows -> codes
+// ------------------------------------------------------------------------------------------------
+#define CLQ_D 1024 /* elements of a row that a workgroup has in LDS at a time */
+
+template <typename IN> struct ClRow;
+template <> struct ClRow<float> {
+    static __device__ __forceinline__ float one(const float *p) { return *p; }
+    static __device__ __forceinline__ float4 four(const float *p) { return *(const float4 *)p; }
+};
+template <> struct ClRow<uint16_t> {
+    static __device__ __forceinline__ float one(const uint16_t *p) { return ks_bf2f(*p); }
+    static __device__ __forceinline__ float4 four(const uint16_t *p) {
+        const uint2 v = *(const uint2 *)p;
+        return make_float4(ks_bf2f(v.x & 0xFFFFu), ks_bf2f(v.x >> 16), ks_bf2f(v.y & 0xFFFFu), ks_bf2f(v.y >> 16));
+    }
+};
+template <> struct ClRow<int8_t> {
+    static __device__ __forceinline__ float one(const int8_t *p) { return (float)*p; }
+    static __device__ __forceinline__ float4 four(const int8_t *p) {
+        const uint32_t v = *(const uint32_t *)p;
+        return make_float4((float)(int8_t)v, (float)(int8_t)(v >> 8), (float)(int8_t)(v >> 16), (float)(int8_t)(v >> 24));
+    }
+};
+// elements d .. d + 3 of a row, 0 beyond D
+template <typename IN, bool VEC> __device__ __forceinline__ float4 cl_load4(const IN *row, int d, int D) {
+    if (VEC && d + 4 <= D) return ClRow<IN>::four(row + d);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (d < D) v.x = ClRow<IN>::one(row + d);
+    if (d + 1 < D) v.y = ClRow<IN>::one(row + d + 1);
+    if (d + 2 < D) v.z = ClRow<IN>::one(row + d + 2);
+    if (d + 3 < D) v.w = ClRow<IN>::one(row + d + 3);
+    return v;
+}
+
+// 127 v / a to the nearest integer, halves to even.  t = v * (127 / a) in fp64 is off by less than 1e-13; where it lies that close
+// to the middle of two integers, |v| * 254 and (2 k + 1) a, which are exact in fp64 (32 bits each), decide.
+__device__ __forceinline__ int cl_code(float v, double inv, double a) {
+    const double t = (double)v * inv;
+    int k = (int)__builtin_rint(t);
+    if (__builtin_fabs(__builtin_fabs(t - (double)k) - 0.5) < 1e-12) {
+        const int lo = (int)__builtin_fabs(t);
+        const double l = __builtin_fabs((double)v) * 254.0, r = (double)(2 * lo + 1) * a;
+        const int m = l > r || (l == r && (lo & 1)) ? lo + 1 : lo;
+        k = v < 0.f ? -m : m;
+    }
+    return k;
+}
+__device__ __forceinline__ double cl_wave_sum_d(double v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        const int lo = __shfl_xor(__double2loint(v), o, 64), hi = __shfl_xor(__double2hiint(v), o, 64);
+        v += __hiloint2double(hi, lo);
+    }
+    return v;
+}
+
+// One workgroup per block of 32 rows; a wavefront takes eight of them one after the other, their codes go through LDS so that
+// whole pieces are stored.
+template <typename IN, bool VEC>
+__global__ void __launch_bounds__(CL_NT)
+cl_quantize_kernel(const IN *__restrict__ V, int64_t n, int D, int64_t ldv, uint32_t flags, int8_t *__restrict__ codes,
+                   float *__restrict__ row_scale) {
+    // piece p of a half h: 32 rows x 16 codes at (2 p + h) * 528 (16 bytes of padding spread the halves over the banks)
+    __shared__ __attribute__((aligned(16))) char lds[CLQ_D / 16 * 528];
+    __shared__ float s_amax[32];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t blk = blockIdx.x;
+    const int kb = (D + 31) / 32;
+    constexpr bool RAW = sizeof(IN) == 1;
+    for (int i = 0; i < 8 && !RAW; ++i) {
+        const int r = wave * 8 + i;
+        const int64_t row = flags & KS_QUANT_CLASSES ? (blk >> 2) * CL_GROUP + 4 * r + (blk & 3) : blk * 32 + r;
+        if (row >= n) continue;
+        const IN *v = V + row * ldv;
+        int top = 0; // bits of |v|: ordered as the values, NaN above infinity
+        double ss = 0.0;
+        for (int d = lane * 4; d < D; d += 256) {
+            const float4 x = cl_load4<IN, VEC>(v, d, D);
+            top = max(max(top, max(__float_as_int(x.x) & 0x7FFFFFFF, __float_as_int(x.y) & 0x7FFFFFFF)),
+                      max(__float_as_int(x.z) & 0x7FFFFFFF, __float_as_int(x.w) & 0x7FFFFFFF));
+            if (flags & KS_QUANT_NORMALIZE) {
+                ss = __builtin_fma((double)x.x, (double)x.x, ss);
+                ss = __builtin_fma((double)x.y, (double)x.y, ss);
+                ss = __builtin_fma((double)x.z, (double)x.z, ss);
+                ss = __builtin_fma((double)x.w, (double)x.w, ss);
+            }
+        }
+        top = ks_wave_max_i(top);
+        const float a = top < 0x7F800000 ? __int_as_float(top) : 0.f; // not finite: codes 0
+        double s = (double)a / 127.0;
+        if (flags & KS_QUANT_NORMALIZE) {
+            ss = cl_wave_sum_d(ss);
+            if (a > 0.f) s /= sqrt(ss);
+        }
+        if (lane == 0) {
+            s_amax[r] = a;
+            row_scale[row] = top < 0x7F800000 ? (float)s : __int_as_float(0x7FC00000);
+        }
+    }
+    __syncthreads();
+    for (int d0 = 0; d0 < D; d0 += CLQ_D) {
+        const int len = min(CLQ_D, kb * 32 - d0); // a multiple of 32
+        for (int i = 0; i < 8; ++i) {
+            const int r = wave * 8 + i;
+            const int64_t row = flags & KS_QUANT_CLASSES ? (blk >> 2) * CL_GROUP + 4 * r + (blk & 3) : blk * 32 + r;
+            const double a = RAW || row >= n ? 0.0 : (double)s_amax[r], inv = a > 0.0 ? 127.0 / a : 0.0;
+            for (int d = lane * 4; d < len; d += 256) {
+                uint32_t q = 0;
+                if (row < n) {
+                    const float4 x = cl_load4<IN, VEC>(V + row * ldv, d0 + d, D);
+                    int c0, c1, c2, c3;
+                    if (RAW) { c0 = (int)x.x; c1 = (int)x.y; c2 = (int)x.z; c3 = (int)x.w; }
+                    else if (a > 0.0) { c0 = cl_code(x.x, inv, a); c1 = cl_code(x.y, inv, a); c2 = cl_code(x.z, inv, a); c3 = cl_code(x.w, inv, a); }
+                    else c0 = c1 = c2 = c3 = 0;
+                    q = (c0 & 255) | (c1 & 255) << 8 | (c2 & 255) << 16 | (uint32_t)c3 << 24;
+                }
+                *(uint32_t *)(lds + (d >> 4) * 528 + r * 16 + (d & 15)) = q;
+            }
+        }
+        __syncthreads();
+        int8_t *out = codes + (blk * kb + d0 / 32) * CL_PIECE;
+        for (int e = threadIdx.x; e < len * 2; e += CL_NT) // 16-byte units: half-piece e / 32, row e % 32
+            *(uint4 *)(out + (int64_t)e * 16) = *(const uint4 *)(lds + (e >> 5) * 528 + (e & 31) * 16);
+        __syncthreads();
+    }
+}
+
+extern "C" size_t class_codes_bytes(int64_t n, int D, uint32_t flags) {
+    if (n < 1 || D < 1 || D > KS_MAX_INT8_D) return 0;
+    const int64_t rows = flags & KS_QUANT_CLASSES ? ks_ceil_div(n, CL_GROUP) * CL_GROUP : ks_ceil_div(n, 32) * 32;
+    return (size_t)rows * ((D + 31) / 32 * 32);
+}
+
+template <typename IN>
+static void cl_quantize(const void *V, int64_t n, int D, int64_t ldv, uint32_t flags, int8_t *codes, float *row_scale, hipStream_t st) {
+    const dim3 grid((unsigned)(flags & KS_QUANT_CLASSES ? ks_ceil_div(n, CL_GROUP) * 4 : ks_ceil_div(n, 32)));
+    const bool vec = ((uintptr_t)V | (uintptr_t)(ldv * sizeof(IN))) % (4 * sizeof(IN)) == 0;
+    if (vec) hipLaunchKernelGGL((cl_quantize_kernel<IN, true>), grid, dim3(CL_NT), 0, st, (const IN *)V, n, D, ldv, flags, codes, row_scale);
+    else hipLaunchKernelGGL((cl_quantize_kernel<IN, false>), grid, dim3(CL_NT), 0, st, (const IN *)V, n, D, ldv, flags, codes, row_scale);
+}
+
+extern "C" int class_quantize_rows(const void *V, int dtype, int64_t n, int D, int64_t ldv, uint32_t flags, int8_t *codes,
+                                   float *row_scale, void *stream) {
+    if (!V || !codes || n < 1 || n >= (int64_t)1 << 31 || D < 1 || ldv < D) return KS_INVALID_ARG;
+    if (dtype != KS_DTYPE_BF16 && dtype != KS_DTYPE_FP32 && dtype != KS_DTYPE_INT8) return KS_INVALID_ARG;
+    if (flags & ~(KS_QUANT_CLASSES | KS_QUANT_NORMALIZE) || (uintptr_t)codes % 16) return KS_INVALID_ARG;
+    if ((uintptr_t)V % (dtype == KS_DTYPE_FP32 ? 4 : dtype == KS_DTYPE_BF16 ? 2 : 1)) return KS_INVALID_ARG;
+    if (dtype == KS_DTYPE_INT8 ? row_scale || (flags & KS_QUANT_NORMALIZE) : !row_scale) return KS_INVALID_ARG;
+    if (D > KS_MAX_INT8_D) return KS_UNSUPPORTED;
+    hipStream_t st = (hipStream_t)stream;
+    if (dtype == KS_DTYPE_FP32) cl_quantize<float>(V, n, D, ldv, flags, codes, row_scale, st);
+    else if (dtype == KS_DTYPE_BF16) cl_quantize<uint16_t>(V, n, D, ldv, flags, codes, row_scale, st);
+    else cl_quantize<int8_t>(V, n, D, ldv, flags, codes, row_scale, st);
+    KS_LAUNCH_CHECK();
+    return KS_OK;
+}
+
+// ------------------------------------------------------------------------------------------------
+// logits
+// ------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void cl_store(float *p, float v) { *p = v; }
+__device__ __forceinline__ void cl_store(uint16_t *p, float v) { *p = (uint16_t)ks_f2bf(v); }
+__device__ __forceinline__ void cl_store4(float *p, float4 v) { *(float4 *)p = v; }
+__device__ __forceinline__ void cl_store4(uint16_t *p, float4 v) { *(uint2 *)p = make_uint2(ks_pack_bf2(v.x, v.y), ks_pack_bf2(v.z, v.w)); }
+
+// One wavefront: 128 classes (the four blocks of a group) by 32 S samples.  A lane of the result holds one column of each of the
+// four blocks, which are four consecutive classes: it stores them as one piece, 32 lanes 512 (fp32) or 256 bytes of a row.
+template <int S, typename OUT>
+__global__ void __launch_bounds__(CL_NT)
+cl_direct_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, const int8_t *__restrict__ wq,
+                 const float *__restrict__ ws, const float *__restrict__ bias, int64_t C, int kb, int B, float scale,
+                 OUT *__restrict__ out, int64_t ldl, int vec) {
+    const int lane = threadIdx.x & 63;
+    const int64_t grp = (int64_t)blockIdx.x * (CL_NT / 64) + (threadIdx.x >> 6);
+    if (grp * CL_GROUP >= C) return;
+    const int sb = blockIdx.y * S, xblocks = (B + 31) / 32; // first block of samples
+    const int8_t *wp = wq + grp * 4 * kb * CL_PIECE + lane * 16;
+    const int8_t *xp[S];
+#pragma unroll
+    for (int s = 0; s < S; ++s) xp[s] = xq + (int64_t)min(sb + s, xblocks - 1) * kb * CL_PIECE + lane * 16;
+    cl_i32x16 acc[S][4];
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[s][g][r] = 0;
+#pragma unroll 4
+    for (int k = 0; k < kb; ++k) {
+        cl_i32x4 w[4], x[S];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) w[g] = *(const cl_i32x4 *)(wp + ((int64_t)g * kb + k) * CL_PIECE);
+#pragma unroll
+        for (int s = 0; s < S; ++s) x[s] = *(const cl_i32x4 *)(xp[s] + (int64_t)k * CL_PIECE);
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) acc[s][g] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[s], w[g], acc[s][g], 0, 0, 0);
+    }
+    const int64_t c = grp * CL_GROUP + 4 * (lane & 31);
+    float sw[4], b[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        sw[g] = c + g < C ? ws[c + g] : 0.f;
+        b[g] = bias && c + g < C ? bias[c + g] : 0.f;
+    }
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int m = (sb + s) * 32 + 8 * (r / 4) + 4 * (lane >> 5) + (r & 3);
+            if (m >= B) continue;
+            const float f = scale * xs[m];
+            float v[4];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                v[g] = (float)acc[s][g][r] * f * sw[g];
+                if (bias) v[g] += b[g];
+            }
+            OUT *p = out + (int64_t)m * ldl + c;
+            if (vec && c + 4 <= C) cl_store4(p, make_float4(v[0], v[1], v[2], v[3]));
+            else
+                for (int g = 0; g < 4; ++g)
+                    if (c + g < C) cl_store(p + g, v[g]);
+        }
+}
+
+template <typename OUT>
+static void cl_logits(const int8_t *xq, const float *xs, const int8_t *wq, const float *ws, const float *bias, int64_t C, int D, int B,
+                      float scale, OUT *out, int64_t ldl, hipStream_t st) {
+    const int vec = ((uintptr_t)out | (uintptr_t)(ldl * sizeof(OUT))) % (4 * sizeof(OUT)) == 0, kb = (D + 31) / 32;
+    const unsigned gx = (unsigned)ks_ceil_div(ks_ceil_div(C, CL_GROUP), CL_NT / 64);
+    if (B <= 32)
+        hipLaunchKernelGGL((cl_direct_kernel<1, OUT>), dim3(gx, 1), dim3(CL_NT), 0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, vec);
+    else
+        hipLaunchKernelGGL((cl_direct_kernel<2, OUT>), dim3(gx, (unsigned)ks_ceil_div(B, 64)), dim3(CL_NT), 0, st, xq, xs, wq, ws, bias, C,
+                           kb, B, scale, out, ldl, vec);
+}
+
+extern "C" int class_logits_int8(const int8_t *x_codes, const float *x_scale, const int8_t *w_codes, const float *w_scale,
+                                 const float *bias, int64_t C, int D, int B, float scale, void *logits, int dtype, int64_t ldl,
+                                 void *stream) {
+    if (!x_codes || !x_scale || !w_codes || !w_scale || !logits) return KS_INVALID_ARG;
+    if (C < 1 || C >= (int64_t)1 << 31 || D < 1 || B < 1 || ldl < C) return KS_INVALID_ARG;
+    if (dtype != KS_DTYPE_BF16 && dtype != KS_DTYPE_FP32) return KS_INVALID_ARG;
+    if (((uintptr_t)x_codes | (uintptr_t)w_codes) % 16 || (uintptr_t)logits % (dtype == KS_DTYPE_FP32 ? 4 : 2)) return KS_INVALID_ARG;
+    if (D > KS_MAX_INT8_D) return KS_UNSUPPORTED;
+    if (dtype == KS_DTYPE_FP32)
+        cl_logits<float>(x_codes, x_scale, w_codes, w_scale, bias, C, D, B, scale, (float *)logits, ldl, (hipStream_t)stream);
+    else
+        cl_logits<uint16_t>(x_codes, x_scale, w_codes, w_scale, bias, C, D, B, scale, (uint16_t *)logits, ldl, (hipStream_t)stream);
+    KS_LAUNCH_CHECK();
+    return KS_OK;
+}
+
+// ------------------------------------------------------------------------------------------------
+// penalties, biases, masks
+// ------------------------------------------------------------------------------------------------
+struct ClAdjust {
+    const void *in;
+    void *out;
+    int64_t ldl, ldo, C, c0, Cg;
+    const int64_t *seen_offsets, *bias_offsets;
+    const int32_t *seen_ids, *bias_ids, *n_prompt, *mask_row;
+    const float *bias_values, *repetition, *presence, *frequency;
+    const uint32_t *allowed;
+    int64_t seen_len, bias_len, ld_allowed;
+    int B, seen_max, bias_max, n_masks, row0; // a launch takes the rows from row0 on
+    int32_t *dev_status;
+};
+
+__device__ __forceinline__ float cl_load(const float *p) { return *p; }
+__device__ __forceinline__ float cl_load(const uint16_t *p) { return ks_bf2f(*p); }
+template <typename T> __device__ __forceinline__ T cl_minus_inf();
+template <> __device__ __forceinline__ float cl_minus_inf<float>() { return __uint_as_float(0xFF800000u); }
+template <> __device__ __forceinline__ uint16_t cl_minus_inf<uint16_t>() { return 0xFF80u; }
+
+// mask of request b, -1: none
+__device__ __forceinline__ int cl_mask_of(const ClAdjust &a, int b) {
+    if (!a.allowed) return -1;
+    const int m = a.mask_row ? a.mask_row[b] : b;
+    if (m >= a.n_masks) {
+        if (threadIdx.x == 0) ks_flag(a.dev_status, KS_DEV_BAD_INDEX);
+        return -1;
+    }
+    return m;
+}
+// list b of a set of lists laid end to end: -> its length (0 where it is not a list), its first entry through *first
+__device__ __forceinline__ int cl_list(const int64_t *offsets, int64_t len, int most, int b, int64_t *first, int32_t *dev_status) {
+    if (!offsets) return 0;
+    const int64_t lo = offsets[b], hi = offsets[b + 1];
+    *first = lo;
+    if (lo < 0 || hi < lo || hi > len || hi - lo > most) {
+        if (threadIdx.x == 0) ks_flag(dev_status, KS_DEV_BAD_COUNT);
+        return 0;
+    }
+    return (int)(hi - lo);
+}
+// column of an id on this node, -1 for an empty entry or another node's class
+__device__ __forceinline__ int64_t cl_column(const ClAdjust &a, int32_t id, int bad) {
+    if (id < 0) return -1;
+    if (id >= a.Cg) {
+        ks_flag(a.dev_status, bad);
+        return -1;
+    }
+    const int64_t c = (int64_t)id - a.c0;
+    return c < 0 || c >= a.C ? -1 : c;
+}
+// steps 1 and 2 on column c of request b.  seen: bit 0: in the prompt, the rest: occurrences behind it; j: entry of the bias list or -1
+template <typename T> __device__ __forceinline__ void cl_adjust_one(const ClAdjust &a, int b, int64_t c, uint32_t seen, int j, int64_t bias_first) {
+    float z = cl_load((const T *)a.in + b * a.ldl + c);
+    if (seen) {
+        if (a.repetition) {
+            const float r = a.repetition[b];
+            z = z > 0.f ? z / r : z * r;
+        }
+        const uint32_t n = seen >> 1;
+        if (n) z -= (a.frequency ? a.frequency[b] * (float)n : 0.f) + (a.presence ? a.presence[b] : 0.f);
+    }
+    if (j >= 0) z += a.bias_values[bias_first + j];
+    cl_store((T *)a.out + b * a.ldo + c, z);
+}
+
+// masks, and where COPY the logits that stay as they are; a workgroup takes a stretch of one row
+#define CLM_U 4
+template <typename T, bool COPY, bool VEC>
+__global__ void __launch_bounds__(CL_NT) cl_mask_kernel(ClAdjust a, int per_row) {
+    constexpr int E = VEC ? 16 / (int)sizeof(T) : 1;
+    const int b = a.row0 + blockIdx.x / per_row;
+    const int m = cl_mask_of(a, b);
+    if (!COPY && m < 0) return;
+    const uint32_t *bits = m < 0 ? nullptr : a.allowed + (int64_t)m * a.ld_allowed;
+    const T *in = (const T *)a.in + b * a.ldl;
+    T *out = (T *)a.out + b * a.ldo;
+    const T none = cl_minus_inf<T>();
+    const int64_t first = ((int64_t)(blockIdx.x % per_row) * CLM_U * CL_NT + threadIdx.x) * E;
+#pragma unroll
+    for (int u = 0; u < CLM_U; ++u) {
+        const int64_t c = first + (int64_t)u * CL_NT * E;
+        if (c >= a.C) break;
+        const uint32_t w = bits ? bits[c >> 5] >> (c & 31) : ~0u;
+        if (E > 1 && c + E <= a.C) {
+            union { uint4 q; T e[E]; } v;
+            if (COPY) {
+                v.q = *(const uint4 *)(in + c);
+#pragma unroll
+                for (int e = 0; e < E; ++e) v.e[e] = w >> e & 1 ? v.e[e] : none;
+                *(uint4 *)(out + c) = v.q;
+            } else if ((w & ((1u << E) - 1)) == 0) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) v.e[e] = none;
+                *(uint4 *)(out + c) = v.q;
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (!(w >> e & 1)) out[c + e] = none;
+            }
+        } else {
+            for (int e = 0; e < E && c + e < a.C; ++e) {
+                if (!(w >> e & 1)) out[c + e] = none;
+                else if (COPY) out[c + e] = in[c + e];
+            }
+        }
+    }
+}
+
+// Lists: a workgroup has one count and one bias entry for each of CLR classes in LDS and takes the request's entries among them.
+#define CLR 8192
+template <typename T>
+__global__ void __launch_bounds__(1024) cl_range_kernel(ClAdjust a, int ranges) {
+    __shared__ uint32_t s_seen[CLR];
+    __shared__ int s_bias[CLR];
+    const int b = a.row0 + blockIdx.x / ranges;
+    const int64_t r0 = (int64_t)(blockIdx.x % ranges) * CLR;
+    int64_t sf = 0, bf = 0;
+    const int ns = cl_list(a.seen_offsets, a.seen_len, a.seen_max, b, &sf, a.dev_status);
+    const int nb = cl_list(a.bias_offsets, a.bias_len, a.bias_max, b, &bf, a.dev_status);
+    const int m = cl_mask_of(a, b);
+    if (ns + nb == 0) return;
+    const int prompt = a.n_prompt ? a.n_prompt[b] : 0;
+    for (int e = threadIdx.x; e < CLR; e += 1024) { s_seen[e] = 0; s_bias[e] = -1; }
+    __syncthreads();
+    for (int e = threadIdx.x; e < ns; e += 1024) {
+        const int64_t c = cl_column(a, a.seen_ids[sf + e], KS_DEV_BAD_LABEL) - r0;
+        if (c < 0 || c >= CLR) continue;
+        if (e < prompt) atomicOr(&s_seen[c], 1u);
+        else atomicAdd(&s_seen[c], 2u);
+    }
+    for (int e = threadIdx.x; e < nb; e += 1024) {
+        const int64_t c = cl_column(a, a.bias_ids[bf + e], KS_DEV_BAD_INDEX) - r0;
+        if (c >= 0 && c < CLR) atomicMax(&s_bias[c], e);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < CLR; e += 1024) {
+        const uint32_t seen = s_seen[e];
+        const int j = s_bias[e];
+        if (!seen && j < 0) continue;
+        const int64_t c = r0 + e;
+        if (m >= 0 && !(a.allowed[(int64_t)m * a.ld_allowed + (c >> 5)] >> (c & 31) & 1)) continue; // masked
+        cl_adjust_one<T>(a, b, c, seen, j, bf);
+    }
+}
+
+#define CL_MAX_GRID (1 << 21) /* workgroups of a launch: threads are counted in 32 bits */
+// launch(a, blocks) for stretches of rows that fit into a launch, per_row workgroups each
+template <class F> static void cl_rows(ClAdjust a, int per_row, F launch) {
+    const int rows = per_row < CL_MAX_GRID ? CL_MAX_GRID / per_row : 1, B = a.B;
+    for (a.row0 = 0; a.row0 < B; a.row0 += rows) launch(a, dim3((unsigned)per_row * (unsigned)(rows < B - a.row0 ? rows : B - a.row0)));
+}
+
+template <typename T> static void cl_adjust(const ClAdjust &args, hipStream_t st) {
+    const bool copy = args.in != args.out;
+    const bool vec = ((uintptr_t)args.in | (uintptr_t)args.out | (uintptr_t)(args.ldl * sizeof(T)) | (uintptr_t)(args.ldo * sizeof(T))) % 16 == 0;
+    if (copy || args.allowed) {
+        const int per_row = (int)ks_ceil_div(args.C, (int64_t)CLM_U * CL_NT * (vec ? 16 / (int)sizeof(T) : 1));
+        cl_rows(args, per_row, [&](const ClAdjust &a, dim3 grid) {
+            if (copy && vec) hipLaunchKernelGGL((cl_mask_kernel<T, true, true>), grid, dim3(CL_NT), 0, st, a, per_row);
+            else if (copy) hipLaunchKernelGGL((cl_mask_kernel<T, true, false>), grid, dim3(CL_NT), 0, st, a, per_row);
+            else if (vec) hipLaunchKernelGGL((cl_mask_kernel<T, false, true>), grid, dim3(CL_NT), 0, st, a, per_row);
+            else hipLaunchKernelGGL((cl_mask_kernel<T, false, false>), grid, dim3(CL_NT), 0, st, a, per_row);
+        });
+    }
+    if ((args.seen_offsets && args.seen_max) || (args.bias_offsets && args.bias_max)) {
+        const int ranges = (int)ks_ceil_div(args.C, CLR);
+        cl_rows(args, ranges, [&](const ClAdjust &a, dim3 grid) { hipLaunchKernelGGL(cl_range_kernel<T>, grid, dim3(1024), 0, st, a, ranges); });
+    }
+}
+
+extern "C" int class_logits_adjust(const void *logits, int64_t ldl, void *out, int64_t ldo, int dtype, int64_t C, int64_t c0,
+                                   int64_t Cg, int B, const int64_t *seen_offsets, const int32_t *seen_ids, int64_t seen_len,
+                                   int seen_max, const int32_t *n_prompt, const float *repetition, const float *presence,
+                                   const float *frequency, const int64_t *bias_offsets, const int32_t *bias_ids,
+                                   const float *bias_values, int64_t bias_len, int bias_max, const uint32_t *allowed,
+                                   int64_t ld_allowed, int n_masks, const int32_t *mask_row, int32_t *dev_status, void *stream) {
+    if (!logits || !out || B < 1 || C < 1 || c0 < 0 || Cg >= (int64_t)1 << 31 || c0 + C > Cg || ldl < C || ldo < C) return KS_INVALID_ARG;
+    if (dtype != KS_DTYPE_BF16 && dtype != KS_DTYPE_FP32) return KS_INVALID_ARG;
+    if (((uintptr_t)logits | (uintptr_t)out) % (dtype == KS_DTYPE_FP32 ? 4 : 2) || (logits == out && ldl != ldo)) return KS_INVALID_ARG;
+    if (seen_len < 0 || bias_len < 0 || seen_max < 0 || bias_max < 0 || (int64_t)seen_max + bias_max >= (int64_t)1 << 30) return KS_INVALID_ARG;
+    if (seen_offsets && seen_len && !seen_ids) return KS_INVALID_ARG;
+    if (bias_offsets && bias_len && (!bias_ids || !bias_values)) return KS_INVALID_ARG;
+    if (allowed && (ld_allowed < (C + 31) / 32 || n_masks < 1 || (!mask_row && n_masks < B))) return KS_INVALID_ARG;
+    if (logits == out && !allowed && !(seen_offsets && seen_max) && !(bias_offsets && bias_max)) return KS_OK; // nothing changes
+    const ClAdjust a = {logits, out, ldl, ldo, C, c0, Cg, seen_offsets, bias_offsets, seen_ids, bias_ids, n_prompt, mask_row, bias_values,
+                        repetition, presence, frequency, allowed, seen_len, bias_len, ld_allowed, B, seen_max, bias_max, n_masks, 0, dev_status};
+    if (dtype == KS_DTYPE_FP32) cl_adjust<float>(a, (hipStream_t)stream);
+    else cl_adjust<uint16_t>(a, (hipStream_t)stream);
+    KS_LAUNCH_CHECK();
+    return KS_OK;
+}
