@@ -36,7 +36,7 @@ extern "C" {
  *              one); a KS_DTYPE_INT8 row is taken as it is.  class_codes_bytes(n, D, flags) bytes, 16-byte aligned, all of them
  *              written: blocks of 32 rows; a block holds ceil(D / 32) pieces of 1,024 bytes; in piece p, byte
  *              (h * 32 + r) * 16 + j  is the code of element 32 p + 16 h + j of the block's row r (h = 0, 1; j = 0 .. 15).
- *              Block b holds rows 32 b + r, with KS_QUANT_CLASSES rows 128 (b / 4) + 4 r + b % 4.  What lies beyond row n or
+ *              Block b holds rows 32 b + r, with KS_QUANT_CLASSES rows 64 (b / 2) + 2 r + b % 2.  What lies beyond row n or
  *              element D is 0.
  * A zero row has codes 0 and scale 0.  A row that holds an infinity or a NaN has codes 0 and scale NaN: all its logits are NaN.
  * Requires n >= 1, 1 <= D <= KS_MAX_INT8_D (KS_UNSUPPORTED beyond); KS_QUANT_NORMALIZE not with KS_DTYPE_INT8.
@@ -56,7 +56,7 @@ int class_quantize_rows(const void *V, int dtype, int64_t n, int D, int64_t ldv,
  *   bias     [C] fp32, may be NULL
  *   logits   [B, C] out, dtype KS_DTYPE_FP32 or KS_DTYPE_BF16; row i begins at element i * ldl (ldl >= C; elements between C and ldl
  *            are not touched, so that a node of a sharded layer may write its columns of a larger matrix).  Aligned to its
- *            elements is enough; rows that begin on 16 bytes (ldl a multiple of 4 or 8) are written faster
+ *            elements is enough; rows that begin on whole 128-byte lines are written fastest, an odd ldl slowest
  * Requires B >= 1, 1 <= C < 2^31, 1 <= D <= KS_MAX_INT8_D (KS_UNSUPPORTED beyond).
  * ---------------------------------------------------------------------------------------------------- */
 int class_logits_int8(const int8_t *x_codes, const float *x_scale, const int8_t *w_codes, const float *w_scale, const float *bias,

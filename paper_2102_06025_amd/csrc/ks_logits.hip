@@ -7,9 +7,12 @@
 typedef int32_t cl_i32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t cl_i32x16 __attribute__((ext_vector_type(16)));
 
+#define CL_GPTR(p) ((const void __attribute__((address_space(1))) *)(p))
+#define CL_LPTR(p) ((void __attribute__((address_space(3))) *)(p))
+
 #define CL_NT 256
 #define CL_PIECE 1024 /* bytes of a piece: 32 rows x 32 codes, the operand of one 32x32x32 matrix instruction */
-#define CL_GROUP 128  /* classes whose four blocks of codes lie next to each other */
+#define CL_GROUP 64   /* classes whose two blocks of codes lie next to each other, every other class in each */
 
 // ------------------------------------------------------------------------------------------------
 // rows -> codes
@@ -83,7 +86,7 @@ cl_quantize_kernel(const IN *__restrict__ V, int64_t n, int D, int64_t ldv, uint
     constexpr bool RAW = sizeof(IN) == 1;
     for (int i = 0; i < 8 && !RAW; ++i) {
         const int r = wave * 8 + i;
-        const int64_t row = flags & KS_QUANT_CLASSES ? (blk >> 2) * CL_GROUP + 4 * r + (blk & 3) : blk * 32 + r;
+        const int64_t row = flags & KS_QUANT_CLASSES ? (blk >> 1) * CL_GROUP + 2 * r + (blk & 1) : blk * 32 + r;
         if (row >= n) continue;
         const IN *v = V + row * ldv;
         int top = 0; // bits of |v|: ordered as the values, NaN above infinity
@@ -116,7 +119,7 @@ cl_quantize_kernel(const IN *__restrict__ V, int64_t n, int D, int64_t ldv, uint
         const int len = min(CLQ_D, kb * 32 - d0); // a multiple of 32
         for (int i = 0; i < 8; ++i) {
             const int r = wave * 8 + i;
-            const int64_t row = flags & KS_QUANT_CLASSES ? (blk >> 2) * CL_GROUP + 4 * r + (blk & 3) : blk * 32 + r;
+            const int64_t row = flags & KS_QUANT_CLASSES ? (blk >> 1) * CL_GROUP + 2 * r + (blk & 1) : blk * 32 + r;
             const double a = RAW || row >= n ? 0.0 : (double)s_amax[r], inv = a > 0.0 ? 127.0 / a : 0.0;
             for (int d = lane * 4; d < len; d += 256) {
                 uint32_t q = 0;
@@ -147,7 +150,7 @@ extern "C" size_t class_codes_bytes(int64_t n, int D, uint32_t flags) {
 
 template <typename IN>
 static void cl_quantize(const void *V, int64_t n, int D, int64_t ldv, uint32_t flags, int8_t *codes, float *row_scale, hipStream_t st) {
-    const dim3 grid((unsigned)(flags & KS_QUANT_CLASSES ? ks_ceil_div(n, CL_GROUP) * 4 : ks_ceil_div(n, 32)));
+    const dim3 grid((unsigned)(flags & KS_QUANT_CLASSES ? ks_ceil_div(n, CL_GROUP) * 2 : ks_ceil_div(n, 32)));
     const bool vec = ((uintptr_t)V | (uintptr_t)(ldv * sizeof(IN))) % (4 * sizeof(IN)) == 0;
     if (vec) hipLaunchKernelGGL((cl_quantize_kernel<IN, true>), grid, dim3(CL_NT), 0, st, (const IN *)V, n, D, ldv, flags, codes, row_scale);
     else hipLaunchKernelGGL((cl_quantize_kernel<IN, false>), grid, dim3(CL_NT), 0, st, (const IN *)V, n, D, ldv, flags, codes, row_scale);
@@ -174,78 +177,197 @@ extern "C" int class_quantize_rows(const void *V, int dtype, int64_t n, int D, i
 // ------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void cl_store(float *p, float v) { *p = v; }
 __device__ __forceinline__ void cl_store(uint16_t *p, float v) { *p = (uint16_t)ks_f2bf(v); }
-__device__ __forceinline__ void cl_store4(float *p, float4 v) { *(float4 *)p = v; }
-__device__ __forceinline__ void cl_store4(uint16_t *p, float4 v) { *(uint2 *)p = make_uint2(ks_pack_bf2(v.x, v.y), ks_pack_bf2(v.z, v.w)); }
+// whole pieces pass by the caches: nobody here reads a logit again, and the codes stay in them
+__device__ __forceinline__ void cl_store2(float *p, float v0, float v1) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    __builtin_nontemporal_store(f32x2{v0, v1}, (f32x2 *)p);
+}
+__device__ __forceinline__ void cl_store2(uint16_t *p, float v0, float v1) { __builtin_nontemporal_store(ks_pack_bf2(v0, v1), (uint32_t *)p); }
 
-// One wavefront: 128 classes (the four blocks of a group) by 32 S samples.  A lane of the result holds one column of each of the
-// four blocks, which are four consecutive classes: it stores them as one piece, 32 lanes 512 (fp32) or 256 bytes of a row.
+// Scales, bias, type and store of 32 S samples by 64 classes.  A lane of the result holds one column of each of the two blocks, which
+// are two consecutive classes.  f: scales of the lane's samples (LDS), p: logit of its first sample and first class, rows: samples
+// from that one on.  WHOLE: everything exists and pairs of classes are aligned.
+template <int S, bool WHOLE, typename OUT>
+__device__ __forceinline__ void cl_finish(const cl_i32x16 (&acc)[S][2], const float *f, const float *__restrict__ ws,
+                                          const float *__restrict__ bias, int64_t c, int64_t C, int rows, OUT *p, int64_t ldl) {
+    float sw[2], b[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        sw[q] = WHOLE || c + q < C ? ws[c + q] : 0.f;
+        b[q] = bias && (WHOLE || c + q < C) ? bias[c + q] : 0.f;
+    }
+    asm volatile("" : "+s"(ldl)); // row addresses are formed here, not kept in registers from group to group
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+            __builtin_amdgcn_sched_barrier(0);
+            const float4 f4 = *(const float4 *)(f + s * 32 + r4 * 8);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float fr = r == 0 ? f4.x : r == 1 ? f4.y : r == 2 ? f4.z : f4.w;
+                float v[2];
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    v[q] = (float)acc[s][q][r4 * 4 + r] * fr * sw[q];
+                    if (bias) v[q] += b[q];
+                }
+                if (WHOLE) cl_store2(p, v[0], v[1]);
+                else if (s * 32 + r4 * 8 + r < rows) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+                        if (c + q < C) cl_store(p + q, v[q]);
+                }
+                p += r < 3 ? ldl : 5 * ldl; // the other half of the wavefront holds the four rows between
+            }
+        }
+}
+
+// One wavefront: 64 classes (the two blocks of a group) by 32 S samples, codes straight from memory.
 template <int S, typename OUT>
 __global__ void __launch_bounds__(CL_NT)
 cl_direct_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, const int8_t *__restrict__ wq,
                  const float *__restrict__ ws, const float *__restrict__ bias, int64_t C, int kb, int B, float scale,
                  OUT *__restrict__ out, int64_t ldl, int vec) {
+    __shared__ __attribute__((aligned(16))) float s_f[32 * S];
     const int lane = threadIdx.x & 63;
-    const int64_t grp = (int64_t)blockIdx.x * (CL_NT / 64) + (threadIdx.x >> 6);
-    if (grp * CL_GROUP >= C) return;
     const int sb = blockIdx.y * S, xblocks = (B + 31) / 32; // first block of samples
-    const int8_t *wp = wq + grp * 4 * kb * CL_PIECE + lane * 16;
+    if (threadIdx.x < 32 * S) s_f[threadIdx.x] = sb * 32 + (int)threadIdx.x < B ? scale * xs[sb * 32 + threadIdx.x] : 0.f;
+    __syncthreads();
+    const int64_t grp = (int64_t)blockIdx.x * (CL_NT / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (grp * CL_GROUP >= C) return;
+    const int8_t *wp = wq + grp * 2 * kb * CL_PIECE + lane * 16;
     const int8_t *xp[S];
 #pragma unroll
     for (int s = 0; s < S; ++s) xp[s] = xq + (int64_t)min(sb + s, xblocks - 1) * kb * CL_PIECE + lane * 16;
-    cl_i32x16 acc[S][4];
+    cl_i32x16 acc[S][2];
 #pragma unroll
     for (int s = 0; s < S; ++s)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
+        for (int q = 0; q < 2; ++q)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[s][g][r] = 0;
-#pragma unroll 4
+            for (int r = 0; r < 16; ++r) acc[s][q][r] = 0;
     for (int k = 0; k < kb; ++k) {
-        cl_i32x4 w[4], x[S];
+        cl_i32x4 w[2], x[S];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) w[g] = *(const cl_i32x4 *)(wp + ((int64_t)g * kb + k) * CL_PIECE);
+        for (int q = 0; q < 2; ++q) w[q] = *(const cl_i32x4 *)(wp + ((int64_t)q * kb + k) * CL_PIECE);
 #pragma unroll
         for (int s = 0; s < S; ++s) x[s] = *(const cl_i32x4 *)(xp[s] + (int64_t)k * CL_PIECE);
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) acc[s][g] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[s], w[g], acc[s][g], 0, 0, 0);
+            for (int q = 0; q < 2; ++q) acc[s][q] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[s], w[q], acc[s][q], 0, 0, 0);
     }
-    const int64_t c = grp * CL_GROUP + 4 * (lane & 31);
-    float sw[4], b[4];
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        sw[g] = c + g < C ? ws[c + g] : 0.f;
-        b[g] = bias && c + g < C ? bias[c + g] : 0.f;
-    }
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int m = (sb + s) * 32 + 8 * (r / 4) + 4 * (lane >> 5) + (r & 3);
-            if (m >= B) continue;
-            const float f = scale * xs[m];
-            float v[4];
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                v[g] = (float)acc[s][g][r] * f * sw[g];
-                if (bias) v[g] += b[g];
-            }
-            OUT *p = out + (int64_t)m * ldl + c;
-            if (vec && c + 4 <= C) cl_store4(p, make_float4(v[0], v[1], v[2], v[3]));
-            else
-                for (int g = 0; g < 4; ++g)
-                    if (c + g < C) cl_store(p + g, v[g]);
+    const int64_t c = grp * CL_GROUP + 2 * (lane & 31);
+    const int m0 = sb * 32 + 4 * (lane >> 5);
+    OUT *to = out + (int64_t)m0 * ldl + c;
+    if (vec && sb * 32 + 32 * S <= B && (grp + 1) * CL_GROUP <= C)
+        cl_finish<S, true>(acc, s_f + 4 * (lane >> 5), ws, bias, c, C, B - m0, to, ldl);
+    else
+        cl_finish<S, false>(acc, s_f + 4 * (lane >> 5), ws, bias, c, C, B - m0, to, ldl);
+}
+
+#define CLX_KB 36 /* pieces of depth of 128 samples that lie in LDS beside their scales */
+#define CLX_NT 512
+// Batches of more than 64 samples, D <= 32 CLX_KB: a workgroup keeps the codes of 128 samples in LDS and its wavefronts, each on its own, go
+// over groups of 64 classes: 8 matrix instructions on 2 pieces of weights, which come straight from memory a chunk of R
+// k-steps ahead, also across the end of a group.
+template <int R, typename OUT>
+__global__ void __launch_bounds__(CLX_NT, 2)
+cl_resident_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, const int8_t *__restrict__ wq,
+                   const float *__restrict__ ws, const float *__restrict__ bias, int64_t C, int kb, int B, float scale,
+                   OUT *__restrict__ out, int64_t ldl, int vec) {
+    constexpr int NW = CLX_NT / 64;
+    __shared__ __attribute__((aligned(16))) char s_x[CLX_KB * 4 * CL_PIECE];
+    __shared__ __attribute__((aligned(16))) float s_f[128];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int xblocks = (B + 31) / 32, n_sb = (B + 127) / 128;
+    const int chunks = (kb + R - 1) / R, last_step = (kb - (chunks - 1 > 1 ? chunks - 2 : 0) * R - R) * CL_PIECE; // kb >= R
+    const int groups = (int)((C + CL_GROUP - 1) / CL_GROUP);
+    // workgroup i runs on XCD i % 8: the classes are dealt to the XCDs in eight ranges; an XCD's workgroups divide its range, once
+    // for every 128 samples, into equal stretches, so that those at the same classes at the same time share its L2
+    const int xcd = blockIdx.x & 7, per_xcd = gridDim.x >> 3, j = blockIdx.x >> 3;
+    const int g_lo = (int)((int64_t)groups * xcd / 8), g_n = (int)((int64_t)groups * (xcd + 1) / 8) - g_lo;
+    const int64_t todo = (int64_t)g_n * n_sb;
+    int64_t at = todo * j / per_xcd;
+    const int64_t end = todo * (j + 1) / per_xcd;
+    while (at < end) {
+        const int sb = (int)(at / g_n), first = (int)(at - (int64_t)sb * g_n);
+        const int last = (int)(end - at < g_n - first ? first + (end - at) : g_n); // this stretch's part for sample block sb
+        at += last - first;
+        __syncthreads();
+        // through registers: reads from LDS that a direct load may have written would wait for every load of weights in flight
+        for (int p = wave; p < chunks * R * 4; p += NW) { // k-step t of sample block s at (4 t + s)
+            const int blk = sb * 4 + (p & 3) < xblocks ? sb * 4 + (p & 3) : xblocks - 1, t = p >> 2;
+            const int k = t < kb / R * R ? t : t - chunks * R + kb; // a last chunk that is short begins R before the end, with zeros
+            cl_i32x4 v = {0, 0, 0, 0};
+            if (k >= t / R * R) v = *(const cl_i32x4 *)(xq + ((int64_t)blk * kb + k) * CL_PIECE + lane * 16);
+            *(cl_i32x4 *)(s_x + p * CL_PIECE + lane * 16) = v;
         }
+        if (threadIdx.x < 128) s_f[threadIdx.x] = sb * 128 + (int)threadIdx.x < B ? scale * xs[sb * 128 + threadIdx.x] : 0.f;
+        __syncthreads();
+
+        int grp = first + wave;
+        if (grp >= last) continue;
+        cl_i32x4 w[R][2];
+        cl_i32x16 acc[4][2];
+        const int block_bytes = kb * CL_PIECE;
+        const int8_t *p = wq + (int64_t)(g_lo + grp) * 2 * block_bytes; // chunk of the group's first block that is loaded next
+#pragma unroll
+        for (int kk = 0; kk < R; ++kk)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) w[kk][q] = *(const cl_i32x4 *)(p + q * block_bytes + kk * CL_PIECE + lane * 16);
+        for (; grp < last; grp += NW) {
+            const int next = grp + NW < last ? grp + NW : grp;
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[s][q][r] = 0;
+            const char *xp = s_x + lane * 16;
+            for (int left = chunks; left > 0; --left, xp += R * 4 * CL_PIECE) {
+                p = left == 1 ? wq + (int64_t)(g_lo + next) * 2 * block_bytes : left == 2 ? p + last_step : p + R * CL_PIECE;
+                const int8_t *p1 = p + block_bytes;
+                cl_i32x4 x[2][4];
+#pragma unroll
+                for (int s = 0; s < 4; ++s) x[0][s] = *(const cl_i32x4 *)(xp + s * CL_PIECE);
+#pragma unroll
+                for (int kk = 0; kk < R; ++kk) {
+                    if (kk < R - 1)
+#pragma unroll
+                        for (int s = 0; s < 4; ++s) x[kk + 1 & 1][s] = *(const cl_i32x4 *)(xp + ((kk + 1) * 4 + s) * CL_PIECE);
+                    // a wavefront stands still until its load is accepted: one at a time, behind the four instructions that used the registers
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int s = 0; s < 4; ++s) acc[s][q] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[kk & 1][s], w[kk][q], acc[s][q], 0, 0, 0);
+                        __builtin_amdgcn_sched_barrier(0);
+                        w[kk][q] = *(const cl_i32x4 *)((q == 0 ? p : p1) + kk * CL_PIECE + lane * 16);
+                    }
+                }
+            }
+            const int64_t c = (int64_t)(g_lo + grp) * CL_GROUP + 2 * (lane & 31);
+            const int m0 = sb * 128 + 4 * (lane >> 5);
+            OUT *to = out + (int64_t)m0 * ldl + c;
+            if (vec && sb * 128 + 128 <= B && (int64_t)(g_lo + grp + 1) * CL_GROUP <= C)
+                cl_finish<4, true>(acc, s_f + 4 * (lane >> 5), ws, bias, c, C, B - m0, to, ldl);
+            else
+                cl_finish<4, false>(acc, s_f + 4 * (lane >> 5), ws, bias, c, C, B - m0, to, ldl);
+        }
+    }
 }
 
 template <typename OUT>
 static void cl_logits(const int8_t *xq, const float *xs, const int8_t *wq, const float *ws, const float *bias, int64_t C, int D, int B,
                       float scale, OUT *out, int64_t ldl, hipStream_t st) {
-    const int vec = ((uintptr_t)out | (uintptr_t)(ldl * sizeof(OUT))) % (4 * sizeof(OUT)) == 0, kb = (D + 31) / 32;
+    const int vec = ((uintptr_t)out | (uintptr_t)(ldl * sizeof(OUT))) % (2 * sizeof(OUT)) == 0, kb = (D + 31) / 32;
     const unsigned gx = (unsigned)ks_ceil_div(ks_ceil_div(C, CL_GROUP), CL_NT / 64);
     if (B <= 32)
         hipLaunchKernelGGL((cl_direct_kernel<1, OUT>), dim3(gx, 1), dim3(CL_NT), 0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, vec);
+    else if (B > 64 && kb >= 4 && kb <= CLX_KB)
+        hipLaunchKernelGGL((cl_resident_kernel<4, OUT>), dim3(256), dim3(CLX_NT), 0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, vec);
     else
         hipLaunchKernelGGL((cl_direct_kernel<2, OUT>), dim3(gx, (unsigned)ks_ceil_div(B, 64)), dim3(CL_NT), 0, st, xq, xs, wq, ws, bias, C,
                            kb, B, scale, out, ldl, vec);

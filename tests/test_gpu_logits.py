@@ -48,7 +48,7 @@ def rows_of(codes, n, D, classes):
     kb = (D + 31) // 32
     c = codes.cpu().numpy().reshape(-1, kb, 2, 32, 16).transpose(0, 3, 1, 2, 4).reshape(-1, 32, kb * 32)  # block, row, element
     if classes:
-        c = c.reshape(-1, 4, 32, kb * 32).transpose(0, 2, 1, 3)
+        c = c.reshape(-1, 2, 32, kb * 32).transpose(0, 2, 1, 3)
     c = c.reshape(-1, kb * 32)
     assert not c[n:].any() and not c[:, D:].any()
     return c[:n, :D]

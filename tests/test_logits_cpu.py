@@ -28,8 +28,8 @@ def test_header_symbols_are_exported(ks):
     assert all(hasattr(ks.lib(), n) and hasattr(ks, n) for n in names)
 
 
-@pytest.mark.parametrize("n,D,rows,classes", [(1, 1, 32, False), (1, 1, 128, True), (33, 64, 64, False), (128, 65, 128, True), (129, 512, 256, True),
-                                              (10_000, 128, 10_112, True)])
+@pytest.mark.parametrize("n,D,rows,classes", [(1, 1, 32, False), (1, 1, 64, True), (33, 64, 64, False), (128, 65, 128, True), (129, 512, 192, True),
+                                              (10_000, 128, 10_048, True)])
 def test_bytes_of_codes(ks, n, D, rows, classes):
     assert ks.class_codes_bytes(n, D, classes) == rows * ((D + 31) // 32 * 32)
 
