@@ -175,6 +175,14 @@ extern "C" int class_quantize_rows(const void *V, int dtype, int64_t n, int D, i
 // ------------------------------------------------------------------------------------------------
 // logits
 // ------------------------------------------------------------------------------------------------
+// workgroup barrier that waits for this wavefront's LDS accesses but, unlike __syncthreads(), not for loads in flight
+__device__ __forceinline__ void cl_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F); // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 __device__ __forceinline__ void cl_store(float *p, float v) { *p = v; }
 __device__ __forceinline__ void cl_store(uint16_t *p, float v) { *p = (uint16_t)ks_f2bf(v); }
 // whole pieces pass by the caches: nobody here reads a logit again, and the codes stay in them
@@ -196,31 +204,38 @@ __device__ __forceinline__ void cl_finish(const cl_i32x16 (&acc)[S][2], const fl
         sw[q] = WHOLE || c + q < C ? ws[c + q] : 0.f;
         b[q] = bias && (WHOLE || c + q < C) ? bias[c + q] : 0.f;
     }
-    asm volatile("" : "+s"(ldl)); // row addresses are formed here, not kept in registers from group to group
+    // row addresses and comparisons are made here, not kept in registers from call to call; scales and biases are waited for here, once
+    asm volatile("" : "+s"(ldl), "+v"(rows), "+v"(sw[0]), "+v"(sw[1]), "+v"(b[0]), "+v"(b[1]));
+    float4 f4[2][4]; // a sample block's scales are read while the one before is stored
 #pragma unroll
-    for (int s = 0; s < S; ++s)
+    for (int r4 = 0; r4 < 4; ++r4) f4[0][r4] = *(const float4 *)(f + r4 * 8);
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        if (s + 1 < S)
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) f4[s + 1 & 1][r4] = *(const float4 *)(f + (s + 1) * 32 + r4 * 8);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4) {
-            __builtin_amdgcn_sched_barrier(0);
-            const float4 f4 = *(const float4 *)(f + s * 32 + r4 * 8);
+            const float4 g = f4[s & 1][r4];
+            float v[4][2];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                    v[r][q] = fmaf((float)acc[s][q][r4 * 4 + r] * (r == 0 ? g.x : r == 1 ? g.y : r == 2 ? g.z : g.w), sw[q], b[q]);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float fr = r == 0 ? f4.x : r == 1 ? f4.y : r == 2 ? f4.z : f4.w;
-                float v[2];
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    v[q] = (float)acc[s][q][r4 * 4 + r] * fr * sw[q];
-                    if (bias) v[q] += b[q];
-                }
-                if (WHOLE) cl_store2(p, v[0], v[1]);
+                if (WHOLE) cl_store2(p, v[r][0], v[r][1]);
                 else if (s * 32 + r4 * 8 + r < rows) {
 #pragma unroll
                     for (int q = 0; q < 2; ++q)
-                        if (c + q < C) cl_store(p + q, v[q]);
+                        if (c + q < C) cl_store(p + q, v[r][q]);
                 }
                 p += r < 3 ? ldl : 5 * ldl; // the other half of the wavefront holds the four rows between
             }
         }
+    }
 }
 
 // One wavefront: 64 classes (the two blocks of a group) by 32 S samples, codes straight from memory.
@@ -280,6 +295,7 @@ cl_resident_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, 
     constexpr int NW = CLX_NT / 64;
     __shared__ __attribute__((aligned(16))) char s_x[CLX_KB * 4 * CL_PIECE];
     __shared__ __attribute__((aligned(16))) float s_f[128];
+    __shared__ int s_next; // group that the next wavefront to ask gets: of two on a SIMD the older one runs ahead
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int xblocks = (B + 31) / 32, n_sb = (B + 127) / 128;
     const int chunks = (kb + R - 1) / R, last_step = (kb - (chunks - 1 > 1 ? chunks - 2 : 0) * R - R) * CL_PIECE; // kb >= R
@@ -305,6 +321,7 @@ cl_resident_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, 
             *(cl_i32x4 *)(s_x + p * CL_PIECE + lane * 16) = v;
         }
         if (threadIdx.x < 128) s_f[threadIdx.x] = sb * 128 + (int)threadIdx.x < B ? scale * xs[sb * 128 + threadIdx.x] : 0.f;
+        if (threadIdx.x == 0) s_next = first + NW;
         __syncthreads();
 
         int grp = first + wave;
@@ -316,9 +333,17 @@ cl_resident_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, 
 #pragma unroll
         for (int kk = 0; kk < R; ++kk)
 #pragma unroll
-            for (int q = 0; q < 2; ++q) w[kk][q] = *(const cl_i32x4 *)(p + q * block_bytes + kk * CL_PIECE + lane * 16);
-        for (; grp < last; grp += NW) {
-            const int next = grp + NW < last ? grp + NW : grp;
+            for (int q = 0; q < 2; ++q) { // in the order in which they are used: the main loop's counted waits hold for these too
+            w[kk][q] = *(const cl_i32x4 *)(p + q * block_bytes + kk * CL_PIECE + lane * 16);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        cl_i32x4 x[2][4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) x[0][s] = *(const cl_i32x4 *)(s_x + lane * 16 + s * CL_PIECE);
+        while (grp < last) {
+            int got = 0;
+            if (lane == 0) got = atomicAdd(&s_next, 1);
+            const int next = __builtin_amdgcn_readfirstlane(got), load_next = next < last ? next : grp;
 #pragma unroll
             for (int s = 0; s < 4; ++s)
 #pragma unroll
@@ -327,16 +352,13 @@ cl_resident_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, 
                     for (int r = 0; r < 16; ++r) acc[s][q][r] = 0;
             const char *xp = s_x + lane * 16;
             for (int left = chunks; left > 0; --left, xp += R * 4 * CL_PIECE) {
-                p = left == 1 ? wq + (int64_t)(g_lo + next) * 2 * block_bytes : left == 2 ? p + last_step : p + R * CL_PIECE;
+                p = left == 1 ? wq + (int64_t)(g_lo + load_next) * 2 * block_bytes : left == 2 ? p + last_step : p + R * CL_PIECE;
                 const int8_t *p1 = p + block_bytes;
-                cl_i32x4 x[2][4];
-#pragma unroll
-                for (int s = 0; s < 4; ++s) x[0][s] = *(const cl_i32x4 *)(xp + s * CL_PIECE);
+                const char *xn = left == 1 ? s_x + lane * 16 : xp + R * 4 * CL_PIECE; // next chunk
 #pragma unroll
                 for (int kk = 0; kk < R; ++kk) {
-                    if (kk < R - 1)
 #pragma unroll
-                        for (int s = 0; s < 4; ++s) x[kk + 1 & 1][s] = *(const cl_i32x4 *)(xp + ((kk + 1) * 4 + s) * CL_PIECE);
+                    for (int s = 0; s < 4; ++s) x[kk + 1 & 1][s] = *(const cl_i32x4 *)((kk < R - 1 ? xp + (kk + 1) * 4 * CL_PIECE : xn) + s * CL_PIECE);
                     // a wavefront stands still until its load is accepted: one at a time, behind the four instructions that used the registers
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
@@ -355,7 +377,138 @@ cl_resident_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, 
                 cl_finish<4, true>(acc, s_f + 4 * (lane >> 5), ws, bias, c, C, B - m0, to, ldl);
             else
                 cl_finish<4, false>(acc, s_f + 4 * (lane >> 5), ws, bias, c, C, B - m0, to, ldl);
+            grp = next;
         }
+    }
+}
+
+// Deeper rows: as above, but the samples pass through LDS in chunks of four k-steps, which eight wavefronts with 64 classes each read at
+// the same time: three buffers, a barrier a chunk.  While chunk t is multiplied, the fragments are read one k-step ahead (the
+// last ones from chunk t + 1, which is there since the barrier), chunk t + 2 is written to LDS from registers and those are
+// requested anew for chunk t + 3.  The chunks run on from one tile of 512 classes by 128 samples to the next.
+template <typename OUT>
+__global__ void __launch_bounds__(CLX_NT, 2)
+cl_staged_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, const int8_t *__restrict__ wq,
+                 const float *__restrict__ ws, const float *__restrict__ bias, int64_t C, int kb, int B, float scale,
+                 OUT *__restrict__ out, int64_t ldl, int vec) {
+    constexpr int NW = CLX_NT / 64, R = 4, CHUNK = R * 4 * CL_PIECE;
+    __shared__ __attribute__((aligned(16))) char s_x[3 * CHUNK];
+    __shared__ __attribute__((aligned(16))) float s_f[NW][128];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int xblocks = (B + 31) / 32, n_sb = (B + 127) / 128;
+    const int chunks = (kb + R - 1) / R, last_step = (kb - (chunks - 1 > 1 ? chunks - 2 : 0) * R - R) * CL_PIECE; // kb >= R
+    const int groups = (int)((C + CL_GROUP - 1) / CL_GROUP), n_ct = (groups + NW - 1) / NW;
+    // workgroup i runs on XCD i % 8; an XCD has a range of the class tiles, and its workgroups take them for all samples before the
+    // next ones: what 32 of them read at a time are a few class tiles and the samples
+    const int xcd = blockIdx.x & 7, per_xcd = gridDim.x >> 3, j = blockIdx.x >> 3;
+    const int c_lo = (int)((int64_t)n_ct * xcd / 8), c_n = (int)((int64_t)n_ct * (xcd + 1) / 8) - c_lo;
+    int64_t left = (int64_t)c_n * n_sb - j; // tiles from this one on, of this and the XCD's other workgroups
+    if (left <= 0) return;
+    const int step_c = per_xcd / n_sb, step_s = per_xcd % n_sb; // from one of this workgroup's tiles to its next
+    int ct = c_lo + j / n_sb, sb = j % n_sb;
+
+    // samples: this wavefront moves two of a chunk's 16 pieces, k-step wave / 2 of sample blocks i and i + 1
+    int64_t r_left = left;
+    int r_sb = sb, r_c = 0; // chunk that is requested next
+    const int x_kk = wave >> 1, x_s = (wave & 1) * 2;
+    const auto request = [&](int i) __attribute__((always_inline)) {
+        const int blk = r_sb * 4 + x_s + i < xblocks ? r_sb * 4 + x_s + i : xblocks - 1;
+        const int k = (r_c < chunks - 1 ? r_c * R : kb - R) + x_kk;
+        return *(const cl_i32x4 *)(xq + ((int64_t)blk * kb + k) * CL_PIECE + lane * 16);
+    };
+    const auto requested = [&]() __attribute__((always_inline)) { // behind the last tile: the same again, read by nobody
+        if (++r_c == chunks) {
+            r_c = 0;
+            if (r_left > per_xcd) {
+                r_left -= per_xcd;
+                r_sb += step_s;
+                if (r_sb >= n_sb) r_sb -= n_sb;
+            }
+        }
+    };
+    // chunk c: one that is short begins R before the end, with zeros for what the one before had
+    const auto place = [&](cl_i32x4 v, int i, int c, char *to) __attribute__((always_inline)) {
+        if (c == chunks - 1 && kb - R + x_kk < c * R) v = cl_i32x4{0, 0, 0, 0};
+        *(cl_i32x4 *)(to + (x_kk * 4 + x_s + i) * CL_PIECE + lane * 16) = v;
+    };
+    const int block_bytes = kb * CL_PIECE;
+    const auto weights = [&](int tile) __attribute__((always_inline)) { // of this wavefront's classes in a tile; beyond the last group: that one
+        const int g = tile * NW + wave;
+        return wq + (int64_t)(g < groups ? g : groups - 1) * 2 * block_bytes;
+    };
+    char *b0 = s_x, *b1 = s_x + CHUNK, *b2 = s_x + 2 * CHUNK; // chunks t, t + 1, t + 2
+    cl_i32x4 held[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) place(request(i), i, r_c, t ? b1 : b0);
+        requested();
+    }
+    held[0] = request(0);
+    held[1] = request(1);
+    int p_c = r_c; // its chunk
+    requested();
+    cl_i32x4 w[R][2], x[2][4];
+    const int8_t *p = weights(ct);
+#pragma unroll
+    for (int kk = 0; kk < R; ++kk)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) { // in the order in which they are used: the main loop's counted waits hold for these too
+            w[kk][q] = *(const cl_i32x4 *)(p + q * block_bytes + kk * CL_PIECE + lane * 16);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    cl_barrier();
+#pragma unroll
+    for (int s = 0; s < 4; ++s) x[0][s] = *(const cl_i32x4 *)(b0 + s * CL_PIECE + lane * 16);
+    for (; left > 0; left -= per_xcd) {
+        int next_ct = ct + step_c, next_sb = sb + step_s;
+        if (next_sb >= n_sb) { next_sb -= n_sb; ++next_ct; }
+        if (left <= per_xcd) next_ct = ct;
+        cl_i32x16 acc[4][2];
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[s][q][r] = 0;
+        for (int c = chunks; c > 0; --c) {
+            p = c == 1 ? weights(next_ct) : c == 2 ? p + last_step : p + R * CL_PIECE;
+            const int8_t *p1 = p + block_bytes;
+            cl_barrier(); // chunk t + 1 is whole, and nobody reads chunk t - 1 any more
+#pragma unroll
+            for (int kk = 0; kk < R; ++kk) {
+#pragma unroll
+                for (int s = 0; s < 4; ++s) x[kk + 1 & 1][s] = *(const cl_i32x4 *)((kk < R - 1 ? b0 + (kk + 1) * 4 * CL_PIECE : b1) + s * CL_PIECE + lane * 16);
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) acc[s][q] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[kk & 1][s], w[kk][q], acc[s][q], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    w[kk][q] = *(const cl_i32x4 *)((q == 0 ? p : p1) + kk * CL_PIECE + lane * 16);
+                    if (kk == 1) {
+                        place(held[q], q, p_c, b2);
+                        held[q] = request(q);
+                    }
+                }
+            }
+            p_c = r_c;
+            requested();
+            char *const b = b0;
+            b0 = b1;
+            b1 = b2;
+            b2 = b;
+        }
+        for (int i = lane; i < 128; i += 64) s_f[wave][i] = sb * 128 + i < B ? scale * xs[sb * 128 + i] : 0.f;
+        const int64_t c0 = ((int64_t)ct * NW + wave) * CL_GROUP, c = c0 + 2 * (lane & 31);
+        const int m0 = sb * 128 + 4 * (lane >> 5);
+        OUT *to = out + (int64_t)m0 * ldl + c;
+        if (vec && sb * 128 + 128 <= B && c0 + CL_GROUP <= C)
+            cl_finish<4, true>(acc, s_f[wave] + 4 * (lane >> 5), ws, bias, c, C, B - m0, to, ldl);
+        else
+            cl_finish<4, false>(acc, s_f[wave] + 4 * (lane >> 5), ws, bias, c, C, B - m0, to, ldl);
+        ct = next_ct;
+        sb = next_sb;
     }
 }
 
@@ -368,6 +521,8 @@ static void cl_logits(const int8_t *xq, const float *xs, const int8_t *wq, const
         hipLaunchKernelGGL((cl_direct_kernel<1, OUT>), dim3(gx, 1), dim3(CL_NT), 0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, vec);
     else if (B > 64 && kb >= 4 && kb <= CLX_KB)
         hipLaunchKernelGGL((cl_resident_kernel<4, OUT>), dim3(256), dim3(CLX_NT), 0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, vec);
+    else if (B > 64 && kb > CLX_KB)
+        hipLaunchKernelGGL(cl_staged_kernel<OUT>, dim3(256), dim3(CLX_NT), 0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, vec);
     else
         hipLaunchKernelGGL((cl_direct_kernel<2, OUT>), dim3(gx, (unsigned)ks_ceil_div(B, 64)), dim3(CL_NT), 0, st, xq, xs, wq, ws, bias, C,
                            kb, B, scale, out, ldl, vec);
