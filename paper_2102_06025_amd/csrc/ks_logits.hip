@@ -3,6 +3,7 @@
 // penalties, biases and masks that requests bring.
 #include "../../include/class_logits.h"
 #include "ks_common.h"
+#include <type_traits>
 
 typedef int32_t cl_i32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t cl_i32x16 __attribute__((ext_vector_type(16)));
@@ -192,6 +193,14 @@ __device__ __forceinline__ void cl_store2(float *p, float v0, float v1) {
 }
 __device__ __forceinline__ void cl_store2(uint16_t *p, float v0, float v1) { __builtin_nontemporal_store(ks_pack_bf2(v0, v1), (uint32_t *)p); }
 
+__device__ __forceinline__ void cl_store2(__amdgpu_buffer_rsrc_t to, uint32_t off, float v0, float v1, const float *) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(v0), __float_as_uint(v1)}, to, off, 0, 2 /* nt */);
+}
+__device__ __forceinline__ void cl_store2(__amdgpu_buffer_rsrc_t to, uint32_t off, float v0, float v1, const uint16_t *) {
+    __builtin_amdgcn_raw_buffer_store_b32(ks_pack_bf2(v0, v1), to, off, 0, 2 /* nt */);
+}
+
 // Scales, bias, type and store of 32 S samples by 64 classes.  A lane of the result holds one column of each of the two blocks, which
 // are two consecutive classes.  f: scales of the lane's samples (LDS), p: logit of its first sample and first class, rows: samples
 // from that one on.  WHOLE: everything exists and pairs of classes are aligned.
@@ -337,9 +346,9 @@ cl_resident_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, 
             w[kk][q] = *(const cl_i32x4 *)(p + q * block_bytes + kk * CL_PIECE + lane * 16);
             __builtin_amdgcn_sched_barrier(0);
         }
-        cl_i32x4 x[2][4];
+        cl_i32x4 x[4];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) x[0][s] = *(const cl_i32x4 *)(s_x + lane * 16 + s * CL_PIECE);
+        for (int s = 0; s < 4; ++s) x[s] = *(const cl_i32x4 *)(s_x + lane * 16 + s * CL_PIECE);
         while (grp < last) {
             int got = 0;
             if (lane == 0) got = atomicAdd(&s_next, 1);
@@ -358,15 +367,15 @@ cl_resident_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, 
 #pragma unroll
                 for (int kk = 0; kk < R; ++kk) {
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) x[kk + 1 & 1][s] = *(const cl_i32x4 *)((kk < R - 1 ? xp + (kk + 1) * 4 * CL_PIECE : xn) + s * CL_PIECE);
-                    // a wavefront stands still until its load is accepted: one at a time, behind the four instructions that used the registers
+                    for (int s = 0; s < 4; ++s) {
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
+                        for (int q = 0; q < 2; ++q) acc[s][q] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[s], w[kk][q], acc[s][q], 0, 0, 0);
                         __builtin_amdgcn_sched_barrier(0);
+                        x[s] = *(const cl_i32x4 *)((kk < R - 1 ? xp + (kk + 1) * 4 * CL_PIECE : xn) + s * CL_PIECE);
+                        if (s == 3)
 #pragma unroll
-                        for (int s = 0; s < 4; ++s) acc[s][q] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[kk & 1][s], w[kk][q], acc[s][q], 0, 0, 0);
+                            for (int q = 0; q < 2; ++q) w[kk][q] = *(const cl_i32x4 *)((q == 0 ? p : p1) + kk * CL_PIECE + lane * 16);
                         __builtin_amdgcn_sched_barrier(0);
-                        w[kk][q] = *(const cl_i32x4 *)((q == 0 ? p : p1) + kk * CL_PIECE + lane * 16);
                     }
                 }
             }
@@ -380,6 +389,154 @@ cl_resident_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, 
             grp = next;
         }
     }
+}
+
+// Rows of up to 32 KB elements: a wavefront keeps the codes of 64 classes in registers, a workgroup those of up to 256 samples in LDS, and
+// the samples go past 32 at a time: 2 KB matrix instructions a block, with the scales, conversions and stores of the block before in
+// between.  (Per SIMD a matrix instruction of 32 clocks leaves room for four others; logits that are stored a row at a time do
+// not hold up the loads behind them as a whole group's do.)  During a group's last block each piece of codes is replaced, when it
+// has been used, by the next group's.
+template <int KB, typename OUT>
+__global__ void __launch_bounds__(CLX_NT, 2)
+cl_steady_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, const int8_t *__restrict__ wq,
+                 const float *__restrict__ ws, const float *__restrict__ bias, int64_t C, int kb, int B, float scale,
+                 OUT *__restrict__ out, int64_t ldl, int tile) { // tile: sample blocks at a time, even, at most 8
+    constexpr int NW = CLX_NT / 64;
+    __shared__ __attribute__((aligned(16))) char s_x[8 * KB * CL_PIECE];
+    __shared__ __attribute__((aligned(16))) float s_f[256];
+    __shared__ int s_next; // group that the next wavefront to ask gets: of two on a SIMD the older one runs ahead
+    const uint32_t row_bytes = (uint32_t)(ldl * sizeof(OUT)); // 32 rows: less than 2^31 bytes
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half4 = 4 * (lane >> 5);
+    const int xblocks = (B + 31) / 32, n_sb = (xblocks + tile - 1) / tile;
+    const int groups = (int)((C + CL_GROUP - 1) / CL_GROUP);
+    // the division of the work as in cl_resident_kernel
+    const int xcd = blockIdx.x & 7, per_xcd = gridDim.x >> 3, j = blockIdx.x >> 3;
+    const int g_lo = (int)((int64_t)groups * xcd / 8), g_n = (int)((int64_t)groups * (xcd + 1) / 8) - g_lo;
+    const int64_t todo = (int64_t)g_n * n_sb;
+    int64_t at = todo * j / per_xcd;
+    const int64_t end = todo * (j + 1) / per_xcd;
+    while (at < end) {
+        const int sb = (int)(at / g_n), first = (int)(at - (int64_t)sb * g_n);
+        const int last = (int)(end - at < g_n - first ? first + (end - at) : g_n); // this stretch's part for samples sb
+        at += last - first;
+        __syncthreads();
+        for (int p = wave; p < tile * KB; p += NW) { // k-step k of block i at (KB i + k), 0 beyond the depth
+            const int blk = sb * tile + p / KB < xblocks ? sb * tile + p / KB : xblocks - 1, k = p % KB;
+            cl_i32x4 v = {0, 0, 0, 0};
+            if (k < kb) v = *(const cl_i32x4 *)(xq + ((int64_t)blk * kb + k) * CL_PIECE + lane * 16);
+            *(cl_i32x4 *)(s_x + p * CL_PIECE + lane * 16) = v;
+        }
+        if ((int)threadIdx.x < tile * 32) {
+            const int m = sb * tile * 32 + threadIdx.x;
+            s_f[threadIdx.x] = m < B ? scale * xs[m] : 0.f;
+        }
+        if (threadIdx.x == 0) s_next = first + NW;
+        __syncthreads();
+
+        int grp = first + wave;
+        if (grp >= last) continue;
+        const int block_bytes = kb * CL_PIECE;
+        const auto group_codes = [&](int g) __attribute__((always_inline)) {
+            return __builtin_amdgcn_make_buffer_rsrc((void *)(wq + (int64_t)(g_lo + g) * 2 * block_bytes), 0, 2 * block_bytes, 0x00020000);
+        };
+        const auto codes = [&](__amdgpu_buffer_rsrc_t p, int k, int q) __attribute__((always_inline)) { // beyond the depth: another piece, or 0
+            return __builtin_bit_cast(cl_i32x4, __builtin_amdgcn_raw_buffer_load_b128(p, lane * 16 + k % 4 * CL_PIECE, q * block_bytes + k / 4 * 4 * CL_PIECE, 0));
+        };
+        cl_i32x4 w[KB][2], x[4];
+        cl_i32x16 acc[2][2];
+        {
+            const __amdgpu_buffer_rsrc_t p = group_codes(grp);
+#pragma unroll
+            for (int k = 0; k < KB; ++k)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) { // in the order in which they are used: the main loop's counted waits hold for these too
+                    w[k][q] = codes(p, k, q);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = *(const cl_i32x4 *)(s_x + k * CL_PIECE + lane * 16);
+        // The block that is finished while the next one is multiplied: its logits go through a buffer that ends behind the last
+        // sample's row, and classes that do not exist lie behind its end; the hardware leaves out what lies there, so that
+        // every row is one store on every way.  None yet: a buffer of no bytes.
+        __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc(out, 0, 0, 0x00020000);
+        uint32_t off = 0;
+        float sw[2] = {0.f, 0.f}, b[2] = {0.f, 0.f};
+        float4 f4 = make_float4(0.f, 0.f, 0.f, 0.f), f4_next;
+        const auto finish = [&](const cl_i32x16 (&a)[2], int r, const float *f) __attribute__((always_inline)) { // one row of each half
+            if (r % 4 == 1 && r < 12) f4_next = *(const float4 *)(f + (r / 4 + 1) * 8);
+            const float g = r % 4 == 0 ? f4.x : r % 4 == 1 ? f4.y : r % 4 == 2 ? f4.z : f4.w;
+            const float v0 = fmaf((float)a[0][r] * g, sw[0], b[0]), v1 = fmaf((float)a[1][r] * g, sw[1], b[1]);
+            cl_store2(to, off, v0, v1, (const OUT *)nullptr);
+            off += r % 4 < 3 ? row_bytes : 5 * row_bytes;
+            asm volatile("" : "+v"(off)); // one register, not sixteen that are kept for every block
+            if (r % 4 == 3) f4 = f4_next;
+        };
+        while (grp < last) {
+            int got = 0;
+            if (lane == 0) got = atomicAdd(&s_next, 1);
+            const int next = __builtin_amdgcn_readfirstlane(got);
+            const __amdgpu_buffer_rsrc_t p_next = group_codes(next < last ? next : grp);
+            const int64_t c0 = (int64_t)(g_lo + grp) * CL_GROUP, c = c0 + 2 * (lane & 31);
+            float nsw[2], nb[2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                nsw[q] = ws[c + q < C ? c + q : C - 1];
+                nb[q] = bias ? bias[c + q < C ? c + q : C - 1] : 0.f;
+            }
+            const uint32_t off0 = c + 1 < C ? half4 * row_bytes + 2 * (lane & 31) * (uint32_t)sizeof(OUT) : 0x80000000u;
+            const auto block = [&](int blk, cl_i32x16 (&a)[2], const cl_i32x16 (&before)[2], auto reload) __attribute__((always_inline)) {
+                const char *xp = s_x + blk * (KB * CL_PIECE) + lane * 16, *xn = reload ? s_x + lane * 16 : xp + KB * CL_PIECE;
+                const float *f = s_f + (blk ? blk - 1 : tile - 1) * 32 + half4; // of the block before
+#pragma unroll
+                for (int k = 0; k < KB; ++k) {
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        if (k == 0) a[q] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[0], w[0][q], cl_i32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0}, 0, 0, 0);
+                        else a[q] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[k & 3], w[k][q], a[q], 0, 0, 0);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    x[k & 3] = *(const cl_i32x4 *)(k + 4 < KB ? xp + (k + 4) * CL_PIECE : xn + (k + 4 - KB) * CL_PIECE);
+                    if (reload)
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) w[k][q] = codes(p_next, k, q);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (r * KB / 16 == k) finish(before, r, f);
+                }
+                const int m0 = (sb * tile + blk) * 32, rows = B - m0 < 32 ? B - m0 : 32;
+                to = __builtin_amdgcn_make_buffer_rsrc(out + (int64_t)m0 * ldl + c0, 0, rows > 0 ? (int)((rows - 1) * row_bytes + CL_GROUP * sizeof(OUT)) : 0, 0x00020000);
+                off = off0;
+#pragma unroll
+                for (int q = 0; q < 2; ++q) { sw[q] = nsw[q]; b[q] = nb[q]; }
+                f4 = *(const float4 *)(s_f + blk * 32 + half4);
+            };
+            for (int i = 0; i + 2 < tile; i += 2) {
+                block(i, acc[0], acc[1], std::false_type());
+                block(i + 1, acc[1], acc[0], std::false_type());
+            }
+            block(tile - 2, acc[0], acc[1], std::false_type());
+            block(tile - 1, acc[1], acc[0], std::true_type());
+            grp = next;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) finish(acc[1], r, s_f + (tile - 1) * 32 + half4);
+    }
+    // the last of an odd number of classes has no pair to be stored with: a wavefront per sample
+    if (C & 1)
+        for (int m = blockIdx.x * NW + wave; m < B; m += gridDim.x * NW) {
+            const int64_t wb = (C - 1) / CL_GROUP * 2; // C is odd: slot (C - 1) % 64 / 2 of the group's first block
+            int sum = 0;
+            if (lane < 2 * kb) {
+                const cl_i32x4 xv = *(const cl_i32x4 *)(xq + ((int64_t)(m / 32) * kb + lane / 2) * CL_PIECE + ((lane & 1) * 32 + m % 32) * 16);
+                const cl_i32x4 wv = *(const cl_i32x4 *)(wq + (wb * kb + lane / 2) * CL_PIECE + ((lane & 1) * 32 + (int)((C - 1) % CL_GROUP / 2)) * 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_sdot4(xv[e], wv[e], sum, false);
+            }
+            sum = ks_wave_sum_i(sum);
+            if (lane == 0) cl_store(out + (int64_t)m * ldl + C - 1, fmaf((float)sum * (scale * xs[m]), ws[C - 1], bias ? bias[C - 1] : 0.f));
+        }
 }
 
 // Deeper rows: as above, but the samples pass through LDS in chunks of four k-steps, which eight wavefronts with 64 classes each read at
@@ -519,7 +676,11 @@ static void cl_logits(const int8_t *xq, const float *xs, const int8_t *wq, const
     const unsigned gx = (unsigned)ks_ceil_div(ks_ceil_div(C, CL_GROUP), CL_NT / 64);
     if (B <= 32)
         hipLaunchKernelGGL((cl_direct_kernel<1, OUT>), dim3(gx, 1), dim3(CL_NT), 0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, vec);
-    else if (B > 64 && kb >= 4 && kb <= CLX_KB)
+    else if (B > 64 && vec && kb <= 16 && ldl * (int64_t)sizeof(OUT) < (1 << 26)) {
+        const int xblocks = (B + 31) / 32, tiles = (xblocks + 7) / 8, tile = ((xblocks + tiles - 1) / tiles + 1) / 2 * 2;
+        hipLaunchKernelGGL((kb <= 4 ? cl_steady_kernel<4, OUT> : kb <= 8 ? cl_steady_kernel<8, OUT> : kb <= 12 ? cl_steady_kernel<12, OUT> : cl_steady_kernel<16, OUT>),
+                           dim3(256), dim3(CLX_NT), 0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, tile);
+    } else if (B > 64 && kb >= 4 && kb <= CLX_KB)
         hipLaunchKernelGGL((cl_resident_kernel<4, OUT>), dim3(256), dim3(CLX_NT), 0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, vec);
     else if (B > 64 && kb > CLX_KB)
         hipLaunchKernelGGL(cl_staged_kernel<OUT>, dim3(256), dim3(CLX_NT), 0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, vec);
