@@ -186,64 +186,78 @@ __device__ __forceinline__ void cl_barrier() {
 
 __device__ __forceinline__ void cl_store(float *p, float v) { *p = v; }
 __device__ __forceinline__ void cl_store(uint16_t *p, float v) { *p = (uint16_t)ks_f2bf(v); }
-// whole pieces pass by the caches: nobody here reads a logit again, and the codes stay in them
-__device__ __forceinline__ void cl_store2(float *p, float v0, float v1) {
-    typedef float f32x2 __attribute__((ext_vector_type(2)));
-    __builtin_nontemporal_store(f32x2{v0, v1}, (f32x2 *)p);
-}
-__device__ __forceinline__ void cl_store2(uint16_t *p, float v0, float v1) { __builtin_nontemporal_store(ks_pack_bf2(v0, v1), (uint32_t *)p); }
-
+// Pairs of classes pass by the caches (aux bit 1): nobody here reads a logit again, and the codes stay in them.
 __device__ __forceinline__ void cl_store2(__amdgpu_buffer_rsrc_t to, uint32_t off, float v0, float v1, const float *) {
     typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-    __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(v0), __float_as_uint(v1)}, to, off, 0, 2 /* nt */);
+    __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(v0), __float_as_uint(v1)}, to, off, 0, 2);
 }
 __device__ __forceinline__ void cl_store2(__amdgpu_buffer_rsrc_t to, uint32_t off, float v0, float v1, const uint16_t *) {
-    __builtin_amdgcn_raw_buffer_store_b32(ks_pack_bf2(v0, v1), to, off, 0, 2 /* nt */);
+    __builtin_amdgcn_raw_buffer_store_b32(ks_pack_bf2(v0, v1), to, off, 0, 2);
 }
+// Logits of 32 samples from m0 on by the 64 classes from c0 on as a buffer that ends with the last sample's row: what lies behind its
+// end (samples that do not exist, and classes: CL_NO_CLASS) the hardware leaves out, so that every row is one store on every
+// way.  32 rows are less than 2^31 bytes (cl_logits sees to that).
+template <typename OUT> __device__ __forceinline__ __amdgpu_buffer_rsrc_t cl_rows_of(OUT *out, int64_t ldl, int m0, int64_t c0, int B) {
+    const int rows = B - m0 < 32 ? B - m0 : 32;
+    return __builtin_amdgcn_make_buffer_rsrc(out + (int64_t)m0 * ldl + c0, 0, rows > 0 ? (int)((rows - 1) * (uint32_t)(ldl * sizeof(OUT)) + CL_GROUP * sizeof(OUT)) : 0, 0x00020000);
+}
+#define CL_NO_CLASS 0x80000000u
 
-// Scales, bias, type and store of 32 S samples by 64 classes.  A lane of the result holds one column of each of the two blocks, which
-// are two consecutive classes.  f: scales of the lane's samples (LDS), p: logit of its first sample and first class, rows: samples
-// from that one on.  WHOLE: everything exists and pairs of classes are aligned.
-template <int S, bool WHOLE, typename OUT>
+// Scales, bias, type and store of 32 S samples from m0 on by the 64 classes from c0 on.  A lane of the result holds one column of each of
+// the two blocks, which are two consecutive classes.  f: scales of the samples (LDS).  vec: pairs of classes are aligned.
+template <int S, typename OUT>
 __device__ __forceinline__ void cl_finish(const cl_i32x16 (&acc)[S][2], const float *f, const float *__restrict__ ws,
-                                          const float *__restrict__ bias, int64_t c, int64_t C, int rows, OUT *p, int64_t ldl) {
+                                          const float *__restrict__ bias, int64_t c0, int64_t C, int m0, int B, OUT *out, int64_t ldl, int vec) {
+    const int lane = threadIdx.x & 63, half4 = 4 * (lane >> 5);
+    const int64_t c = c0 + 2 * (lane & 31);
     float sw[2], b[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        sw[q] = WHOLE || c + q < C ? ws[c + q] : 0.f;
-        b[q] = bias && (WHOLE || c + q < C) ? bias[c + q] : 0.f;
+        sw[q] = ws[c + q < C ? c + q : C - 1];
+        b[q] = bias ? bias[c + q < C ? c + q : C - 1] : 0.f;
     }
-    // row addresses and comparisons are made here, not kept in registers from call to call; scales and biases are waited for here, once
-    asm volatile("" : "+s"(ldl), "+v"(rows), "+v"(sw[0]), "+v"(sw[1]), "+v"(b[0]), "+v"(b[1]));
-    float4 f4[2][4]; // a sample block's scales are read while the one before is stored
+    // waited for here, once: a load left open on some way would be waited for, with all that followed it, where its register is next used
+    asm volatile("" : "+v"(sw[0]), "+v"(sw[1]), "+v"(b[0]), "+v"(b[1]));
+    const auto value = [&](int s, int r, int q, float4 g) __attribute__((always_inline)) {
+        return fmaf((float)acc[s][q][r] * (r % 4 == 0 ? g.x : r % 4 == 1 ? g.y : r % 4 == 2 ? g.z : g.w), sw[q], b[q]);
+    };
+    if (vec) {
+        const uint32_t row_bytes = (uint32_t)(ldl * sizeof(OUT)), off0 = c + 1 < C ? half4 * row_bytes + 2 * (lane & 31) * (uint32_t)sizeof(OUT) : CL_NO_CLASS;
+        float4 f4[2][4]; // a sample block's scales are read while the one before is stored
 #pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) f4[0][r4] = *(const float4 *)(f + r4 * 8);
+        for (int r4 = 0; r4 < 4; ++r4) f4[0][r4] = *(const float4 *)(f + half4 + r4 * 8);
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-        if (s + 1 < S)
+        for (int s = 0; s < S; ++s) {
+            if (s + 1 < S)
 #pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4) f4[s + 1 & 1][r4] = *(const float4 *)(f + (s + 1) * 32 + r4 * 8);
-        __builtin_amdgcn_sched_barrier(0);
+                for (int r4 = 0; r4 < 4; ++r4) f4[s + 1 & 1][r4] = *(const float4 *)(f + half4 + (s + 1) * 32 + r4 * 8);
+            __builtin_amdgcn_sched_barrier(0);
+            const __amdgpu_buffer_rsrc_t to = cl_rows_of(out, ldl, m0 + s * 32, c0, B);
+            uint32_t off = off0;
 #pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-            const float4 g = f4[s & 1][r4];
-            float v[4][2];
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int q = 0; q < 2; ++q)
-                    v[r][q] = fmaf((float)acc[s][q][r4 * 4 + r] * (r == 0 ? g.x : r == 1 ? g.y : r == 2 ? g.z : g.w), sw[q], b[q]);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                if (WHOLE) cl_store2(p, v[r][0], v[r][1]);
-                else if (s * 32 + r4 * 8 + r < rows) {
-#pragma unroll
-                    for (int q = 0; q < 2; ++q)
-                        if (c + q < C) cl_store(p + q, v[r][q]);
-                }
-                p += r < 3 ? ldl : 5 * ldl; // the other half of the wavefront holds the four rows between
+            for (int r = 0; r < 16; ++r) {
+                cl_store2(to, off, value(s, r, 0, f4[s & 1][r / 4]), value(s, r, 1, f4[s & 1][r / 4]), (const OUT *)nullptr);
+                off += r % 4 < 3 ? row_bytes : 5 * row_bytes; // the other half of the wavefront holds the four rows between
+                asm volatile("" : "+v"(off));                 // one register, not sixteen that are kept from call to call
             }
         }
+    }
+    if (!vec || c0 + CL_GROUP > C) { // element by element: all of them, or the last of an odd number of classes
+        int rows = B - m0 - half4;
+        asm volatile("" : "+v"(rows), "+s"(ldl));
+        OUT *p = out + (int64_t)(m0 + half4) * ldl + c;
+        if (!vec || (c == C - 1))
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float4 g = *(const float4 *)(f + half4 + s * 32 + r / 4 * 8);
+                    if (s * 32 + r / 4 * 8 + r % 4 < rows) {
+                        if (c < C) cl_store(p, value(s, r, 0, g));
+                        if (c + 1 < C && !vec) cl_store(p + 1, value(s, r, 1, g));
+                    }
+                    p += r % 4 < 3 ? ldl : 5 * ldl;
+                }
     }
 }
 
@@ -282,13 +296,7 @@ cl_direct_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
 #pragma unroll
             for (int q = 0; q < 2; ++q) acc[s][q] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[s], w[q], acc[s][q], 0, 0, 0);
     }
-    const int64_t c = grp * CL_GROUP + 2 * (lane & 31);
-    const int m0 = sb * 32 + 4 * (lane >> 5);
-    OUT *to = out + (int64_t)m0 * ldl + c;
-    if (vec && sb * 32 + 32 * S <= B && (grp + 1) * CL_GROUP <= C)
-        cl_finish<S, true>(acc, s_f + 4 * (lane >> 5), ws, bias, c, C, B - m0, to, ldl);
-    else
-        cl_finish<S, false>(acc, s_f + 4 * (lane >> 5), ws, bias, c, C, B - m0, to, ldl);
+    cl_finish<S>(acc, s_f, ws, bias, grp * CL_GROUP, C, sb * 32, B, out, ldl, vec);
 }
 
 #define CLX_KB 36 /* pieces of depth of 128 samples that lie in LDS beside their scales */
@@ -379,13 +387,7 @@ cl_resident_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, 
                     }
                 }
             }
-            const int64_t c = (int64_t)(g_lo + grp) * CL_GROUP + 2 * (lane & 31);
-            const int m0 = sb * 128 + 4 * (lane >> 5);
-            OUT *to = out + (int64_t)m0 * ldl + c;
-            if (vec && sb * 128 + 128 <= B && (int64_t)(g_lo + grp + 1) * CL_GROUP <= C)
-                cl_finish<4, true>(acc, s_f + 4 * (lane >> 5), ws, bias, c, C, B - m0, to, ldl);
-            else
-                cl_finish<4, false>(acc, s_f + 4 * (lane >> 5), ws, bias, c, C, B - m0, to, ldl);
+            cl_finish<4>(acc, s_f, ws, bias, (int64_t)(g_lo + grp) * CL_GROUP, C, sb * 128, B, out, ldl, vec);
             grp = next;
         }
     }
@@ -456,9 +458,7 @@ cl_steady_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) x[k] = *(const cl_i32x4 *)(s_x + k * CL_PIECE + lane * 16);
-        // The block that is finished while the next one is multiplied: its logits go through a buffer that ends behind the last
-        // sample's row, and classes that do not exist lie behind its end; the hardware leaves out what lies there, so that
-        // every row is one store on every way.  None yet: a buffer of no bytes.
+        // the block that is finished while the next one is multiplied; none yet: a buffer of no bytes
         __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc(out, 0, 0, 0x00020000);
         uint32_t off = 0;
         float sw[2] = {0.f, 0.f}, b[2] = {0.f, 0.f};
@@ -484,7 +484,7 @@ cl_steady_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
                 nsw[q] = ws[c + q < C ? c + q : C - 1];
                 nb[q] = bias ? bias[c + q < C ? c + q : C - 1] : 0.f;
             }
-            const uint32_t off0 = c + 1 < C ? half4 * row_bytes + 2 * (lane & 31) * (uint32_t)sizeof(OUT) : 0x80000000u;
+            const uint32_t off0 = c + 1 < C ? half4 * row_bytes + 2 * (lane & 31) * (uint32_t)sizeof(OUT) : CL_NO_CLASS;
             const auto block = [&](int blk, cl_i32x16 (&a)[2], const cl_i32x16 (&before)[2], auto reload) __attribute__((always_inline)) {
                 const char *xp = s_x + blk * (KB * CL_PIECE) + lane * 16, *xn = reload ? s_x + lane * 16 : xp + KB * CL_PIECE;
                 const float *f = s_f + (blk ? blk - 1 : tile - 1) * 32 + half4; // of the block before
@@ -505,8 +505,7 @@ cl_steady_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
                     for (int r = 0; r < 16; ++r)
                         if (r * KB / 16 == k) finish(before, r, f);
                 }
-                const int m0 = (sb * tile + blk) * 32, rows = B - m0 < 32 ? B - m0 : 32;
-                to = __builtin_amdgcn_make_buffer_rsrc(out + (int64_t)m0 * ldl + c0, 0, rows > 0 ? (int)((rows - 1) * row_bytes + CL_GROUP * sizeof(OUT)) : 0, 0x00020000);
+                to = cl_rows_of(out, ldl, (sb * tile + blk) * 32, c0, B);
                 off = off0;
 #pragma unroll
                 for (int q = 0; q < 2; ++q) { sw[q] = nsw[q]; b[q] = nb[q]; }
@@ -657,13 +656,8 @@ cl_staged_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
             b2 = b;
         }
         for (int i = lane; i < 128; i += 64) s_f[wave][i] = sb * 128 + i < B ? scale * xs[sb * 128 + i] : 0.f;
-        const int64_t c0 = ((int64_t)ct * NW + wave) * CL_GROUP, c = c0 + 2 * (lane & 31);
-        const int m0 = sb * 128 + 4 * (lane >> 5);
-        OUT *to = out + (int64_t)m0 * ldl + c;
-        if (vec && sb * 128 + 128 <= B && c0 + CL_GROUP <= C)
-            cl_finish<4, true>(acc, s_f[wave] + 4 * (lane >> 5), ws, bias, c, C, B - m0, to, ldl);
-        else
-            cl_finish<4, false>(acc, s_f[wave] + 4 * (lane >> 5), ws, bias, c, C, B - m0, to, ldl);
+        const int g = ct * NW + wave;
+        if (g < groups) cl_finish<4>(acc, s_f[wave], ws, bias, (int64_t)g * CL_GROUP, C, sb * 128, B, out, ldl, vec);
         ct = next_ct;
         sb = next_sb;
     }
@@ -672,11 +666,11 @@ cl_staged_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
 template <typename OUT>
 static void cl_logits(const int8_t *xq, const float *xs, const int8_t *wq, const float *ws, const float *bias, int64_t C, int D, int B,
                       float scale, OUT *out, int64_t ldl, hipStream_t st) {
-    const int vec = ((uintptr_t)out | (uintptr_t)(ldl * sizeof(OUT))) % (2 * sizeof(OUT)) == 0, kb = (D + 31) / 32;
+    const int vec = ((uintptr_t)out | (uintptr_t)(ldl * sizeof(OUT))) % (2 * sizeof(OUT)) == 0 && ldl < (1 << 26) / (int64_t)sizeof(OUT), kb = (D + 31) / 32;
     const unsigned gx = (unsigned)ks_ceil_div(ks_ceil_div(C, CL_GROUP), CL_NT / 64);
     if (B <= 32)
         hipLaunchKernelGGL((cl_direct_kernel<1, OUT>), dim3(gx, 1), dim3(CL_NT), 0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, vec);
-    else if (B > 64 && vec && kb <= 16 && ldl * (int64_t)sizeof(OUT) < (1 << 26)) {
+    else if (B > 64 && vec && kb <= 16) {
         const int xblocks = (B + 31) / 32, tiles = (xblocks + 7) / 8, tile = ((xblocks + tiles - 1) / tiles + 1) / 2 * 2;
         hipLaunchKernelGGL((kb <= 4 ? cl_steady_kernel<4, OUT> : kb <= 8 ? cl_steady_kernel<8, OUT> : kb <= 12 ? cl_steady_kernel<12, OUT> : cl_steady_kernel<16, OUT>),
                            dim3(256), dim3(CLX_NT), 0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, tile);
