@@ -23,7 +23,8 @@ extern "C" {
 #define KS_QUANT_CLASSES 1u   /* the rows are class weights: codes in the order of the product's class side */
 #define KS_QUANT_NORMALIZE 2u /* scales of the L2-normalised rows: row_scale is divided by the row's norm */
 
-#define KS_MAX_INT8_D 65536 /* largest depth: the integer sums stay below 2^30 */
+#define KS_MAX_INT8_D 65536   /* largest depth: the integer sums stay below 2^30 */
+#define KS_MAX_INT8_B 4194240 /* largest batch of one class_logits_int8 call */
 
 /* ------------------------------------------------------------------------------------------------------
  * class_quantize_rows -- rows as 8-bit integer codes with one scale each, in the order in which class_logits_int8 reads them.
@@ -57,7 +58,7 @@ int class_quantize_rows(const void *V, int dtype, int64_t n, int D, int64_t ldv,
  *   logits   [B, C] out, dtype KS_DTYPE_FP32 or KS_DTYPE_BF16; row i begins at element i * ldl (ldl >= C; elements between C and ldl
  *            are not touched, so that a node of a sharded layer may write its columns of a larger matrix).  Aligned to its
  *            elements is enough; rows that begin on whole 128-byte lines are written fastest, an odd ldl slowest
- * Requires B >= 1, 1 <= C < 2^31, 1 <= D <= KS_MAX_INT8_D (KS_UNSUPPORTED beyond).
+ * Requires 1 <= B <= KS_MAX_INT8_B, 1 <= C < 2^31, 1 <= D <= KS_MAX_INT8_D (KS_UNSUPPORTED beyond the maxima).
  * ---------------------------------------------------------------------------------------------------- */
 int class_logits_int8(const int8_t *x_codes, const float *x_scale, const int8_t *w_codes, const float *w_scale, const float *bias,
                       int64_t C, int D, int B, float scale, void *logits, int dtype, int64_t ldl, void *stream);

@@ -18,8 +18,6 @@ typedef int32_t cl_i32x16 __attribute__((ext_vector_type(16)));
 // ------------------------------------------------------------------------------------------------
 // rows -> codes
 // ------------------------------------------------------------------------------------------------
-#define CLQ_D 1024 /* elements of a row that a workgroup has in LDS at a time */
-
 template <typename IN> struct ClRow;
 template <> struct ClRow<float> {
     static __device__ __forceinline__ float one(const float *p) { return *p; }
@@ -72,74 +70,93 @@ __device__ __forceinline__ double cl_wave_sum_d(double v) {
     return v;
 }
 
-// One workgroup per block of 32 rows; a wavefront takes eight of them one after the other, their codes go through LDS so that
-// whole pieces are stored.
-template <typename IN, bool VEC>
-__global__ void __launch_bounds__(CL_NT)
+// A workgroup takes RB consecutive slots (32: a whole block, or 8) of a block of 32 rows, each of its eight wavefronts RB / 8 of them at
+// the same time, and NP * 256 elements of a row at a time: they stay in registers from the search for the largest to the
+// codes (longer rows are read twice), the codes go through LDS so that RB * 16 bytes in a row are stored.
+// What bounds it: the rows in, the codes out (390,625 x 512 fp32 with norms: 1.0 GB).
+#define CLQ_NT 512
+template <int RB, int NP, typename IN, bool VEC>
+__global__ void __launch_bounds__(CLQ_NT)
 cl_quantize_kernel(const IN *__restrict__ V, int64_t n, int D, int64_t ldv, uint32_t flags, int8_t *__restrict__ codes,
-                   float *__restrict__ row_scale) {
-    // piece p of a half h: 32 rows x 16 codes at (2 p + h) * 528 (16 bytes of padding spread the halves over the banks)
-    __shared__ __attribute__((aligned(16))) char lds[CLQ_D / 16 * 528];
-    __shared__ float s_amax[32];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t blk = blockIdx.x;
-    const int kb = (D + 31) / 32;
+                   float *__restrict__ row_scale, int64_t blk0) { // blk0: the launch's first block
+    constexpr int RW = RB / 8, DC = NP * 256, HALF = RB * 16 + 16; // rows of a wavefront; elements at a time; bytes of a half of a piece and padding that spreads the halves over the banks
+    __shared__ __attribute__((aligned(16))) char lds[DC / 16 * HALF];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t blk = blk0 + blockIdx.x / (32 / RB);
+    const int slot0 = blockIdx.x % (32 / RB) * RB, kb = (D + 31) / 32;
     constexpr bool RAW = sizeof(IN) == 1;
-    for (int i = 0; i < 8 && !RAW; ++i) {
-        const int r = wave * 8 + i;
-        const int64_t row = flags & KS_QUANT_CLASSES ? (blk >> 1) * CL_GROUP + 2 * r + (blk & 1) : blk * 32 + r;
-        if (row >= n) continue;
-        const IN *v = V + row * ldv;
-        int top = 0; // bits of |v|: ordered as the values, NaN above infinity
-        double ss = 0.0;
-        for (int d = lane * 4; d < D; d += 256) {
-            const float4 x = cl_load4<IN, VEC>(v, d, D);
-            top = max(max(top, max(__float_as_int(x.x) & 0x7FFFFFFF, __float_as_int(x.y) & 0x7FFFFFFF)),
-                      max(__float_as_int(x.z) & 0x7FFFFFFF, __float_as_int(x.w) & 0x7FFFFFFF));
-            if (flags & KS_QUANT_NORMALIZE) {
-                ss = __builtin_fma((double)x.x, (double)x.x, ss);
-                ss = __builtin_fma((double)x.y, (double)x.y, ss);
-                ss = __builtin_fma((double)x.z, (double)x.z, ss);
-                ss = __builtin_fma((double)x.w, (double)x.w, ss);
-            }
+    const auto row_of = [&](int i) __attribute__((always_inline)) {
+        const int slot = slot0 + wave * RW + i;
+        return flags & KS_QUANT_CLASSES ? (blk >> 1) * CL_GROUP + 2 * slot + (blk & 1) : blk * 32 + slot;
+    };
+    float4 x[RW][NP];
+    const auto load = [&](int d0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < RW; ++i) {
+            const int64_t row = row_of(i);
+            const IN *v = V + (row < n ? row : n - 1) * ldv;
+#pragma unroll
+            for (int e = 0; e < NP; ++e) x[i][e] = cl_load4<IN, VEC>(v, d0 + e * 256 + lane * 4, row < n ? D : 0);
         }
-        top = ks_wave_max_i(top);
-        const float a = top < 0x7F800000 ? __int_as_float(top) : 0.f; // not finite: codes 0
-        double s = (double)a / 127.0;
-        if (flags & KS_QUANT_NORMALIZE) {
-            ss = cl_wave_sum_d(ss);
-            if (a > 0.f) s /= sqrt(ss);
-        }
-        if (lane == 0) {
-            s_amax[r] = a;
-            row_scale[row] = top < 0x7F800000 ? (float)s : __int_as_float(0x7FC00000);
-        }
-    }
-    __syncthreads();
-    for (int d0 = 0; d0 < D; d0 += CLQ_D) {
-        const int len = min(CLQ_D, kb * 32 - d0); // a multiple of 32
-        for (int i = 0; i < 8; ++i) {
-            const int r = wave * 8 + i;
-            const int64_t row = flags & KS_QUANT_CLASSES ? (blk >> 1) * CL_GROUP + 2 * r + (blk & 1) : blk * 32 + r;
-            const double a = RAW || row >= n ? 0.0 : (double)s_amax[r], inv = a > 0.0 ? 127.0 / a : 0.0;
-            for (int d = lane * 4; d < len; d += 256) {
-                uint32_t q = 0;
-                if (row < n) {
-                    const float4 x = cl_load4<IN, VEC>(V + row * ldv, d0 + d, D);
-                    int c0, c1, c2, c3;
-                    if (RAW) { c0 = (int)x.x; c1 = (int)x.y; c2 = (int)x.z; c3 = (int)x.w; }
-                    else if (a > 0.0) { c0 = cl_code(x.x, inv, a); c1 = cl_code(x.y, inv, a); c2 = cl_code(x.z, inv, a); c3 = cl_code(x.w, inv, a); }
-                    else c0 = c1 = c2 = c3 = 0;
-                    q = (c0 & 255) | (c1 & 255) << 8 | (c2 & 255) << 16 | (uint32_t)c3 << 24;
+    };
+    int top[RW];  // bits of the largest |v|: ordered as the values, NaN above infinity
+    double ss[RW];
+#pragma unroll
+    for (int i = 0; i < RW; ++i) { top[i] = 0; ss[i] = 0.0; }
+    if (!RAW)
+        for (int d0 = 0; d0 < D; d0 += DC) {
+            load(d0);
+#pragma unroll
+            for (int i = 0; i < RW; ++i)
+#pragma unroll
+                for (int e = 0; e < NP; ++e) {
+                    const float4 v = x[i][e];
+                    top[i] = max(max(top[i], max(__float_as_int(v.x) & 0x7FFFFFFF, __float_as_int(v.y) & 0x7FFFFFFF)),
+                                 max(__float_as_int(v.z) & 0x7FFFFFFF, __float_as_int(v.w) & 0x7FFFFFFF));
+                    if (flags & KS_QUANT_NORMALIZE) {
+                        ss[i] = __builtin_fma((double)v.x, (double)v.x, ss[i]);
+                        ss[i] = __builtin_fma((double)v.y, (double)v.y, ss[i]);
+                        ss[i] = __builtin_fma((double)v.z, (double)v.z, ss[i]);
+                        ss[i] = __builtin_fma((double)v.w, (double)v.w, ss[i]);
+                    }
                 }
-                *(uint32_t *)(lds + (d >> 4) * 528 + r * 16 + (d & 15)) = q;
-            }
         }
+    double a[RW], inv[RW];
+#pragma unroll
+    for (int i = 0; i < RW; ++i) {
+        top[i] = ks_wave_max_i(top[i]);
+        a[i] = top[i] < 0x7F800000 ? (double)__int_as_float(top[i]) : 0.0; // not finite: codes 0
+        inv[i] = a[i] > 0.0 ? 127.0 / a[i] : 0.0;
+        if (RAW) continue;
+        double s = a[i] / 127.0;
+        if (flags & KS_QUANT_NORMALIZE) {
+            const double norm = sqrt(cl_wave_sum_d(ss[i]));
+            if (a[i] > 0.0) s /= norm;
+        }
+        if (lane == 0 && row_of(i) < n) row_scale[row_of(i)] = top[i] < 0x7F800000 ? (float)s : __int_as_float(0x7FC00000);
+    }
+    for (int d0 = 0; d0 < D; d0 += DC) {
+        if (RAW || D > DC) load(d0);
+        const int len = min(DC, kb * 32 - d0); // a multiple of 32
+#pragma unroll
+        for (int i = 0; i < RW; ++i)
+#pragma unroll
+            for (int e = 0; e < NP; ++e) {
+                const int d = e * 256 + lane * 4;
+                const float4 v = x[i][e];
+                int c0 = (int)v.x, c1 = (int)v.y, c2 = (int)v.z, c3 = (int)v.w;
+                if (!RAW) {
+                    if (a[i] > 0.0) { c0 = cl_code(v.x, inv[i], a[i]); c1 = cl_code(v.y, inv[i], a[i]); c2 = cl_code(v.z, inv[i], a[i]); c3 = cl_code(v.w, inv[i], a[i]); }
+                    else c0 = c1 = c2 = c3 = 0;
+                }
+                const uint32_t q = (c0 & 255) | (c1 & 255) << 8 | (c2 & 255) << 16 | (uint32_t)c3 << 24;
+                if (d < len) *(uint32_t *)(lds + (d >> 4) * HALF + (wave * RW + i) * 16 + (d & 15)) = q;
+            }
         __syncthreads();
-        int8_t *out = codes + (blk * kb + d0 / 32) * CL_PIECE;
-        for (int e = threadIdx.x; e < len * 2; e += CL_NT) // 16-byte units: half-piece e / 32, row e % 32
-            *(uint4 *)(out + (int64_t)e * 16) = *(const uint4 *)(lds + (e >> 5) * 528 + (e & 31) * 16);
-        __syncthreads();
+        int8_t *out = codes + (blk * kb + d0 / 32) * CL_PIECE + slot0 * 16;
+        for (int e = threadIdx.x; e < len / 16 * RB; e += CLQ_NT) // 16 bytes each: row e % RB of half-piece e / RB
+            *(uint4 *)(out + (int64_t)(e / RB) * 512 + e % RB * 16) = *(const uint4 *)(lds + e / RB * HALF + e % RB * 16);
+        if (d0 + DC < D) __syncthreads();
     }
 }
 
@@ -149,12 +166,25 @@ extern "C" size_t class_codes_bytes(int64_t n, int D, uint32_t flags) {
     return (size_t)rows * ((D + 31) / 32 * 32);
 }
 
+template <typename IN, bool VEC>
+static void cl_quantize(const void *V, int64_t n, int D, int64_t ldv, uint32_t flags, int8_t *codes, float *row_scale, hipStream_t st) {
+    const int64_t blocks = flags & KS_QUANT_CLASSES ? ks_ceil_div(n, CL_GROUP) * 2 : ks_ceil_div(n, 32);
+    const auto go = [&](auto kernel, int rb) { // a launch's threads are counted in 32 bits
+        for (int64_t b0 = 0; b0 < blocks; b0 += 1 << 20)
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((blocks - b0 < 1 << 20 ? blocks - b0 : 1 << 20) * (32 / rb))), dim3(CLQ_NT), 0, st, (const IN *)V,
+                               n, D, ldv, flags, codes, row_scale, b0);
+    };
+    // whole blocks where there are enough of them and a wavefront holds four rows; else a row a wavefront
+    if (blocks >= 512 && D <= 512) go(cl_quantize_kernel<32, 2, IN, VEC>, 32);
+    else if (blocks >= 512 && D <= 1024) go(cl_quantize_kernel<32, 4, IN, VEC>, 32);
+    else if (D <= 512) go(cl_quantize_kernel<8, 2, IN, VEC>, 8);
+    else go(cl_quantize_kernel<8, 16, IN, VEC>, 8);
+}
 template <typename IN>
 static void cl_quantize(const void *V, int64_t n, int D, int64_t ldv, uint32_t flags, int8_t *codes, float *row_scale, hipStream_t st) {
-    const dim3 grid((unsigned)(flags & KS_QUANT_CLASSES ? ks_ceil_div(n, CL_GROUP) * 2 : ks_ceil_div(n, 32)));
     const bool vec = ((uintptr_t)V | (uintptr_t)(ldv * sizeof(IN))) % (4 * sizeof(IN)) == 0;
-    if (vec) hipLaunchKernelGGL((cl_quantize_kernel<IN, true>), grid, dim3(CL_NT), 0, st, (const IN *)V, n, D, ldv, flags, codes, row_scale);
-    else hipLaunchKernelGGL((cl_quantize_kernel<IN, false>), grid, dim3(CL_NT), 0, st, (const IN *)V, n, D, ldv, flags, codes, row_scale);
+    if (vec) cl_quantize<IN, true>(V, n, D, ldv, flags, codes, row_scale, st);
+    else cl_quantize<IN, false>(V, n, D, ldv, flags, codes, row_scale, st);
 }
 
 extern "C" int class_quantize_rows(const void *V, int dtype, int64_t n, int D, int64_t ldv, uint32_t flags, int8_t *codes,
@@ -261,19 +291,22 @@ __device__ __forceinline__ void cl_finish(const cl_i32x16 (&acc)[S][2], const fl
     }
 }
 
-// One wavefront: 64 classes (the two blocks of a group) by 32 S samples, codes straight from memory.
-template <int S, typename OUT>
+// One wavefront: 64 classes (the two blocks of a group) by 32 S samples, codes straight from memory.  KS > 1: KS wavefronts of a
+// workgroup take a part of the depth each and add their (whole) sums in LDS.
+template <int S, int KS, typename OUT>
 __global__ void __launch_bounds__(CL_NT)
 cl_direct_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, const int8_t *__restrict__ wq,
                  const float *__restrict__ ws, const float *__restrict__ bias, int64_t C, int kb, int B, float scale,
                  OUT *__restrict__ out, int64_t ldl, int vec) {
+    constexpr int NG = CL_NT / 64 / KS; // groups of a workgroup
     __shared__ __attribute__((aligned(16))) float s_f[32 * S];
-    const int lane = threadIdx.x & 63;
+    __shared__ int s_sum[KS > 1 ? (KS - 1) * S * 32 * 64 : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = wave % KS;
     const int sb = blockIdx.y * S, xblocks = (B + 31) / 32; // first block of samples
     if (threadIdx.x < 32 * S) s_f[threadIdx.x] = sb * 32 + (int)threadIdx.x < B ? scale * xs[sb * 32 + threadIdx.x] : 0.f;
-    __syncthreads();
-    const int64_t grp = (int64_t)blockIdx.x * (CL_NT / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (grp * CL_GROUP >= C) return;
+    if (KS == 1) __syncthreads();
+    const int64_t grp = (int64_t)blockIdx.x * NG + wave / KS;
+    if (grp * CL_GROUP >= C) return; // KS > 1: a workgroup has one group, all its wavefronts or none
     const int8_t *wp = wq + grp * 2 * kb * CL_PIECE + lane * 16;
     const int8_t *xp[S];
 #pragma unroll
@@ -285,7 +318,8 @@ cl_direct_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
         for (int q = 0; q < 2; ++q)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[s][q][r] = 0;
-    for (int k = 0; k < kb; ++k) {
+    const int end = kb * (part + 1) / KS;
+    for (int k = kb * part / KS; k < end; ++k) {
         cl_i32x4 w[2], x[S];
 #pragma unroll
         for (int q = 0; q < 2; ++q) w[q] = *(const cl_i32x4 *)(wp + ((int64_t)q * kb + k) * CL_PIECE);
@@ -296,8 +330,55 @@ cl_direct_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
 #pragma unroll
             for (int q = 0; q < 2; ++q) acc[s][q] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[s], w[q], acc[s][q], 0, 0, 0);
     }
+    if (KS > 1) {
+        static_assert(KS == 1 || NG == 1, "barriers");
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (part) s_sum[((part - 1) * S * 32 + s * 32 + q * 16 + r) * 64 + lane] = acc[s][q][r];
+        __syncthreads();
+        if (part) return;
+#pragma unroll
+        for (int o = 0; o < KS - 1; ++o)
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[s][q][r] += s_sum[(o * S * 32 + s * 32 + q * 16 + r) * 64 + lane];
+    }
     cl_finish<S>(acc, s_f, ws, bias, grp * CL_GROUP, C, sb * 32, B, out, ldl, vec);
 }
+
+// The work of a workgroup: stretches of an XCD's class groups for one sample tile each.  Workgroup i runs on XCD i % 8, and the groups are
+// dealt to the XCDs in eight ranges.  Workgroups that are at the same groups at the same time share their codes in the L2, so
+// the tiles of a round, at most eight, are taken by as many workgroups side by side, and the groups are divided among as many
+// such sets as an XCD has room for (at least 28 of its 32 workgroups then have work).  Tiles that are not in step with each
+// other read the weights from memory for each of them: 482 us instead of 320 at 1,400 x 390,625 x 512.
+struct ClShare {
+    int g_lo, g_n, n_sb, sb0; // the XCD's groups; tiles, those of the rounds before
+    __device__ __forceinline__ ClShare(int groups, int n_sb_) {
+        const int xcd = blockIdx.x & 7;
+        g_lo = (int)((int64_t)groups * xcd / 8);
+        g_n = (int)((int64_t)groups * (xcd + 1) / 8) - g_lo;
+        n_sb = n_sb_;
+        sb0 = 0;
+    }
+    // the next stretch: groups [first, last) of g_lo on, for tile sb (none: first >= last)
+    __device__ __forceinline__ bool next(int &sb, int &first, int &last) {
+        if (sb0 >= n_sb) return false;
+        const int rounds = (n_sb - sb0 + 7) / 8, tiles = (n_sb - sb0 + rounds - 1) / rounds;
+        const int sets = (int)(gridDim.x >> 3) / tiles, j = blockIdx.x >> 3, set = j / tiles;
+        sb = sb0 + j % tiles;
+        first = set < sets ? (int)((int64_t)g_n * set / sets) : 0;
+        last = set < sets ? (int)((int64_t)g_n * (set + 1) / sets) : 0;
+        sb0 += tiles;
+        return true;
+    }
+};
 
 #define CLX_KB 36 /* pieces of depth of 128 samples that lie in LDS beside their scales */
 #define CLX_NT 512
@@ -317,17 +398,11 @@ cl_resident_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, 
     const int xblocks = (B + 31) / 32, n_sb = (B + 127) / 128;
     const int chunks = (kb + R - 1) / R, last_step = (kb - (chunks - 1 > 1 ? chunks - 2 : 0) * R - R) * CL_PIECE; // kb >= R
     const int groups = (int)((C + CL_GROUP - 1) / CL_GROUP);
-    // workgroup i runs on XCD i % 8: the classes are dealt to the XCDs in eight ranges; an XCD's workgroups divide its range, once
-    // for every 128 samples, into equal stretches, so that those at the same classes at the same time share its L2
-    const int xcd = blockIdx.x & 7, per_xcd = gridDim.x >> 3, j = blockIdx.x >> 3;
-    const int g_lo = (int)((int64_t)groups * xcd / 8), g_n = (int)((int64_t)groups * (xcd + 1) / 8) - g_lo;
-    const int64_t todo = (int64_t)g_n * n_sb;
-    int64_t at = todo * j / per_xcd;
-    const int64_t end = todo * (j + 1) / per_xcd;
-    while (at < end) {
-        const int sb = (int)(at / g_n), first = (int)(at - (int64_t)sb * g_n);
-        const int last = (int)(end - at < g_n - first ? first + (end - at) : g_n); // this stretch's part for sample block sb
-        at += last - first;
+    ClShare share(groups, n_sb);
+    const int g_lo = share.g_lo;
+    int sb, first, last;
+    while (share.next(sb, first, last)) {
+        if (first >= last) continue;
         __syncthreads();
         // through registers: reads from LDS that a direct load may have written would wait for every load of weights in flight
         for (int p = wave; p < chunks * R * 4; p += NW) { // k-step t of sample block s at (4 t + s)
@@ -411,16 +486,11 @@ cl_steady_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half4 = 4 * (lane >> 5);
     const int xblocks = (B + 31) / 32, n_sb = (xblocks + tile - 1) / tile;
     const int groups = (int)((C + CL_GROUP - 1) / CL_GROUP);
-    // the division of the work as in cl_resident_kernel
-    const int xcd = blockIdx.x & 7, per_xcd = gridDim.x >> 3, j = blockIdx.x >> 3;
-    const int g_lo = (int)((int64_t)groups * xcd / 8), g_n = (int)((int64_t)groups * (xcd + 1) / 8) - g_lo;
-    const int64_t todo = (int64_t)g_n * n_sb;
-    int64_t at = todo * j / per_xcd;
-    const int64_t end = todo * (j + 1) / per_xcd;
-    while (at < end) {
-        const int sb = (int)(at / g_n), first = (int)(at - (int64_t)sb * g_n);
-        const int last = (int)(end - at < g_n - first ? first + (end - at) : g_n); // this stretch's part for samples sb
-        at += last - first;
+    ClShare share(groups, n_sb);
+    const int g_lo = share.g_lo;
+    int sb, first, last;
+    while (share.next(sb, first, last)) {
+        if (first >= last) continue;
         __syncthreads();
         for (int p = wave; p < tile * KB; p += NW) { // k-step k of block i at (KB i + k), 0 beyond the depth
             const int blk = sb * tile + p / KB < xblocks ? sb * tile + p / KB : xblocks - 1, k = p % KB;
@@ -538,8 +608,10 @@ cl_steady_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
         }
 }
 
-// Deeper rows: as above, but the samples pass through LDS in chunks of four k-steps, which eight wavefronts with 64 classes each read at
-// the same time: three buffers, a barrier a chunk.  While chunk t is multiplied, the fragments are read one k-step ahead (the
+// Deeper rows: as in cl_resident_kernel, but the samples pass through LDS in chunks of eight k-steps, which eight wavefronts with 64
+// classes each read at the same time: three buffers, a barrier a chunk (2,048 x 131,072 x 4,096: 1,069 us = 2.06 POP/s, with
+// chunks of four 1,092; the matrix pipes are busy half of the time at 1.96 GHz, what holds them up is the load path, busy for two thirds
+// of it, and the barriers.  A tile of 256 x 256 with both sides in LDS and one wavefront a SIMD came to 1,118).  While chunk t is multiplied, the fragments are read one k-step ahead (the
 // last ones from chunk t + 1, which is there since the barrier), chunk t + 2 is written to LDS from registers and those are
 // requested anew for chunk t + 3.  The chunks run on from one tile of 512 classes by 128 samples to the next.
 template <typename OUT>
@@ -547,7 +619,7 @@ __global__ void __launch_bounds__(CLX_NT, 2)
 cl_staged_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, const int8_t *__restrict__ wq,
                  const float *__restrict__ ws, const float *__restrict__ bias, int64_t C, int kb, int B, float scale,
                  OUT *__restrict__ out, int64_t ldl, int vec) {
-    constexpr int NW = CLX_NT / 64, R = 4, CHUNK = R * 4 * CL_PIECE;
+    constexpr int NW = CLX_NT / 64, R = 8, RW = 4 /* k-steps of weights ahead */, CHUNK = R * 4 * CL_PIECE;
     __shared__ __attribute__((aligned(16))) char s_x[3 * CHUNK];
     __shared__ __attribute__((aligned(16))) float s_f[NW][128];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -563,13 +635,12 @@ cl_staged_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
     const int step_c = per_xcd / n_sb, step_s = per_xcd % n_sb; // from one of this workgroup's tiles to its next
     int ct = c_lo + j / n_sb, sb = j % n_sb;
 
-    // samples: this wavefront moves two of a chunk's 16 pieces, k-step wave / 2 of sample blocks i and i + 1
+    // samples: this wavefront moves four of a chunk's 32 pieces, k-step `wave` of the four sample blocks
     int64_t r_left = left;
     int r_sb = sb, r_c = 0; // chunk that is requested next
-    const int x_kk = wave >> 1, x_s = (wave & 1) * 2;
     const auto request = [&](int i) __attribute__((always_inline)) {
-        const int blk = r_sb * 4 + x_s + i < xblocks ? r_sb * 4 + x_s + i : xblocks - 1;
-        const int k = (r_c < chunks - 1 ? r_c * R : kb - R) + x_kk;
+        const int blk = r_sb * 4 + i < xblocks ? r_sb * 4 + i : xblocks - 1;
+        const int k = (r_c < chunks - 1 ? r_c * R : kb - R) + wave;
         return *(const cl_i32x4 *)(xq + ((int64_t)blk * kb + k) * CL_PIECE + lane * 16);
     };
     const auto requested = [&]() __attribute__((always_inline)) { // behind the last tile: the same again, read by nobody
@@ -584,8 +655,8 @@ cl_staged_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
     };
     // chunk c: one that is short begins R before the end, with zeros for what the one before had
     const auto place = [&](cl_i32x4 v, int i, int c, char *to) __attribute__((always_inline)) {
-        if (c == chunks - 1 && kb - R + x_kk < c * R) v = cl_i32x4{0, 0, 0, 0};
-        *(cl_i32x4 *)(to + (x_kk * 4 + x_s + i) * CL_PIECE + lane * 16) = v;
+        if (c == chunks - 1 && kb - R + wave < c * R) v = cl_i32x4{0, 0, 0, 0};
+        *(cl_i32x4 *)(to + (wave * 4 + i) * CL_PIECE + lane * 16) = v;
     };
     const int block_bytes = kb * CL_PIECE;
     const auto weights = [&](int tile) __attribute__((always_inline)) { // of this wavefront's classes in a tile; beyond the last group: that one
@@ -593,21 +664,21 @@ cl_staged_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
         return wq + (int64_t)(g < groups ? g : groups - 1) * 2 * block_bytes;
     };
     char *b0 = s_x, *b1 = s_x + CHUNK, *b2 = s_x + 2 * CHUNK; // chunks t, t + 1, t + 2
-    cl_i32x4 held[2];
+    cl_i32x4 held[4];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) place(request(i), i, r_c, t ? b1 : b0);
+        for (int i = 0; i < 4; ++i) place(request(i), i, r_c, t ? b1 : b0);
         requested();
     }
-    held[0] = request(0);
-    held[1] = request(1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) held[i] = request(i);
     int p_c = r_c; // its chunk
     requested();
-    cl_i32x4 w[R][2], x[2][4];
+    cl_i32x4 w[RW][2], x[2][4];
     const int8_t *p = weights(ct);
 #pragma unroll
-    for (int kk = 0; kk < R; ++kk)
+    for (int kk = 0; kk < RW; ++kk)
 #pragma unroll
         for (int q = 0; q < 2; ++q) { // in the order in which they are used: the main loop's counted waits hold for these too
             w[kk][q] = *(const cl_i32x4 *)(p + q * block_bytes + kk * CL_PIECE + lane * 16);
@@ -628,6 +699,7 @@ cl_staged_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[s][q][r] = 0;
         for (int c = chunks; c > 0; --c) {
+            const int8_t *pc = p + RW * CL_PIECE, *pc1 = pc + block_bytes;
             p = c == 1 ? weights(next_ct) : c == 2 ? p + last_step : p + R * CL_PIECE;
             const int8_t *p1 = p + block_bytes;
             cl_barrier(); // chunk t + 1 is whole, and nobody reads chunk t - 1 any more
@@ -639,12 +711,13 @@ cl_staged_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
                 for (int q = 0; q < 2; ++q) {
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) acc[s][q] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[kk & 1][s], w[kk][q], acc[s][q], 0, 0, 0);
+                    for (int s = 0; s < 4; ++s) acc[s][q] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[kk & 1][s], w[kk % RW][q], acc[s][q], 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
-                    w[kk][q] = *(const cl_i32x4 *)((q == 0 ? p : p1) + kk * CL_PIECE + lane * 16);
-                    if (kk == 1) {
-                        place(held[q], q, p_c, b2);
-                        held[q] = request(q);
+                    w[kk % RW][q] = *(const cl_i32x4 *)((kk < RW ? (q == 0 ? pc : pc1) : (q == 0 ? p : p1)) + kk % RW * CL_PIECE + lane * 16);
+                    if (kk == 1 || kk == 4) {
+                        const int i = kk == 1 ? q : 2 + q;
+                        place(held[i], i, p_c, b2);
+                        held[i] = request(i);
                     }
                 }
             }
@@ -667,20 +740,32 @@ template <typename OUT>
 static void cl_logits(const int8_t *xq, const float *xs, const int8_t *wq, const float *ws, const float *bias, int64_t C, int D, int B,
                       float scale, OUT *out, int64_t ldl, hipStream_t st) {
     const int vec = ((uintptr_t)out | (uintptr_t)(ldl * sizeof(OUT))) % (2 * sizeof(OUT)) == 0 && ldl < (1 << 26) / (int64_t)sizeof(OUT), kb = (D + 31) / 32;
-    const unsigned gx = (unsigned)ks_ceil_div(ks_ceil_div(C, CL_GROUP), CL_NT / 64);
-    if (B <= 32)
-        hipLaunchKernelGGL((cl_direct_kernel<1, OUT>), dim3(gx, 1), dim3(CL_NT), 0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, vec);
-    else if (B > 64 && vec && kb <= 16) {
-        const int xblocks = (B + 31) / 32, tiles = (xblocks + 7) / 8, tile = ((xblocks + tiles - 1) / tiles + 1) / 2 * 2;
-        hipLaunchKernelGGL((kb <= 4 ? cl_steady_kernel<4, OUT> : kb <= 8 ? cl_steady_kernel<8, OUT> : kb <= 12 ? cl_steady_kernel<12, OUT> : cl_steady_kernel<16, OUT>),
-                           dim3(256), dim3(CLX_NT), 0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, tile);
-    } else if (B > 64 && kb >= 4 && kb <= CLX_KB)
+    const int64_t groups = ks_ceil_div(C, CL_GROUP);
+    const auto direct = [&](auto kernel, int samples, int per_workgroup) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)ks_ceil_div(groups, per_workgroup), (unsigned)ks_ceil_div(B, samples)), dim3(CL_NT), 0, st, xq, xs,
+                           wq, ws, bias, C, kb, B, scale, out, ldl, vec);
+    };
+    // Few samples: the codes of the weights are what moves, and every wavefront reads its own.  Few wavefronts in all (a kernel of
+    // 256 workgroups that keep the samples would leave most idle: 10,000 x 512, batch 256: 5.9 us, 8.0 in 128-sample tiles; 50,000
+    // x 512, 128: 11.3 and 9.3): the same for any batch.  Where they are deep, four wavefronts divide each group's depth (10,000 x
+    // 4,096, one sample: 39 us, 13; 64: 44, 16; 50,000 x 2,048, one: 25, 20; but 64 samples, whose sums take 320 registers, only
+    // where a compute unit would have a wavefront or so: 50,000 x 768: 12 us, 21).
+    const int64_t waves = groups * ks_ceil_div(B, 64);
+    if (B <= 32) return waves <= 1024 && kb >= 24 ? direct(cl_direct_kernel<1, 4, OUT>, 32, 1) : direct(cl_direct_kernel<1, 1, OUT>, 32, 4);
+    if (B <= 64 || waves <= 1280 || (kb < 4 && !vec))
+        return waves <= 320 && kb >= 24 ? direct(cl_direct_kernel<2, 4, OUT>, 64, 1) : direct(cl_direct_kernel<2, 1, OUT>, 64, 4);
+    // Registers hold 64 classes' codes while samples stream, or LDS holds samples while codes stream: the former is ahead for thin
+    // rows (390,625 x 64, batch 1,024: 162 us, 176) and for large products (x 512: 214, 229; 1,024 x 120,000 x 512: 75, 71), if
+    // the wavefronts' last round of groups is well filled.
+    const int xblocks = (B + 31) / 32, tiles = (xblocks + 7) / 8, tile = ((xblocks + tiles - 1) / tiles + 1) / 2 * 2;
+    const int64_t sets = 32 / (tiles < 8 ? tiles : 8) * 64, rounds = ks_ceil_div(groups, sets);
+    if (vec && (kb < 4 || ((kb == 4 || (kb > 8 && kb <= 16 && tiles >= 4)) && groups * 100 >= rounds * sets * 85)))
+        hipLaunchKernelGGL((kb <= 4 ? cl_steady_kernel<4, OUT> : kb <= 12 ? cl_steady_kernel<12, OUT> : cl_steady_kernel<16, OUT>), dim3(256), dim3(CLX_NT),
+                           0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, tile);
+    else if (kb <= CLX_KB)
         hipLaunchKernelGGL((cl_resident_kernel<4, OUT>), dim3(256), dim3(CLX_NT), 0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, vec);
-    else if (B > 64 && kb > CLX_KB)
-        hipLaunchKernelGGL(cl_staged_kernel<OUT>, dim3(256), dim3(CLX_NT), 0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, vec);
     else
-        hipLaunchKernelGGL((cl_direct_kernel<2, OUT>), dim3(gx, (unsigned)ks_ceil_div(B, 64)), dim3(CL_NT), 0, st, xq, xs, wq, ws, bias, C,
-                           kb, B, scale, out, ldl, vec);
+        hipLaunchKernelGGL(cl_staged_kernel<OUT>, dim3(256), dim3(CLX_NT), 0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, vec);
 }
 
 extern "C" int class_logits_int8(const int8_t *x_codes, const float *x_scale, const int8_t *w_codes, const float *w_scale,
@@ -690,7 +775,7 @@ extern "C" int class_logits_int8(const int8_t *x_codes, const float *x_scale, co
     if (C < 1 || C >= (int64_t)1 << 31 || D < 1 || B < 1 || ldl < C) return KS_INVALID_ARG;
     if (dtype != KS_DTYPE_BF16 && dtype != KS_DTYPE_FP32) return KS_INVALID_ARG;
     if (((uintptr_t)x_codes | (uintptr_t)w_codes) % 16 || (uintptr_t)logits % (dtype == KS_DTYPE_FP32 ? 4 : 2)) return KS_INVALID_ARG;
-    if (D > KS_MAX_INT8_D) return KS_UNSUPPORTED;
+    if (D > KS_MAX_INT8_D || B > KS_MAX_INT8_B) return KS_UNSUPPORTED;
     if (dtype == KS_DTYPE_FP32)
         cl_logits<float>(x_codes, x_scale, w_codes, w_scale, bias, C, D, B, scale, (float *)logits, ldl, (hipStream_t)stream);
     else

@@ -55,6 +55,7 @@ def test_product_refuses(ks):
                 dict(out=ct.c_void_p(258)), dict(C=0), dict(C=1 << 31, ldl=1 << 31), dict(D=0), dict(B=0), dict(ldl=4), dict(dtype=2)):
         assert call(**bad) == ks.KS_INVALID_ARG, bad
     assert call(D=65_537) == ks.KS_UNSUPPORTED
+    assert call(B=4_194_241) == ks.KS_UNSUPPORTED
 
 
 def test_adjust_refuses(ks):
