@@ -58,6 +58,12 @@ def lib():
                 L.grad_topk_plan.restype = ct.c_int64
             elif name != "ks_version":
                 getattr(L, name).restype = ct.c_int
+        # declared argument types: plain numbers are converted in C, which takes a third of the time of a ctypes object each
+        i, i64, u32, f, p = ct.c_int, ct.c_int64, ct.c_uint32, ct.c_float, ct.c_void_p
+        L.class_codes_bytes.argtypes = (i64, i, u32)
+        L.class_quantize_rows.argtypes = (p, i, i64, i, i64, u32, p, p, p)
+        L.class_logits_int8.argtypes = (p, p, p, p, p, i64, i, i, f, p, i, i64, p)
+        L.class_logits_adjust.argtypes = (p, i64, p, i64, i, i64, i64, i64, i, p, p, i64, i, p, p, p, p, p, p, p, i64, i, p, i64, i, p, p, p)
         _LIB = L
     return _LIB
 
@@ -756,31 +762,36 @@ def grad_topk_select(g, plan: GradTopkPlan, out_idx=None, out_val=None, ws=None,
 # answering with a trained layer (include/class_logits.h)
 # ---------------------------------------------------------------------------------------------------
 QUANT_CLASSES, QUANT_NORMALIZE = 1, 2  # KS_QUANT_*
-_FLOAT_CODES = {torch.bfloat16: 0, torch.float32: 1}
+_ROW_CODES = {torch.bfloat16: 0, torch.float32: 1, torch.int8: 2}
+_LOGIT_CODES = {torch.bfloat16: 0, torch.float32: 1}
 
 
-def _home(stream, first, *others):
-    """The device all of a call's tensors are on; the call's stream has to be one of that device's."""
-    dev = first.device
-    for t in others:
-        if t is not None and t.device != dev:
-            raise ValueError(f"tensors of one call on {dev} and {t.device}")
-    if stream is not None and stream.device != dev:
-        raise ValueError(f"stream of {stream.device} for tensors on {dev}")
-    return dev
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
-class _Home:
-    """The current device and stream are the call's own while its outputs are allocated and its kernels launched."""
+class _Launch:
+    """The device that all tensors of a call are on, and its stream there, both current while outputs are allocated and kernels
+    launched.  (Entered only where they are not current already.)"""
 
-    def __init__(self, dev, stream):
-        if stream is None and dev.index != torch.cuda.current_device():
-            stream = torch.cuda.current_stream(dev)
-        self.inner = torch.cuda.stream(stream) if stream is not None else None
+    def __init__(self, stream, first, *others):
+        dev = self.device = first.device
+        index = first.get_device()
+        for t in others:
+            if t is not None and t.get_device() != index:
+                raise ValueError(f"tensors of one call on {dev} and {t.device}")
+        self.inner = None
+        if stream is not None:
+            if stream.device != dev:
+                raise ValueError(f"stream of {stream.device} for tensors on {dev}")
+            self.inner = torch.cuda.stream(stream)
+        elif index != torch.cuda.current_device():
+            self.inner = torch.cuda.stream(torch.cuda.current_stream(dev))
 
     def __enter__(self):
         if self.inner is not None:
             self.inner.__enter__()
+        return torch._C._cuda_getCurrentRawStream(self.device.index)
 
     def __exit__(self, *e):
         if self.inner is not None:
@@ -788,38 +799,48 @@ class _Home:
 
 
 def _rows(t, types, name):
-    """A device matrix of one of `types` whose rows are contiguous (any distance from row to row)."""
-    if t.dtype not in types or not t.is_cuda or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1) or (t.stride(0) < t.shape[1] and t.shape[0] > 1):
-        raise TypeError(f"{name} must be a 2-D device tensor of {' or '.join(str(x) for x in types)} with contiguous rows")
-    return max(t.stride(0), t.shape[1])
+    """A device matrix of one of `types` whose rows are contiguous (any distance from row to row): -> type code, rows, columns, distance."""
+    code = types.get(t.dtype)
+    if code is None or not t.is_cuda or t.dim() != 2:
+        raise TypeError(f"{name} must be a 2-D device tensor of {' or '.join(str(x) for x in types)}")
+    (n, d), (ld, step) = t.shape, t.stride()
+    if (step != 1 and d > 1) or (ld < d and n > 1):
+        raise TypeError(f"{name} must have contiguous rows")
+    return code, n, d, max(ld, d)
+
+
+def _list(t, dtype, n, name):
+    """A contiguous device tensor of n elements, or none."""
+    if t is not None and (t.dtype != dtype or not t.is_cuda or not t.is_contiguous()):
+        raise TypeError(f"{name} must be a contiguous device tensor of {dtype}")
+    if t is not None and t.numel() != n:
+        raise ValueError(f"{name} must have {n} elements")
+    return t
 
 
 def class_codes_bytes(n, D, classes=False) -> int:
-    return int(lib().class_codes_bytes(ct.c_int64(n), ct.c_int(D), ct.c_uint32(QUANT_CLASSES if classes else 0)))
+    return int(lib().class_codes_bytes(n, D, QUANT_CLASSES if classes else 0))
 
 
 def class_quantize_rows(V, classes=False, normalize=False, codes=None, row_scale=None, stream=None):
     """Rows of V [n, D] (bf16, fp32, or int8: codes as they are; the rows may lie apart) as 8-bit codes in the order that class_logits_int8
     reads, class weights with classes=True.  Returns (codes int8 [class_codes_bytes], row_scale fp32 [n], None for int8 rows);
     `codes` / `row_scale` are used as the outputs when given.  normalize=True: scales of the L2-normalised rows."""
-    ldv = _rows(V, (torch.bfloat16, torch.float32, torch.int8), "V")
-    n, D = V.shape
-    raw = V.dtype == torch.int8
-    if raw and (normalize or row_scale is not None):
+    L = lib()
+    code, n, D, ldv = _rows(V, _ROW_CODES, "V")
+    if code == 2 and (normalize or row_scale is not None):
         raise ValueError("int8 rows are taken as they are: no normalize, no row_scale")
-    need = class_codes_bytes(n, D, classes)
-    with _Home(_home(stream, V, codes, row_scale), stream):
+    flags = (QUANT_CLASSES if classes else 0) | (QUANT_NORMALIZE if normalize else 0)
+    need = L.class_codes_bytes(n, D, flags)
+    _list(codes, torch.int8, need, "codes")
+    _list(row_scale, torch.float32, n, "row_scale")
+    launch = _Launch(stream, V, codes, row_scale)
+    with launch as raw:
         if codes is None:
-            codes = torch.empty(need, dtype=torch.int8, device=V.device)
-        elif _need(codes, torch.int8, "codes").numel() != need:
-            raise ValueError(f"codes must have {need} bytes")
-        if row_scale is None and not raw:
-            row_scale = torch.empty(n, dtype=torch.float32, device=V.device)
-        elif not raw and _need(row_scale, torch.float32, "row_scale").numel() != n:
-            raise ValueError("row_scale must be [n]")
-        rc = lib().class_quantize_rows(_ptr(V), ct.c_int(2 if raw else _FLOAT_CODES[V.dtype]), ct.c_int64(n), ct.c_int(D), ct.c_int64(ldv),
-                                       ct.c_uint32((QUANT_CLASSES if classes else 0) | (QUANT_NORMALIZE if normalize else 0)),
-                                       _ptr(codes), _ptr(row_scale), _stream(stream))
+            codes = torch.empty(need, dtype=torch.int8, device=launch.device)
+        if row_scale is None and code != 2:
+            row_scale = torch.empty(n, dtype=torch.float32, device=launch.device)
+        rc = L.class_quantize_rows(V.data_ptr(), code, n, D, ldv, flags, codes.data_ptr(), _at(row_scale), raw)
     _check("class_quantize_rows", rc)
     return codes, row_scale
 
@@ -827,29 +848,27 @@ def class_quantize_rows(V, classes=False, normalize=False, codes=None, row_scale
 def class_logits_int8(x_codes, x_scale, w_codes, w_scale, scale, bias=None, out=None, dtype=torch.float32, stream=None):
     """Logits [B, C] of B feature rows against all C classes, from the codes and scales of class_quantize_rows (w_codes made with
     classes=True).  Without `out` (bf16 or fp32, rows may lie apart) the result is of `dtype` and its rows lie on 128-byte lines."""
-    _need(x_codes, torch.int8, "x_codes")
-    _need(w_codes, torch.int8, "w_codes")
-    _need(x_scale, torch.float32, "x_scale")
-    _need(w_scale, torch.float32, "w_scale")
+    L = lib()
     B, C = x_scale.numel(), w_scale.numel()
     if B < 1 or C < 1:
         raise ValueError("x_scale [B] and w_scale [C] must not be empty")
     D = x_codes.numel() // ((B + 31) // 32 * 32)  # a multiple of 32: what lies beyond the rows' own depth is 0
-    if D < 1 or class_codes_bytes(B, D) != x_codes.numel() or class_codes_bytes(C, D, True) != w_codes.numel():
-        raise ValueError("x_codes and w_codes must be the codes of B feature rows and C class rows of one depth")
-    if bias is not None and _need(bias, torch.float32, "bias").numel() != C:
-        raise ValueError("bias must be [C]")
-    with _Home(_home(stream, x_codes, x_scale, w_codes, w_scale, bias, out), stream):
+    _list(x_codes, torch.int8, L.class_codes_bytes(B, D, 0), "x_codes (of B feature rows)")
+    _list(w_codes, torch.int8, L.class_codes_bytes(C, D, QUANT_CLASSES), "w_codes (of C class rows of the features' depth)")
+    _list(x_scale, torch.float32, B, "x_scale")
+    _list(w_scale, torch.float32, C, "w_scale")
+    _list(bias, torch.float32, C, "bias")
+    launch = _Launch(stream, x_codes, x_scale, w_codes, w_scale, bias, out)
+    with launch as raw:
         if out is None:
-            if dtype not in _FLOAT_CODES:
+            if dtype not in _LOGIT_CODES:
                 raise TypeError("dtype must be torch.bfloat16 or torch.float32")
-            out = torch.empty((B, (C + 63) // 64 * 64), dtype=dtype, device=x_codes.device)[:, :C]
-        ldl = _rows(out, (torch.bfloat16, torch.float32), "out")
-        if tuple(out.shape) != (B, C):
+            out = torch.empty((B, (C + 63) // 64 * 64), dtype=dtype, device=launch.device)[:, :C]
+        code, n, d, ldl = _rows(out, _LOGIT_CODES, "out")
+        if n != B or d != C:
             raise ValueError("out must be [B, C]")
-        rc = lib().class_logits_int8(_ptr(x_codes), _ptr(x_scale), _ptr(w_codes), _ptr(w_scale), _ptr(bias), ct.c_int64(C), ct.c_int(D),
-                                     ct.c_int(B), ct.c_float(scale), _ptr(out), ct.c_int(_FLOAT_CODES[out.dtype]), ct.c_int64(ldl),
-                                     _stream(stream))
+        rc = L.class_logits_int8(x_codes.data_ptr(), x_scale.data_ptr(), w_codes.data_ptr(), w_scale.data_ptr(), _at(bias), C, D, B, scale,
+                                 out.data_ptr(), code, ldl, raw)
     _check("class_logits_int8", rc)
     return out
 
@@ -861,39 +880,40 @@ def class_logits_adjust(logits, seen=None, seen_max=None, n_prompt=None, repetit
     [B + 1]): lists laid end to end, of at most seen_max / bias_max entries (default: all that the array holds; say it where it is
     known, short lists are faster).  n_prompt int32 [B]; repetition, presence, frequency fp32 [B]; allowed: int32 [n_masks,
     >= ceil(C / 32)] words of bits; mask_row int32 [B]."""
-    types = (torch.bfloat16, torch.float32)
-    ldl = _rows(logits, types, "logits")
-    B, C = logits.shape
-    out = logits if out is None else out
-    ldo = _rows(out, types, "out")
-    if out.dtype != logits.dtype or out.shape != logits.shape:
-        raise ValueError("out must have the logits' type and shape")
+    code, B, C, ldl = _rows(logits, _LOGIT_CODES, "logits")
+    if out is None or out is logits:
+        out, ldo = logits, ldl
+    else:
+        other, n, d, ldo = _rows(out, _LOGIT_CODES, "out")
+        if (other, n, d) != (code, B, C):
+            raise ValueError("out must have the logits' type and shape")
     s_ids, s_off = seen if seen is not None else (None, None)
     b_ids, b_val, b_off = bias if bias is not None else (None, None, None)
-    for t, dtype, n, name in ((s_off, torch.int64, B + 1, "seen offsets"), (b_off, torch.int64, B + 1, "bias offsets"),
-                              (n_prompt, torch.int32, B, "n_prompt"), (repetition, torch.float32, B, "repetition"),
-                              (presence, torch.float32, B, "presence"), (frequency, torch.float32, B, "frequency"),
-                              (mask_row, torch.int32, B, "mask_row"), (s_ids, torch.int32, None, "seen ids"),
-                              (b_ids, torch.int32, None, "bias ids"), (b_val, torch.float32, b_ids.numel() if b_ids is not None else 0, "bias values")):
-        if t is not None and _need(t, dtype, name).numel() != n and n is not None:
-            raise ValueError(f"{name} must have {n} entries")
-    n_masks, lda = 0, 0
+    s_len, b_len = 0 if s_ids is None else s_ids.numel(), 0 if b_ids is None else b_ids.numel()
+    _list(s_ids, torch.int32, s_len, "seen ids")
+    _list(s_off, torch.int64, B + 1, "seen offsets")
+    _list(n_prompt, torch.int32, B, "n_prompt")
+    _list(repetition, torch.float32, B, "repetition")
+    _list(presence, torch.float32, B, "presence")
+    _list(frequency, torch.float32, B, "frequency")
+    _list(b_ids, torch.int32, b_len, "bias ids")
+    _list(b_val, torch.float32, b_len, "bias values")
+    _list(b_off, torch.int64, B + 1, "bias offsets")
+    _list(mask_row, torch.int32, B, "mask_row")
+    _list(dev_status, torch.int32, 1, "dev_status")
+    n_masks = lda = 0
     if allowed is not None:
-        lda = _rows(allowed, (torch.int32,), "allowed")
-        n_masks = allowed.shape[0]
-        if allowed.shape[1] < (C + 31) // 32 or n_masks < 1 or (mask_row is None and n_masks < B):
+        _, n_masks, words, lda = _rows(allowed, {torch.int32: 0}, "allowed")
+        if words < (C + 31) // 32 or n_masks < 1 or (mask_row is None and n_masks < B):
             raise ValueError("allowed must be [n_masks, >= ceil(C / 32)], a mask per request without mask_row")
     elif mask_row is not None:
         raise ValueError("mask_row without allowed")
-    s_len, b_len = (0 if t is None else t.numel() for t in (s_ids, b_ids))
-    with _Home(_home(stream, logits, out, s_ids, s_off, n_prompt, repetition, presence, frequency, b_ids, b_val, b_off, allowed, mask_row,
-                     dev_status), stream):
-        dev_status = _status(logits.device, dev_status)
+    launch = _Launch(stream, logits, out, s_ids, s_off, n_prompt, repetition, presence, frequency, b_ids, b_val, b_off, allowed, mask_row, dev_status)
+    with launch as raw:
         rc = lib().class_logits_adjust(
-            _ptr(logits), ct.c_int64(ldl), _ptr(out), ct.c_int64(ldo), ct.c_int(_FLOAT_CODES[logits.dtype]), ct.c_int64(C), ct.c_int64(c0),
-            ct.c_int64(c0 + C if Cg is None else Cg), ct.c_int(B), _ptr(s_off), _ptr(s_ids), ct.c_int64(s_len),
-            ct.c_int(min(s_len, s_len if seen_max is None else seen_max)), _ptr(n_prompt), _ptr(repetition), _ptr(presence), _ptr(frequency),
-            _ptr(b_off), _ptr(b_ids), _ptr(b_val), ct.c_int64(b_len), ct.c_int(min(b_len, b_len if bias_max is None else bias_max)),
-            _ptr(allowed), ct.c_int64(lda), ct.c_int(n_masks), _ptr(mask_row), _ptr(dev_status), _stream(stream))
+            logits.data_ptr(), ldl, out.data_ptr(), ldo, code, C, c0, c0 + C if Cg is None else Cg, B, _at(s_off), _at(s_ids), s_len,
+            s_len if seen_max is None else min(s_len, seen_max), _at(n_prompt), _at(repetition), _at(presence), _at(frequency), _at(b_off),
+            _at(b_ids), _at(b_val), b_len, b_len if bias_max is None else min(b_len, bias_max), _at(allowed), lda, n_masks, _at(mask_row),
+            _at(dev_status), raw)
     _check("class_logits_adjust", rc)
     return out

@@ -61,13 +61,43 @@ __device__ __forceinline__ int cl_code(float v, double inv, double a) {
     }
     return k;
 }
-__device__ __forceinline__ double cl_wave_sum_d(double v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        const int lo = __shfl_xor(__double2loint(v), o, 64), hi = __shfl_xor(__double2hiint(v), o, 64);
-        v += __hiloint2double(hi, lo);
+// Reductions of N = 1 or 4 values a lane over the wavefront at once.  Of four, every lane passes two on to its neighbour and keeps two, then
+// one and one; lanes of equal number modulo 4 then hold the same value's parts, and go on as in ks_wave_sum: 7 steps for four values
+// instead of 24.  Value i ends up in lane 63, or in lane 60 + i / 2 + i % 2 * 2.
+struct ClMaxI {
+    typedef int T;
+    static __device__ __forceinline__ int op(int a, int b) { return max(a, b); }
+    template <int CTRL, int ROWS> static __device__ __forceinline__ int move(int v) { return KS_DPP(0, v, CTRL, ROWS); }
+    static __device__ __forceinline__ int lane(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
+};
+struct ClSumD {
+    typedef double T;
+    static __device__ __forceinline__ double op(double a, double b) { return a + b; }
+    template <int CTRL, int ROWS> static __device__ __forceinline__ double move(double v) {
+        return __hiloint2double(KS_DPP(0, __double2hiint(v), CTRL, ROWS), KS_DPP(0, __double2loint(v), CTRL, ROWS));
     }
-    return v;
+    static __device__ __forceinline__ double lane(double v, int l) {
+        return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), l), __builtin_amdgcn_readlane(__double2loint(v), l));
+    }
+};
+template <class R, int N> __device__ __forceinline__ void cl_wave_reduce(typename R::T (&t)[N]) { // no value is below 0: 0 is neutral
+    static_assert(N == 1 || N == 4, "");
+    typename R::T v = t[0];
+    if constexpr (N == 4) {
+        const bool b0 = threadIdx.x & 1, b1 = threadIdx.x & 2;
+        const typename R::T u0 = R::op(b0 ? t[2] : t[0], R::template move<0xB1, 0xf>(b0 ? t[0] : t[2])); // quad_perm [1, 0, 3, 2]
+        const typename R::T u1 = R::op(b0 ? t[3] : t[1], R::template move<0xB1, 0xf>(b0 ? t[1] : t[3]));
+        v = R::op(b1 ? u1 : u0, R::template move<0x4E, 0xf>(b1 ? u0 : u1)); // quad_perm [2, 3, 0, 1]
+    } else {
+        v = R::op(v, R::template move<0x111, 0xf>(v));
+        v = R::op(v, R::template move<0x112, 0xf>(v));
+    }
+    v = R::op(v, R::template move<0x114, 0xf>(v));
+    v = R::op(v, R::template move<0x118, 0xf>(v));
+    v = R::op(v, R::template move<0x142, 0xa>(v));
+    v = R::op(v, R::template move<0x143, 0xc>(v));
+#pragma unroll
+    for (int i = 0; i < N; ++i) t[i] = R::lane(v, N == 1 ? 63 : 60 + i / 2 + i % 2 * 2);
 }
 
 // A workgroup takes RB consecutive slots (32: a whole block, or 8) of a block of 32 rows, each of its eight wavefronts RB / 8 of them at
@@ -121,19 +151,27 @@ cl_quantize_kernel(const IN *__restrict__ V, int64_t n, int D, int64_t ldv, uint
                     }
                 }
         }
+    if (!RAW) cl_wave_reduce<ClMaxI>(top);
+    if (flags & KS_QUANT_NORMALIZE) cl_wave_reduce<ClSumD>(ss);
+    // the divisions and the root of row i in the lanes i modulo RW, all rows at once
+    int my_top = top[0];
+    double my_ss = ss[0];
+#pragma unroll
+    for (int i = 1; i < RW; ++i)
+        if (lane % RW == i) { my_top = top[i]; my_ss = ss[i]; }
+    const double my_a = my_top < 0x7F800000 ? (double)__int_as_float(my_top) : 0.0; // not finite: codes 0
+    const double my_inv = my_a > 0.0 ? 127.0 / my_a : 0.0;
+    if (!RAW) {
+        double scale = my_a / 127.0;
+        if ((flags & KS_QUANT_NORMALIZE) && my_a > 0.0) scale /= sqrt(my_ss);
+        const int64_t row = row_of(lane % RW);
+        if (lane < RW && row < n) row_scale[row] = my_top < 0x7F800000 ? (float)scale : __int_as_float(0x7FC00000);
+    }
     double a[RW], inv[RW];
 #pragma unroll
     for (int i = 0; i < RW; ++i) {
-        top[i] = ks_wave_max_i(top[i]);
-        a[i] = top[i] < 0x7F800000 ? (double)__int_as_float(top[i]) : 0.0; // not finite: codes 0
-        inv[i] = a[i] > 0.0 ? 127.0 / a[i] : 0.0;
-        if (RAW) continue;
-        double s = a[i] / 127.0;
-        if (flags & KS_QUANT_NORMALIZE) {
-            const double norm = sqrt(cl_wave_sum_d(ss[i]));
-            if (a[i] > 0.0) s /= norm;
-        }
-        if (lane == 0 && row_of(i) < n) row_scale[row_of(i)] = top[i] < 0x7F800000 ? (float)s : __int_as_float(0x7FC00000);
+        a[i] = ClSumD::lane(my_a, i);
+        inv[i] = ClSumD::lane(my_inv, i);
     }
     for (int d0 = 0; d0 < D; d0 += DC) {
         if (RAW || D > DC) load(d0);
@@ -175,7 +213,8 @@ static void cl_quantize(const void *V, int64_t n, int D, int64_t ldv, uint32_t f
                                n, D, ldv, flags, codes, row_scale, b0);
     };
     // whole blocks where there are enough of them and a wavefront holds four rows; else a row a wavefront
-    if (blocks >= 512 && D <= 512) go(cl_quantize_kernel<32, 2, IN, VEC>, 32);
+    if (blocks >= 512 && D <= 256) go(cl_quantize_kernel<32, 1, IN, VEC>, 32);
+    else if (blocks >= 512 && D <= 512) go(cl_quantize_kernel<32, 2, IN, VEC>, 32);
     else if (blocks >= 512 && D <= 1024) go(cl_quantize_kernel<32, 4, IN, VEC>, 32);
     else if (D <= 512) go(cl_quantize_kernel<8, 2, IN, VEC>, 8);
     else go(cl_quantize_kernel<8, 16, IN, VEC>, 8);
@@ -837,9 +876,8 @@ __device__ __forceinline__ int64_t cl_column(const ClAdjust &a, int32_t id, int 
     const int64_t c = (int64_t)id - a.c0;
     return c < 0 || c >= a.C ? -1 : c;
 }
-// steps 1 and 2 on column c of request b.  seen: bit 0: in the prompt, the rest: occurrences behind it; j: entry of the bias list or -1
-template <typename T> __device__ __forceinline__ void cl_adjust_one(const ClAdjust &a, int b, int64_t c, uint32_t seen, int j, int64_t bias_first) {
-    float z = cl_load((const T *)a.in + b * a.ldl + c);
+// steps 1 and 2 on a logit of request b.  seen: bit 0: in the prompt, the rest: occurrences behind it; j: entry of the bias list or -1
+__device__ __forceinline__ float cl_adjusted(const ClAdjust &a, int b, float z, uint32_t seen, int j, int64_t bias_first) {
     if (seen) {
         if (a.repetition) {
             const float r = a.repetition[b];
@@ -848,26 +886,27 @@ template <typename T> __device__ __forceinline__ void cl_adjust_one(const ClAdju
         const uint32_t n = seen >> 1;
         if (n) z -= (a.frequency ? a.frequency[b] * (float)n : 0.f) + (a.presence ? a.presence[b] : 0.f);
     }
-    if (j >= 0) z += a.bias_values[bias_first + j];
-    cl_store((T *)a.out + b * a.ldo + c, z);
+    return j >= 0 ? z + a.bias_values[bias_first + j] : z;
+}
+__device__ __forceinline__ bool cl_masked(const ClAdjust &a, int m, int64_t c) { // m: cl_mask_of's
+    return m >= 0 && !(a.allowed[(int64_t)m * a.ld_allowed + (c >> 5)] >> (c & 31) & 1);
 }
 
 // masks, and where COPY the logits that stay as they are; a workgroup takes a stretch of one row
 #define CLM_U 4
-template <typename T, bool COPY, bool VEC>
-__global__ void __launch_bounds__(CL_NT) cl_mask_kernel(ClAdjust a, int per_row) {
+template <typename T, bool COPY, bool VEC, int NT>
+__device__ __forceinline__ void cl_mask_part(const ClAdjust &a, int b, int part) {
     constexpr int E = VEC ? 16 / (int)sizeof(T) : 1;
-    const int b = a.row0 + blockIdx.x / per_row;
     const int m = cl_mask_of(a, b);
     if (!COPY && m < 0) return;
     const uint32_t *bits = m < 0 ? nullptr : a.allowed + (int64_t)m * a.ld_allowed;
     const T *in = (const T *)a.in + b * a.ldl;
     T *out = (T *)a.out + b * a.ldo;
     const T none = cl_minus_inf<T>();
-    const int64_t first = ((int64_t)(blockIdx.x % per_row) * CLM_U * CL_NT + threadIdx.x) * E;
+    const int64_t first = ((int64_t)part * CLM_U * NT + threadIdx.x) * E;
 #pragma unroll
     for (int u = 0; u < CLM_U; ++u) {
-        const int64_t c = first + (int64_t)u * CL_NT * E;
+        const int64_t c = first + (int64_t)u * NT * E;
         if (c >= a.C) break;
         const uint32_t w = bits ? bits[c >> 5] >> (c & 31) : ~0u;
         if (E > 1 && c + E <= a.C) {
@@ -895,7 +934,77 @@ __global__ void __launch_bounds__(CL_NT) cl_mask_kernel(ClAdjust a, int per_row)
     }
 }
 
-// Lists: a workgroup has one count and one bias entry for each of CLR classes in LDS and takes the request's entries among them.
+template <typename T, bool COPY, bool VEC>
+__global__ void __launch_bounds__(CL_NT) cl_mask_kernel(ClAdjust a, int per_row) {
+    cl_mask_part<T, COPY, VEC, CL_NT>(a, a.row0 + blockIdx.x / per_row, blockIdx.x % per_row);
+}
+
+// Lists of a request that a hash table of SLOTS classes in LDS holds (three quarters of the slots): each of them counts the class's occurrences
+// and keeps the last of its biases.  The entry that takes a slot fetches the logit at once, so that it arrives while the others
+// are counted, and adjusts it afterwards; nothing is read or written but the lists and the logits of their classes.
+// MASKS > 0: the workgroups behind the requests' carry out the masks in place (1: element by element, 2: vectors): no logit
+// belongs to both, so that one launch does for both.
+template <typename T, int SLOTS, int NT, int MASKS>
+__global__ void __launch_bounds__(NT) cl_hash_kernel(ClAdjust a, int requests, int per_row) {
+    constexpr int K = SLOTS / 4 * 3 / NT; // entries of a thread
+    static_assert(K * NT == SLOTS / 4 * 3, "");
+    __shared__ uint32_t s_key[SLOTS], s_seen[SLOTS]; // column + 1, 0: free
+    __shared__ int s_bias[SLOTS];
+    if (MASKS && (int)blockIdx.x >= requests) {
+        const int i = blockIdx.x - requests;
+        cl_mask_part<T, false, MASKS == 2, NT>(a, a.row0 + i / per_row, i % per_row);
+        return;
+    }
+    const int b = a.row0 + blockIdx.x;
+    int64_t sf = 0, bf = 0;
+    const int ns = cl_list(a.seen_offsets, a.seen_len, a.seen_max, b, &sf, a.dev_status);
+    const int nb = cl_list(a.bias_offsets, a.bias_len, a.bias_max, b, &bf, a.dev_status);
+    const int m = cl_mask_of(a, b);
+    if (ns + nb == 0) return;
+    const int prompt = a.n_prompt ? a.n_prompt[b] : 0;
+    for (int e = threadIdx.x; e < SLOTS; e += NT) { s_key[e] = 0; s_seen[e] = 0; s_bias[e] = -1; }
+    int32_t id[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+        const int e = i * NT + threadIdx.x;
+        id[i] = e < ns ? a.seen_ids[sf + e] : e < ns + nb ? a.bias_ids[bf + e - ns] : -1;
+    }
+    __syncthreads();
+    const T *in = (const T *)a.in + b * a.ldl;
+    T *out = (T *)a.out + b * a.ldo;
+    int slot[K]; // where this thread's entry was the one to take it, else -1
+    float z[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+        const int e = i * NT + threadIdx.x;
+        const int64_t c = cl_column(a, id[i], e < ns ? KS_DEV_BAD_LABEL : KS_DEV_BAD_INDEX);
+        slot[i] = -1;
+        if (c < 0) continue;
+        const uint32_t key = (uint32_t)c + 1;
+        uint32_t at = __umulhi(key * 0x9E3779B1u, SLOTS);
+        for (;;) { // there are more slots than entries
+            const uint32_t was = atomicCAS(&s_key[at], 0u, key);
+            if (was == 0) {
+                if (!cl_masked(a, m, c)) {
+                    slot[i] = (int)at;
+                    z[i] = cl_load(in + c);
+                }
+                break;
+            }
+            if (was == key) break;
+            at = at + 1 == SLOTS ? 0 : at + 1;
+        }
+        if (e >= ns) atomicMax(&s_bias[at], e - ns);
+        else if (e < prompt) atomicOr(&s_seen[at], 1u);
+        else atomicAdd(&s_seen[at], 2u);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+        if (slot[i] >= 0) cl_store(out + s_key[slot[i]] - 1, cl_adjusted(a, b, z[i], s_seen[slot[i]], s_bias[slot[i]], bf));
+}
+
+// Longer lists: a workgroup has a count and a bias entry for each of CLR classes and takes the request's entries among them.
 #define CLR 8192
 template <typename T>
 __global__ void __launch_bounds__(1024) cl_range_kernel(ClAdjust a, int ranges) {
@@ -925,35 +1034,49 @@ __global__ void __launch_bounds__(1024) cl_range_kernel(ClAdjust a, int ranges) 
     for (int e = threadIdx.x; e < CLR; e += 1024) {
         const uint32_t seen = s_seen[e];
         const int j = s_bias[e];
-        if (!seen && j < 0) continue;
         const int64_t c = r0 + e;
-        if (m >= 0 && !(a.allowed[(int64_t)m * a.ld_allowed + (c >> 5)] >> (c & 31) & 1)) continue; // masked
-        cl_adjust_one<T>(a, b, c, seen, j, bf);
+        if ((!seen && j < 0) || cl_masked(a, m, c)) continue;
+        cl_store((T *)a.out + b * a.ldo + c, cl_adjusted(a, b, cl_load((const T *)a.in + b * a.ldl + c), seen, j, bf));
     }
 }
 
 #define CL_MAX_GRID (1 << 21) /* workgroups of a launch: threads are counted in 32 bits */
-// launch(a, blocks) for stretches of rows that fit into a launch, per_row workgroups each
+// launch(a, rows) for stretches of rows from a.row0 on that fit into a launch, per_row workgroups each
 template <class F> static void cl_rows(ClAdjust a, int per_row, F launch) {
     const int rows = per_row < CL_MAX_GRID ? CL_MAX_GRID / per_row : 1, B = a.B;
-    for (a.row0 = 0; a.row0 < B; a.row0 += rows) launch(a, dim3((unsigned)per_row * (unsigned)(rows < B - a.row0 ? rows : B - a.row0)));
+    for (a.row0 = 0; a.row0 < B; a.row0 += rows) launch(a, rows < B - a.row0 ? rows : B - a.row0);
 }
 
 template <typename T> static void cl_adjust(const ClAdjust &args, hipStream_t st) {
     const bool copy = args.in != args.out;
     const bool vec = ((uintptr_t)args.in | (uintptr_t)args.out | (uintptr_t)(args.ldl * sizeof(T)) | (uintptr_t)(args.ldo * sizeof(T))) % 16 == 0;
-    if (copy || args.allowed) {
-        const int per_row = (int)ks_ceil_div(args.C, (int64_t)CLM_U * CL_NT * (vec ? 16 / (int)sizeof(T) : 1));
-        cl_rows(args, per_row, [&](const ClAdjust &a, dim3 grid) {
+    const int entries = (args.seen_offsets ? args.seen_max : 0) + (args.bias_offsets ? args.bias_max : 0), E = vec ? 16 / (int)sizeof(T) : 1;
+    const bool fused = !copy && args.allowed && entries > 0 && entries <= 3072;
+    if ((copy || args.allowed) && !fused) {
+        const int per_row = (int)ks_ceil_div(args.C, (int64_t)CLM_U * CL_NT * E);
+        cl_rows(args, per_row, [&](const ClAdjust &a, int rows) {
+            const dim3 grid((unsigned)per_row * (unsigned)rows);
             if (copy && vec) hipLaunchKernelGGL((cl_mask_kernel<T, true, true>), grid, dim3(CL_NT), 0, st, a, per_row);
             else if (copy) hipLaunchKernelGGL((cl_mask_kernel<T, true, false>), grid, dim3(CL_NT), 0, st, a, per_row);
             else if (vec) hipLaunchKernelGGL((cl_mask_kernel<T, false, true>), grid, dim3(CL_NT), 0, st, a, per_row);
             else hipLaunchKernelGGL((cl_mask_kernel<T, false, false>), grid, dim3(CL_NT), 0, st, a, per_row);
         });
     }
-    if ((args.seen_offsets && args.seen_max) || (args.bias_offsets && args.bias_max)) {
+    if (entries == 0) return;
+    const auto hash = [&](auto alone, auto with_elements, auto with_vectors, int nt) {
+        const int per_row = fused ? (int)ks_ceil_div(args.C, (int64_t)CLM_U * nt * E) : 0;
+        cl_rows(args, 1 + per_row, [&](const ClAdjust &a, int rows) {
+            hipLaunchKernelGGL(!fused ? alone : vec ? with_vectors : with_elements, dim3((unsigned)rows * (unsigned)(1 + per_row)), dim3(nt), 0, st, a, rows, per_row);
+        });
+    };
+    if (entries <= 768) hash(cl_hash_kernel<T, 1024, 256, 0>, cl_hash_kernel<T, 1024, 256, 1>, cl_hash_kernel<T, 1024, 256, 2>, 256);
+    else if (entries <= 3072) hash(cl_hash_kernel<T, 4096, 512, 0>, cl_hash_kernel<T, 4096, 512, 1>, cl_hash_kernel<T, 4096, 512, 2>, 512);
+    else if (entries <= 9216) hash(cl_hash_kernel<T, 12288, 1024, 0>, cl_hash_kernel<T, 12288, 1024, 0>, cl_hash_kernel<T, 12288, 1024, 0>, 1024);
+    else {
         const int ranges = (int)ks_ceil_div(args.C, CLR);
-        cl_rows(args, ranges, [&](const ClAdjust &a, dim3 grid) { hipLaunchKernelGGL(cl_range_kernel<T>, grid, dim3(1024), 0, st, a, ranges); });
+        cl_rows(args, ranges, [&](const ClAdjust &a, int rows) {
+            hipLaunchKernelGGL(cl_range_kernel<T>, dim3((unsigned)ranges * (unsigned)rows), dim3(1024), 0, st, a, ranges);
+        });
     }
 }
 
