@@ -763,59 +763,47 @@ def grad_topk_select(g, plan: GradTopkPlan, out_idx=None, out_val=None, ws=None,
 # ---------------------------------------------------------------------------------------------------
 QUANT_CLASSES, QUANT_NORMALIZE = 1, 2  # KS_QUANT_*
 _ROW_CODES = {torch.bfloat16: 0, torch.float32: 1, torch.int8: 2}
-_LOGIT_CODES = {torch.bfloat16: 0, torch.float32: 1}
+_LOGIT_CODES, _WORD_CODES = {torch.bfloat16: 0, torch.float32: 1}, {torch.int32: 0}
 
 
 def _at(t):
     return None if t is None else t.data_ptr()
 
 
-class _Launch:
-    """The device that all tensors of a call are on, and its stream there, both current while outputs are allocated and kernels
-    launched.  (Entered only where they are not current already.)"""
-
-    def __init__(self, stream, first, *others):
-        dev = self.device = first.device
-        index = first.get_device()
-        for t in others:
-            if t is not None and t.get_device() != index:
-                raise ValueError(f"tensors of one call on {dev} and {t.device}")
-        self.inner = None
-        if stream is not None:
-            if stream.device != dev:
-                raise ValueError(f"stream of {stream.device} for tensors on {dev}")
-            self.inner = torch.cuda.stream(stream)
-        elif index != torch.cuda.current_device():
-            self.inner = torch.cuda.stream(torch.cuda.current_stream(dev))
-
-    def __enter__(self):
-        if self.inner is not None:
-            self.inner.__enter__()
-        return torch._C._cuda_getCurrentRawStream(self.device.index)
-
-    def __exit__(self, *e):
-        if self.inner is not None:
-            self.inner.__exit__(*e)
-
-
-def _rows(t, types, name):
-    """A device matrix of one of `types` whose rows are contiguous (any distance from row to row): -> type code, rows, columns, distance."""
+def _rows(t, types, name, dev=None):
+    """A device matrix of one of `types` whose rows are contiguous (any distance from row to row), on device `dev` where that is given:
+    -> type code, rows, columns, distance."""
     code = types.get(t.dtype)
     if code is None or not t.is_cuda or t.dim() != 2:
         raise TypeError(f"{name} must be a 2-D device tensor of {' or '.join(str(x) for x in types)}")
     (n, d), (ld, step) = t.shape, t.stride()
     if (step != 1 and d > 1) or (ld < d and n > 1):
         raise TypeError(f"{name} must have contiguous rows")
-    return code, n, d, max(ld, d)
+    if dev is not None and t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, other tensors of the call on cuda:{dev}")
+    return code, n, d, ld if ld > d else d
 
 
-def _list(t, dtype, n, name):
-    """A contiguous device tensor of n elements, or none."""
-    if t is not None and (t.dtype != dtype or not t.is_cuda or not t.is_contiguous()):
+def _list(t, dtype, n, name, dev):
+    """A contiguous tensor of n elements on device `dev`."""
+    if t.dtype is not dtype or not t.is_contiguous() or t.get_device() != dev:
+        if t.dtype is dtype and t.is_cuda and t.is_contiguous():
+            raise ValueError(f"{name} is on {t.device}, other tensors of the call on cuda:{dev}")
         raise TypeError(f"{name} must be a contiguous device tensor of {dtype}")
-    if t is not None and t.numel() != n:
+    if t.numel() != n:
         raise ValueError(f"{name} must have {n} elements")
-    return t
+
+
+def _launch(dev, stream, call):
+    """call(raw stream) with device `dev` and the call's stream current, so that what it allocates belongs to that stream."""
+    if stream is None and dev == torch._C._cuda_getDevice():
+        return call(torch._C._cuda_getCurrentRawStream(dev))
+    if stream is None:
+        stream = torch.cuda.current_stream(dev)
+    elif stream.device_index != dev:
+        raise ValueError(f"stream of {stream.device} for tensors on cuda:{dev}")
+    with torch.cuda.stream(stream):
+        return call(stream.cuda_stream)
 
 
 def class_codes_bytes(n, D, classes=False) -> int:
@@ -830,47 +818,51 @@ def class_quantize_rows(V, classes=False, normalize=False, codes=None, row_scale
     code, n, D, ldv = _rows(V, _ROW_CODES, "V")
     if code == 2 and (normalize or row_scale is not None):
         raise ValueError("int8 rows are taken as they are: no normalize, no row_scale")
-    flags = (QUANT_CLASSES if classes else 0) | (QUANT_NORMALIZE if normalize else 0)
+    dev, flags = V.get_device(), (QUANT_CLASSES if classes else 0) | (QUANT_NORMALIZE if normalize else 0)
     need = L.class_codes_bytes(n, D, flags)
-    _list(codes, torch.int8, need, "codes")
-    _list(row_scale, torch.float32, n, "row_scale")
-    launch = _Launch(stream, V, codes, row_scale)
-    with launch as raw:
-        if codes is None:
-            codes = torch.empty(need, dtype=torch.int8, device=launch.device)
-        if row_scale is None and code != 2:
-            row_scale = torch.empty(n, dtype=torch.float32, device=launch.device)
-        rc = L.class_quantize_rows(V.data_ptr(), code, n, D, ldv, flags, codes.data_ptr(), _at(row_scale), raw)
-    _check("class_quantize_rows", rc)
-    return codes, row_scale
+    if codes is not None:
+        _list(codes, torch.int8, need, "codes", dev)
+    if row_scale is not None:
+        _list(row_scale, torch.float32, n, "row_scale", dev)
+
+    def call(raw):
+        c = codes if codes is not None else torch.empty(need, dtype=torch.int8, device=V.device)
+        s = row_scale if row_scale is not None or code == 2 else torch.empty(n, dtype=torch.float32, device=V.device)
+        _check("class_quantize_rows", L.class_quantize_rows(V.data_ptr(), code, n, D, ldv, flags, c.data_ptr(), _at(s), raw))
+        return c, s
+
+    return _launch(dev, stream, call)
 
 
 def class_logits_int8(x_codes, x_scale, w_codes, w_scale, scale, bias=None, out=None, dtype=torch.float32, stream=None):
     """Logits [B, C] of B feature rows against all C classes, from the codes and scales of class_quantize_rows (w_codes made with
     classes=True).  Without `out` (bf16 or fp32, rows may lie apart) the result is of `dtype` and its rows lie on 128-byte lines."""
     L = lib()
-    B, C = x_scale.numel(), w_scale.numel()
+    B, C, dev = x_scale.numel(), w_scale.numel(), x_codes.get_device()
     if B < 1 or C < 1:
         raise ValueError("x_scale [B] and w_scale [C] must not be empty")
     D = x_codes.numel() // ((B + 31) // 32 * 32)  # a multiple of 32: what lies beyond the rows' own depth is 0
-    _list(x_codes, torch.int8, L.class_codes_bytes(B, D, 0), "x_codes (of B feature rows)")
-    _list(w_codes, torch.int8, L.class_codes_bytes(C, D, QUANT_CLASSES), "w_codes (of C class rows of the features' depth)")
-    _list(x_scale, torch.float32, B, "x_scale")
-    _list(w_scale, torch.float32, C, "w_scale")
-    _list(bias, torch.float32, C, "bias")
-    launch = _Launch(stream, x_codes, x_scale, w_codes, w_scale, bias, out)
-    with launch as raw:
-        if out is None:
-            if dtype not in _LOGIT_CODES:
-                raise TypeError("dtype must be torch.bfloat16 or torch.float32")
-            out = torch.empty((B, (C + 63) // 64 * 64), dtype=dtype, device=launch.device)[:, :C]
-        code, n, d, ldl = _rows(out, _LOGIT_CODES, "out")
+    if dev < 0:
+        raise TypeError("x_codes must be a device tensor")
+    _list(x_codes, torch.int8, L.class_codes_bytes(B, D, 0), "x_codes (of B feature rows)", dev)
+    _list(w_codes, torch.int8, L.class_codes_bytes(C, D, QUANT_CLASSES), "w_codes (of C class rows of the features' depth)", dev)
+    _list(x_scale, torch.float32, B, "x_scale", dev)
+    _list(w_scale, torch.float32, C, "w_scale", dev)
+    if bias is not None:
+        _list(bias, torch.float32, C, "bias", dev)
+    if out is None and dtype not in _LOGIT_CODES:
+        raise TypeError("dtype must be torch.bfloat16 or torch.float32")
+
+    def call(raw):
+        z = out if out is not None else torch.empty((B, (C + 63) // 64 * 64), dtype=dtype, device=x_codes.device)[:, :C]
+        code, n, d, ldl = _rows(z, _LOGIT_CODES, "out", dev)
         if n != B or d != C:
             raise ValueError("out must be [B, C]")
-        rc = L.class_logits_int8(x_codes.data_ptr(), x_scale.data_ptr(), w_codes.data_ptr(), w_scale.data_ptr(), _at(bias), C, D, B, scale,
-                                 out.data_ptr(), code, ldl, raw)
-    _check("class_logits_int8", rc)
-    return out
+        _check("class_logits_int8", L.class_logits_int8(x_codes.data_ptr(), x_scale.data_ptr(), w_codes.data_ptr(), w_scale.data_ptr(), _at(bias),
+                                                        C, D, B, scale, z.data_ptr(), code, ldl, raw))
+        return z
+
+    return _launch(dev, stream, call)
 
 
 def class_logits_adjust(logits, seen=None, seen_max=None, n_prompt=None, repetition=None, presence=None, frequency=None, bias=None,
@@ -879,41 +871,53 @@ def class_logits_adjust(logits, seen=None, seen_max=None, n_prompt=None, repetit
     or into `out`; returns the result.  seen = (ids int32, offsets int64 [B + 1]), bias = (ids int32, values fp32, offsets int64
     [B + 1]): lists laid end to end, of at most seen_max / bias_max entries (default: all that the array holds; say it where it is
     known, short lists are faster).  n_prompt int32 [B]; repetition, presence, frequency fp32 [B]; allowed: int32 [n_masks,
-    >= ceil(C / 32)] words of bits; mask_row int32 [B]."""
+    >= ceil(C / 32)] words of bits; mask_row int32 [B]; dev_status int32 [1], None: nothing is reported."""
     code, B, C, ldl = _rows(logits, _LOGIT_CODES, "logits")
+    dev = logits.get_device()
     if out is None or out is logits:
         out, ldo = logits, ldl
     else:
-        other, n, d, ldo = _rows(out, _LOGIT_CODES, "out")
-        if (other, n, d) != (code, B, C):
+        other, n, d, ldo = _rows(out, _LOGIT_CODES, "out", dev)
+        if other != code or n != B or d != C:
             raise ValueError("out must have the logits' type and shape")
-    s_ids, s_off = seen if seen is not None else (None, None)
-    b_ids, b_val, b_off = bias if bias is not None else (None, None, None)
-    s_len, b_len = 0 if s_ids is None else s_ids.numel(), 0 if b_ids is None else b_ids.numel()
-    _list(s_ids, torch.int32, s_len, "seen ids")
-    _list(s_off, torch.int64, B + 1, "seen offsets")
-    _list(n_prompt, torch.int32, B, "n_prompt")
-    _list(repetition, torch.float32, B, "repetition")
-    _list(presence, torch.float32, B, "presence")
-    _list(frequency, torch.float32, B, "frequency")
-    _list(b_ids, torch.int32, b_len, "bias ids")
-    _list(b_val, torch.float32, b_len, "bias values")
-    _list(b_off, torch.int64, B + 1, "bias offsets")
-    _list(mask_row, torch.int32, B, "mask_row")
-    _list(dev_status, torch.int32, 1, "dev_status")
-    n_masks = lda = 0
+    s_ids = s_off = b_ids = b_val = b_off = None
+    s_len = b_len = n_masks = lda = 0
+    if seen is not None:
+        s_ids, s_off = seen
+        s_len = s_ids.numel()
+        _list(s_ids, torch.int32, s_len, "seen ids", dev)
+        _list(s_off, torch.int64, B + 1, "seen offsets", dev)
+    if bias is not None:
+        b_ids, b_val, b_off = bias
+        b_len = b_ids.numel()
+        _list(b_ids, torch.int32, b_len, "bias ids", dev)
+        _list(b_val, torch.float32, b_len, "bias values", dev)
+        _list(b_off, torch.int64, B + 1, "bias offsets", dev)
+    if n_prompt is not None:
+        _list(n_prompt, torch.int32, B, "n_prompt", dev)
+    if repetition is not None:
+        _list(repetition, torch.float32, B, "repetition", dev)
+    if presence is not None:
+        _list(presence, torch.float32, B, "presence", dev)
+    if frequency is not None:
+        _list(frequency, torch.float32, B, "frequency", dev)
+    if dev_status is not None:
+        _list(dev_status, torch.int32, 1, "dev_status", dev)
+    if mask_row is not None:
+        if allowed is None:
+            raise ValueError("mask_row without allowed")
+        _list(mask_row, torch.int32, B, "mask_row", dev)
     if allowed is not None:
-        _, n_masks, words, lda = _rows(allowed, {torch.int32: 0}, "allowed")
+        _, n_masks, words, lda = _rows(allowed, _WORD_CODES, "allowed", dev)
         if words < (C + 31) // 32 or n_masks < 1 or (mask_row is None and n_masks < B):
             raise ValueError("allowed must be [n_masks, >= ceil(C / 32)], a mask per request without mask_row")
-    elif mask_row is not None:
-        raise ValueError("mask_row without allowed")
-    launch = _Launch(stream, logits, out, s_ids, s_off, n_prompt, repetition, presence, frequency, b_ids, b_val, b_off, allowed, mask_row, dev_status)
-    with launch as raw:
-        rc = lib().class_logits_adjust(
+
+    def call(raw):
+        return lib().class_logits_adjust(
             logits.data_ptr(), ldl, out.data_ptr(), ldo, code, C, c0, c0 + C if Cg is None else Cg, B, _at(s_off), _at(s_ids), s_len,
-            s_len if seen_max is None else min(s_len, seen_max), _at(n_prompt), _at(repetition), _at(presence), _at(frequency), _at(b_off),
-            _at(b_ids), _at(b_val), b_len, b_len if bias_max is None else min(b_len, bias_max), _at(allowed), lda, n_masks, _at(mask_row),
-            _at(dev_status), raw)
-    _check("class_logits_adjust", rc)
+            s_len if seen_max is None or seen_max > s_len else seen_max, _at(n_prompt), _at(repetition), _at(presence), _at(frequency),
+            _at(b_off), _at(b_ids), _at(b_val), b_len, b_len if bias_max is None or bias_max > b_len else bias_max, _at(allowed), lda, n_masks,
+            _at(mask_row), _at(dev_status), raw)
+
+    _check("class_logits_adjust", _launch(dev, stream, call))
     return out

@@ -263,6 +263,12 @@ __device__ __forceinline__ void cl_store2(__amdgpu_buffer_rsrc_t to, uint32_t of
 __device__ __forceinline__ void cl_store2(__amdgpu_buffer_rsrc_t to, uint32_t off, float v0, float v1, const uint16_t *) {
     __builtin_amdgcn_raw_buffer_store_b32(ks_pack_bf2(v0, v1), to, off, 0, 2);
 }
+__device__ __forceinline__ void cl_store1(__amdgpu_buffer_rsrc_t to, uint32_t off, float v, const float *) {
+    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), to, off, 0, 0);
+}
+__device__ __forceinline__ void cl_store1(__amdgpu_buffer_rsrc_t to, uint32_t off, float v, const uint16_t *) {
+    __builtin_amdgcn_raw_buffer_store_b16((uint16_t)ks_f2bf(v), to, off, 0, 0);
+}
 // Logits of 32 samples from m0 on by the 64 classes from c0 on as a buffer that ends with the last sample's row: what lies behind its
 // end (samples that do not exist, and classes: CL_NO_CLASS) the hardware leaves out, so that every row is one store on every
 // way.  32 rows are less than 2^31 bytes (cl_logits sees to that).
@@ -273,8 +279,9 @@ template <typename OUT> __device__ __forceinline__ __amdgpu_buffer_rsrc_t cl_row
 #define CL_NO_CLASS 0x80000000u
 
 // Scales, bias, type and store of 32 S samples from m0 on by the 64 classes from c0 on.  A lane of the result holds one column of each of
-// the two blocks, which are two consecutive classes.  f: scales of the samples (LDS).  vec: pairs of classes are aligned.
-template <int S, typename OUT>
+// the two blocks, which are two consecutive classes.  f: scales of the samples (LDS).  vec: pairs of classes are aligned.  ODD: the last
+// of an odd number of classes, which has no pair, is stored here too (else by cl_last_class).
+template <int S, bool ODD, typename OUT>
 __device__ __forceinline__ void cl_finish(const cl_i32x16 (&acc)[S][2], const float *f, const float *__restrict__ ws,
                                           const float *__restrict__ bias, int64_t c0, int64_t C, int m0, int B, OUT *out, int64_t ldl, int vec) {
     const int lane = threadIdx.x & 63, half4 = 4 * (lane >> 5);
@@ -311,22 +318,54 @@ __device__ __forceinline__ void cl_finish(const cl_i32x16 (&acc)[S][2], const fl
             }
         }
     }
-    if (!vec || c0 + CL_GROUP > C) { // element by element: all of them, or the last of an odd number of classes
+    if (ODD && vec && (C & 1) && c0 + CL_GROUP > C) {
+        const uint32_t row_bytes = (uint32_t)(ldl * sizeof(OUT)), off0 = c + 1 == C ? half4 * row_bytes + 2 * (lane & 31) * (uint32_t)sizeof(OUT) : CL_NO_CLASS;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const __amdgpu_buffer_rsrc_t to = cl_rows_of(out, ldl, m0 + s * 32, c0, B);
+            uint32_t off = off0;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                cl_store1(to, off, value(s, r, 0, *(const float4 *)(f + half4 + s * 32 + r / 4 * 8)), (const OUT *)nullptr);
+                off += r % 4 < 3 ? row_bytes : 5 * row_bytes;
+                asm volatile("" : "+v"(off));
+            }
+        }
+    }
+    if (!vec) { // element by element
         int rows = B - m0 - half4;
         asm volatile("" : "+v"(rows), "+s"(ldl));
         OUT *p = out + (int64_t)(m0 + half4) * ldl + c;
-        if (!vec || (c == C - 1))
 #pragma unroll
-            for (int s = 0; s < S; ++s)
+        for (int s = 0; s < S; ++s)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float4 g = *(const float4 *)(f + half4 + s * 32 + r / 4 * 8);
-                    if (s * 32 + r / 4 * 8 + r % 4 < rows) {
-                        if (c < C) cl_store(p, value(s, r, 0, g));
-                        if (c + 1 < C && !vec) cl_store(p + 1, value(s, r, 1, g));
-                    }
-                    p += r % 4 < 3 ? ldl : 5 * ldl;
+            for (int r = 0; r < 16; ++r) {
+                const float4 g = *(const float4 *)(f + half4 + s * 32 + r / 4 * 8);
+                if (s * 32 + r / 4 * 8 + r % 4 < rows) {
+                    if (c < C) cl_store(p, value(s, r, 0, g));
+                    if (c + 1 < C) cl_store(p + 1, value(s, r, 1, g));
                 }
+                p += r % 4 < 3 ? ldl : 5 * ldl;
+            }
+    }
+}
+
+// The last of an odd number of classes, which has no pair to be stored with: the wavefronts of all workgroups take a sample each.
+template <typename OUT>
+__device__ __forceinline__ void cl_last_class(const int8_t *xq, const float *xs, const int8_t *wq, const float *ws, const float *bias,
+                                              int64_t C, int kb, int B, float scale, OUT *out, int64_t ldl) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int64_t wb = (C - 1) / CL_GROUP * 2; // C is odd: slot (C - 1) % 64 / 2 of the group's first block
+    for (int m = blockIdx.x * waves + wave; m < B; m += gridDim.x * waves) {
+        int sum = 0;
+        for (int u = lane; u < 2 * kb; u += 64) { // half-pieces
+            const cl_i32x4 xv = *(const cl_i32x4 *)(xq + ((int64_t)(m / 32) * kb + u / 2) * CL_PIECE + ((u & 1) * 32 + m % 32) * 16);
+            const cl_i32x4 wv = *(const cl_i32x4 *)(wq + (wb * kb + u / 2) * CL_PIECE + ((u & 1) * 32 + (int)((C - 1) % CL_GROUP / 2)) * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_sdot4(xv[e], wv[e], sum, false);
+        }
+        sum = ks_wave_sum_i(sum);
+        if (lane == 0) cl_store(out + (int64_t)m * ldl + C - 1, fmaf((float)sum * (scale * xs[m]), ws[C - 1], bias ? bias[C - 1] : 0.f));
     }
 }
 
@@ -389,7 +428,7 @@ cl_direct_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
 #pragma unroll
                     for (int r = 0; r < 16; ++r) acc[s][q][r] += s_sum[(o * S * 32 + s * 32 + q * 16 + r) * 64 + lane];
     }
-    cl_finish<S>(acc, s_f, ws, bias, grp * CL_GROUP, C, sb * 32, B, out, ldl, vec);
+    cl_finish<S, true>(acc, s_f, ws, bias, grp * CL_GROUP, C, sb * 32, B, out, ldl, vec);
 }
 
 // The work of a workgroup: stretches of an XCD's class groups for one sample tile each.  Workgroup i runs on XCD i % 8, and the groups are
@@ -501,10 +540,11 @@ cl_resident_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, 
                     }
                 }
             }
-            cl_finish<4>(acc, s_f, ws, bias, (int64_t)(g_lo + grp) * CL_GROUP, C, sb * 128, B, out, ldl, vec);
+            cl_finish<4, false>(acc, s_f, ws, bias, (int64_t)(g_lo + grp) * CL_GROUP, C, sb * 128, B, out, ldl, vec);
             grp = next;
         }
     }
+    if (vec && (C & 1)) cl_last_class(xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl);
 }
 
 // Rows of up to 32 KB elements: a wavefront keeps the codes of 64 classes in registers, a workgroup those of up to 256 samples in LDS, and
@@ -631,20 +671,7 @@ cl_steady_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
 #pragma unroll
         for (int r = 0; r < 16; ++r) finish(acc[1], r, s_f + (tile - 1) * 32 + half4);
     }
-    // the last of an odd number of classes has no pair to be stored with: a wavefront per sample
-    if (C & 1)
-        for (int m = blockIdx.x * NW + wave; m < B; m += gridDim.x * NW) {
-            const int64_t wb = (C - 1) / CL_GROUP * 2; // C is odd: slot (C - 1) % 64 / 2 of the group's first block
-            int sum = 0;
-            if (lane < 2 * kb) {
-                const cl_i32x4 xv = *(const cl_i32x4 *)(xq + ((int64_t)(m / 32) * kb + lane / 2) * CL_PIECE + ((lane & 1) * 32 + m % 32) * 16);
-                const cl_i32x4 wv = *(const cl_i32x4 *)(wq + (wb * kb + lane / 2) * CL_PIECE + ((lane & 1) * 32 + (int)((C - 1) % CL_GROUP / 2)) * 16);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_sdot4(xv[e], wv[e], sum, false);
-            }
-            sum = ks_wave_sum_i(sum);
-            if (lane == 0) cl_store(out + (int64_t)m * ldl + C - 1, fmaf((float)sum * (scale * xs[m]), ws[C - 1], bias ? bias[C - 1] : 0.f));
-        }
+    if (C & 1) cl_last_class(xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl);
 }
 
 // Deeper rows: as in cl_resident_kernel, but the samples pass through LDS in chunks of eight k-steps, which eight wavefronts with 64
@@ -670,7 +697,6 @@ cl_staged_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
     const int xcd = blockIdx.x & 7, per_xcd = gridDim.x >> 3, j = blockIdx.x >> 3;
     const int c_lo = (int)((int64_t)n_ct * xcd / 8), c_n = (int)((int64_t)n_ct * (xcd + 1) / 8) - c_lo;
     int64_t left = (int64_t)c_n * n_sb - j; // tiles from this one on, of this and the XCD's other workgroups
-    if (left <= 0) return;
     const int step_c = per_xcd / n_sb, step_s = per_xcd % n_sb; // from one of this workgroup's tiles to its next
     int ct = c_lo + j / n_sb, sb = j % n_sb;
 
@@ -769,10 +795,11 @@ cl_staged_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
         }
         for (int i = lane; i < 128; i += 64) s_f[wave][i] = sb * 128 + i < B ? scale * xs[sb * 128 + i] : 0.f;
         const int g = ct * NW + wave;
-        if (g < groups) cl_finish<4>(acc, s_f[wave], ws, bias, (int64_t)g * CL_GROUP, C, sb * 128, B, out, ldl, vec);
+        if (g < groups) cl_finish<4, false>(acc, s_f[wave], ws, bias, (int64_t)g * CL_GROUP, C, sb * 128, B, out, ldl, vec);
         ct = next_ct;
         sb = next_sb;
     }
+    if (vec && (C & 1)) cl_last_class(xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl);
 }
 
 template <typename OUT>
@@ -786,12 +813,12 @@ static void cl_logits(const int8_t *xq, const float *xs, const int8_t *wq, const
     };
     // Few samples: the codes of the weights are what moves, and every wavefront reads its own.  Few wavefronts in all (a kernel of
     // 256 workgroups that keep the samples would leave most idle: 10,000 x 512, batch 256: 5.9 us, 8.0 in 128-sample tiles; 50,000
-    // x 512, 128: 11.3 and 9.3): the same for any batch.  Where they are deep, four wavefronts divide each group's depth (10,000 x
+    // x 512, 128: 11.3 and 9.3; x 256: 6.8 and 8.4): the same for any batch.  Where they are deep, four wavefronts divide each group's depth (10,000 x
     // 4,096, one sample: 39 us, 13; 64: 44, 16; 50,000 x 2,048, one: 25, 20; but 64 samples, whose sums take 320 registers, only
     // where a compute unit would have a wavefront or so: 50,000 x 768: 12 us, 21).
     const int64_t waves = groups * ks_ceil_div(B, 64);
     if (B <= 32) return waves <= 1024 && kb >= 24 ? direct(cl_direct_kernel<1, 4, OUT>, 32, 1) : direct(cl_direct_kernel<1, 1, OUT>, 32, 4);
-    if (B <= 64 || waves <= 1280 || (kb < 4 && !vec))
+    if (B <= 64 || waves <= 1280 || (waves <= 2048 && kb <= 8) || (kb < 4 && !vec))
         return waves <= 320 && kb >= 24 ? direct(cl_direct_kernel<2, 4, OUT>, 64, 1) : direct(cl_direct_kernel<2, 1, OUT>, 64, 4);
     // Registers hold 64 classes' codes while samples stream, or LDS holds samples while codes stream: the former is ahead for thin
     // rows (390,625 x 64, batch 1,024: 162 us, 176) and for large products (x 512: 214, 229; 1,024 x 120,000 x 512: 75, 71), if
@@ -892,9 +919,10 @@ __device__ __forceinline__ bool cl_masked(const ClAdjust &a, int m, int64_t c) {
     return m >= 0 && !(a.allowed[(int64_t)m * a.ld_allowed + (c >> 5)] >> (c & 31) & 1);
 }
 
-// masks, and where COPY the logits that stay as they are; a workgroup takes a stretch of one row
-#define CLM_U 4
-template <typename T, bool COPY, bool VEC, int NT>
+// Masks, and where COPY the logits that stay as they are; a workgroup takes a stretch of one row.  In place a vector of which some are
+// masked is stored element by element, or with RMW read, changed and stored (then no other launch may change it meanwhile).
+#define CLM_U(copy) ((copy) ? 2 : 4) /* vectors of a thread; copies of 256 x 390,625 fp32: 136 us, 157 with four; masks in place of bf16: 51, 47 */
+template <typename T, bool COPY, bool VEC, bool RMW, int NT>
 __device__ __forceinline__ void cl_mask_part(const ClAdjust &a, int b, int part) {
     constexpr int E = VEC ? 16 / (int)sizeof(T) : 1;
     const int m = cl_mask_of(a, b);
@@ -903,9 +931,9 @@ __device__ __forceinline__ void cl_mask_part(const ClAdjust &a, int b, int part)
     const T *in = (const T *)a.in + b * a.ldl;
     T *out = (T *)a.out + b * a.ldo;
     const T none = cl_minus_inf<T>();
-    const int64_t first = ((int64_t)part * CLM_U * NT + threadIdx.x) * E;
+    const int64_t first = ((int64_t)part * CLM_U(COPY) * NT + threadIdx.x) * E;
 #pragma unroll
-    for (int u = 0; u < CLM_U; ++u) {
+    for (int u = 0; u < CLM_U(COPY); ++u) {
         const int64_t c = first + (int64_t)u * NT * E;
         if (c >= a.C) break;
         const uint32_t w = bits ? bits[c >> 5] >> (c & 31) : ~0u;
@@ -915,10 +943,16 @@ __device__ __forceinline__ void cl_mask_part(const ClAdjust &a, int b, int part)
                 v.q = *(const uint4 *)(in + c);
 #pragma unroll
                 for (int e = 0; e < E; ++e) v.e[e] = w >> e & 1 ? v.e[e] : none;
-                *(uint4 *)(out + c) = v.q;
+                __builtin_nontemporal_store(__builtin_bit_cast(cl_i32x4, v.q), (cl_i32x4 *)(out + c)); // 256 x 390,625 bf16: 58 us, 85 without
             } else if ((w & ((1u << E) - 1)) == 0) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) v.e[e] = none;
+                *(uint4 *)(out + c) = v.q;
+            } else if (RMW) {
+                if ((~w & ((1u << E) - 1)) == 0) continue;
+                v.q = *(const uint4 *)(out + c);
+#pragma unroll
+                for (int e = 0; e < E; ++e) v.e[e] = w >> e & 1 ? v.e[e] : none;
                 *(uint4 *)(out + c) = v.q;
             } else {
 #pragma unroll
@@ -934,9 +968,9 @@ __device__ __forceinline__ void cl_mask_part(const ClAdjust &a, int b, int part)
     }
 }
 
-template <typename T, bool COPY, bool VEC>
+template <typename T, bool COPY, bool VEC, bool RMW>
 __global__ void __launch_bounds__(CL_NT) cl_mask_kernel(ClAdjust a, int per_row) {
-    cl_mask_part<T, COPY, VEC, CL_NT>(a, a.row0 + blockIdx.x / per_row, blockIdx.x % per_row);
+    cl_mask_part<T, COPY, VEC, RMW, CL_NT>(a, a.row0 + blockIdx.x / per_row, blockIdx.x % per_row);
 }
 
 // Lists of a request that a hash table of SLOTS classes in LDS holds (three quarters of the slots): each of them counts the class's occurrences
@@ -952,7 +986,7 @@ __global__ void __launch_bounds__(NT) cl_hash_kernel(ClAdjust a, int requests, i
     __shared__ int s_bias[SLOTS];
     if (MASKS && (int)blockIdx.x >= requests) {
         const int i = blockIdx.x - requests;
-        cl_mask_part<T, false, MASKS == 2, NT>(a, a.row0 + i / per_row, i % per_row);
+        cl_mask_part<T, false, MASKS == 2, false, NT>(a, a.row0 + i / per_row, i % per_row);
         return;
     }
     const int b = a.row0 + blockIdx.x;
@@ -1004,39 +1038,71 @@ __global__ void __launch_bounds__(NT) cl_hash_kernel(ClAdjust a, int requests, i
         if (slot[i] >= 0) cl_store(out + s_key[slot[i]] - 1, cl_adjusted(a, b, z[i], s_seen[slot[i]], s_bias[slot[i]], bf));
 }
 
-// Longer lists: a workgroup has a count and a bias entry for each of CLR classes and takes the request's entries among them.
-#define CLR 8192
+// Longer lists: `parts` workgroups to a request, each with the classes whose keys, spread by an odd factor over the 32-bit numbers, lie in its
+// part of them; all of them go over the whole list.  A part whose table is so full that an entry finds no slot within CLL_TRIES
+// is done in several rounds, over half of the part, a quarter, and so on (different classes have different keys: that ends).
+#define CLL_SLOTS 6144
+#define CLL_TRIES 256
 template <typename T>
-__global__ void __launch_bounds__(1024) cl_range_kernel(ClAdjust a, int ranges) {
-    __shared__ uint32_t s_seen[CLR];
-    __shared__ int s_bias[CLR];
-    const int b = a.row0 + blockIdx.x / ranges;
-    const int64_t r0 = (int64_t)(blockIdx.x % ranges) * CLR;
+__global__ void __launch_bounds__(1024) cl_long_kernel(ClAdjust a, int parts) {
+    __shared__ uint32_t s_key[CLL_SLOTS], s_seen[CLL_SLOTS]; // column + 1, 0: free
+    __shared__ int s_bias[CLL_SLOTS];
+    __shared__ int s_full;
+    const int b = a.row0 + blockIdx.x / parts, part = blockIdx.x % parts;
     int64_t sf = 0, bf = 0;
     const int ns = cl_list(a.seen_offsets, a.seen_len, a.seen_max, b, &sf, a.dev_status);
     const int nb = cl_list(a.bias_offsets, a.bias_len, a.bias_max, b, &bf, a.dev_status);
     const int m = cl_mask_of(a, b);
     if (ns + nb == 0) return;
     const int prompt = a.n_prompt ? a.n_prompt[b] : 0;
-    for (int e = threadIdx.x; e < CLR; e += 1024) { s_seen[e] = 0; s_bias[e] = -1; }
-    __syncthreads();
-    for (int e = threadIdx.x; e < ns; e += 1024) {
-        const int64_t c = cl_column(a, a.seen_ids[sf + e], KS_DEV_BAD_LABEL) - r0;
-        if (c < 0 || c >= CLR) continue;
-        if (e < prompt) atomicOr(&s_seen[c], 1u);
-        else atomicAdd(&s_seen[c], 2u);
-    }
-    for (int e = threadIdx.x; e < nb; e += 1024) {
-        const int64_t c = cl_column(a, a.bias_ids[bf + e], KS_DEV_BAD_INDEX) - r0;
-        if (c >= 0 && c < CLR) atomicMax(&s_bias[c], e);
-    }
-    __syncthreads();
-    for (int e = threadIdx.x; e < CLR; e += 1024) {
-        const uint32_t seen = s_seen[e];
-        const int j = s_bias[e];
-        const int64_t c = r0 + e;
-        if ((!seen && j < 0) || cl_masked(a, m, c)) continue;
-        cl_store((T *)a.out + b * a.ldo + c, cl_adjusted(a, b, cl_load((const T *)a.in + b * a.ldl + c), seen, j, bf));
+    const T *in = (const T *)a.in + b * a.ldl;
+    T *out = (T *)a.out + b * a.ldo;
+    const uint64_t end = ((uint64_t)(part + 1) << 32) / parts;
+    uint64_t lo = ((uint64_t)part << 32) / parts, width = end - lo;
+    while (lo < end) { // spread keys [lo, lo + width)
+        if (lo + width > end) width = end - lo;
+        __syncthreads();
+        for (int e = threadIdx.x; e < CLL_SLOTS; e += 1024) { s_key[e] = 0; s_seen[e] = 0; s_bias[e] = -1; }
+        if (threadIdx.x == 0) s_full = 0;
+        __syncthreads();
+        for (int e0 = threadIdx.x; e0 < ns + nb; e0 += 8 * 1024) {
+            int32_t id[8]; // eight loads at a time
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int e = e0 + i * 1024;
+                id[i] = e < ns ? a.seen_ids[sf + e] : e < ns + nb ? a.bias_ids[bf + e - ns] : -1;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int e = e0 + i * 1024;
+                const int64_t c = cl_column(a, id[i], e < ns ? KS_DEV_BAD_LABEL : KS_DEV_BAD_INDEX);
+                const uint32_t key = (uint32_t)c + 1, spread = key * 0x9E3779B1u;
+                if (c < 0 || (uint64_t)spread - lo >= width) continue;
+                uint32_t at = __umulhi(spread * 0x85EBCA6Bu, CLL_SLOTS);
+                int tries = 0;
+                for (; tries < CLL_TRIES; ++tries) {
+                    const uint32_t was = atomicCAS(&s_key[at], 0u, key);
+                    if (was == 0 || was == key) break;
+                    at = at + 1 == CLL_SLOTS ? 0 : at + 1;
+                }
+                if (tries == CLL_TRIES) s_full = 1;
+                else if (e >= ns) atomicMax(&s_bias[at], e - ns);
+                else if (e < prompt) atomicOr(&s_seen[at], 1u);
+                else atomicAdd(&s_seen[at], 2u);
+            }
+        }
+        __syncthreads();
+        if (s_full) {
+            width = (width + 1) / 2;
+            continue;
+        }
+#pragma unroll
+        for (int i = 0; i < CLL_SLOTS / 1024; ++i) {
+            const int e = i * 1024 + threadIdx.x;
+            const uint32_t key = s_key[e];
+            if (key && !cl_masked(a, m, (int64_t)key - 1)) cl_store(out + key - 1, cl_adjusted(a, b, cl_load(in + key - 1), s_seen[e], s_bias[e], bf));
+        }
+        lo += width;
     }
 }
 
@@ -1051,31 +1117,36 @@ template <typename T> static void cl_adjust(const ClAdjust &args, hipStream_t st
     const bool copy = args.in != args.out;
     const bool vec = ((uintptr_t)args.in | (uintptr_t)args.out | (uintptr_t)(args.ldl * sizeof(T)) | (uintptr_t)(args.ldo * sizeof(T))) % 16 == 0;
     const int entries = (args.seen_offsets ? args.seen_max : 0) + (args.bias_offsets ? args.bias_max : 0), E = vec ? 16 / (int)sizeof(T) : 1;
-    const bool fused = !copy && args.allowed && entries > 0 && entries <= 3072;
+    // masks in place: together with short lists (16 x 390,625 bf16, 1,088 entries: 7.9 us, 14.2 in two launches); but from 32 MB of
+    // bf16 on by themselves, reading what they change in part: a bf16 vector has eight elements, stored one by one, and reading
+    // it costs less than they do (256 x 390,625, half of the classes: 49 us, 82; fp32, four elements: 112, 90)
+    const bool rmw = !copy && vec && sizeof(T) == 2 && (int64_t)args.B * args.C >= 1 << 24;
+    const bool fused = !copy && args.allowed && !rmw && entries > 0 && entries <= 3072;
     if ((copy || args.allowed) && !fused) {
-        const int per_row = (int)ks_ceil_div(args.C, (int64_t)CLM_U * CL_NT * E);
+        const int per_row = (int)ks_ceil_div(args.C, (int64_t)CLM_U(copy) * CL_NT * E);
         cl_rows(args, per_row, [&](const ClAdjust &a, int rows) {
             const dim3 grid((unsigned)per_row * (unsigned)rows);
-            if (copy && vec) hipLaunchKernelGGL((cl_mask_kernel<T, true, true>), grid, dim3(CL_NT), 0, st, a, per_row);
-            else if (copy) hipLaunchKernelGGL((cl_mask_kernel<T, true, false>), grid, dim3(CL_NT), 0, st, a, per_row);
-            else if (vec) hipLaunchKernelGGL((cl_mask_kernel<T, false, true>), grid, dim3(CL_NT), 0, st, a, per_row);
-            else hipLaunchKernelGGL((cl_mask_kernel<T, false, false>), grid, dim3(CL_NT), 0, st, a, per_row);
+            if (copy && vec) hipLaunchKernelGGL((cl_mask_kernel<T, true, true, false>), grid, dim3(CL_NT), 0, st, a, per_row);
+            else if (copy) hipLaunchKernelGGL((cl_mask_kernel<T, true, false, false>), grid, dim3(CL_NT), 0, st, a, per_row);
+            else if (sizeof(T) == 2 && rmw) hipLaunchKernelGGL((cl_mask_kernel<T, false, true, sizeof(T) == 2>), grid, dim3(CL_NT), 0, st, a, per_row);
+            else if (vec) hipLaunchKernelGGL((cl_mask_kernel<T, false, true, false>), grid, dim3(CL_NT), 0, st, a, per_row);
+            else hipLaunchKernelGGL((cl_mask_kernel<T, false, false, false>), grid, dim3(CL_NT), 0, st, a, per_row);
         });
     }
     if (entries == 0) return;
     const auto hash = [&](auto alone, auto with_elements, auto with_vectors, int nt) {
-        const int per_row = fused ? (int)ks_ceil_div(args.C, (int64_t)CLM_U * nt * E) : 0;
+        const int per_row = fused ? (int)ks_ceil_div(args.C, (int64_t)CLM_U(false) * nt * E) : 0;
         cl_rows(args, 1 + per_row, [&](const ClAdjust &a, int rows) {
             hipLaunchKernelGGL(!fused ? alone : vec ? with_vectors : with_elements, dim3((unsigned)rows * (unsigned)(1 + per_row)), dim3(nt), 0, st, a, rows, per_row);
         });
     };
     if (entries <= 768) hash(cl_hash_kernel<T, 1024, 256, 0>, cl_hash_kernel<T, 1024, 256, 1>, cl_hash_kernel<T, 1024, 256, 2>, 256);
-    else if (entries <= 3072) hash(cl_hash_kernel<T, 4096, 512, 0>, cl_hash_kernel<T, 4096, 512, 1>, cl_hash_kernel<T, 4096, 512, 2>, 512);
-    else if (entries <= 9216) hash(cl_hash_kernel<T, 12288, 1024, 0>, cl_hash_kernel<T, 12288, 1024, 0>, cl_hash_kernel<T, 12288, 1024, 0>, 1024);
+    else if (entries <= 3072) hash(cl_hash_kernel<T, 4096, 1024, 0>, cl_hash_kernel<T, 4096, 1024, 1>, cl_hash_kernel<T, 4096, 1024, 2>, 1024);
     else {
-        const int ranges = (int)ks_ceil_div(args.C, CLR);
-        cl_rows(args, ranges, [&](const ClAdjust &a, int rows) {
-            hipLaunchKernelGGL(cl_range_kernel<T>, dim3((unsigned)ranges * (unsigned)rows), dim3(1024), 0, st, a, ranges);
+        // parts of 4,096 entries on average, more where there are few requests: two workgroups fit on a compute unit
+        const int fill = (int)ks_ceil_div(512, args.B) < 16 ? (int)ks_ceil_div(512, args.B) : 16, need = (int)ks_ceil_div(entries, 4096), parts = need > fill ? need : fill;
+        cl_rows(args, parts, [&](const ClAdjust &a, int rows) {
+            hipLaunchKernelGGL(cl_long_kernel<T>, dim3((unsigned)parts * (unsigned)rows), dim3(1024), 0, st, a, parts);
         });
     }
 }

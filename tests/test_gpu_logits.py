@@ -329,7 +329,8 @@ def check_adjust(ks, r, B, C, c0, Cg, a, dtype, in_place, ld, shift=0, extreme=T
 @pytest.mark.parametrize("B,C,nodes,seen,biases,masks,ld", [
     (1, 1, 1, 1, 1, True, 1), (1, 10_000, 1, 300, 20, True, 10_000), (5, 1_000, 1, 40, 0, False, 1_000), (4, 999, 3, 0, 30, True, 1_003),
     (3, 8_193, 2, 500, 3, False, 8_200), (7, 4_133, 1, 0, 0, True, 4_136), (9, 20_001, 4, 3_000, 700, True, 20_001), (2, 100, 1, 9_000, 0, True, 104),
-    (3, 40_000, 1, 20_000, 100, True, 40_064), (33, 555, 1, 60, 60, True, 560)])
+    (3, 40_000, 1, 20_000, 100, True, 40_064), (33, 555, 1, 60, 60, True, 560), (70, 250_001, 1, 100, 20, True, 250_008),
+    (2, 70_000, 1, 50_000, 5_000, True, 70_001)])
 def test_adjust(ks, B, C, nodes, seen, biases, masks, ld, in_place, dtype):
     r = rng_of(B, C, seen, biases)
     Cg, c0 = C * nodes, C * (nodes // 2)
@@ -372,6 +373,20 @@ def test_adjust_ids_that_share_their_low_bits(ks):
         ids = (np.arange(n, dtype=np.int64) * step).astype(np.int32)
         a = {"seen": (ids, np.array([0, n], dtype=np.int64)), "presence": np.array([2.0], dtype=np.float32)}
         check_adjust(ks, rng_of(step), 1, C, 0, C, a, torch.float32, True, C)
+
+
+@pytest.mark.parametrize("B,n,twice", [(1, 9_000, False), (40, 5_000, True)])
+def test_adjust_classes_that_fall_into_one_part(ks, B, n, twice):
+    """Lists of which all classes are neighbours once their keys are spread (by the odd factor that divides long lists among
+    workgroups): one workgroup gets them all, several times what its table takes."""
+    C = 1 << 20
+    keys = (np.arange(1, C + 1, dtype=np.uint64) * 0x9E3779B1 % 2 ** 32).argsort()[:n].astype(np.int32)
+    ids = np.concatenate([keys, keys[::-1]]) if twice else keys
+    off = np.zeros(B + 1, dtype=np.int64)
+    off[1:] = len(ids)  # the first request's list; the others have none
+    a = {"seen": (ids, off), "presence": np.full(B, 2.0, dtype=np.float32), "frequency": np.full(B, 0.5, dtype=np.float32),
+         "repetition": np.full(B, 1.5, dtype=np.float32)}
+    check_adjust(ks, rng_of(B, n), B, C, 0, C, a, torch.bfloat16, True, C)
 
 
 def test_adjust_reports_what_it_cannot_use(ks):
