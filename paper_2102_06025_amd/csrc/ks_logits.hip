@@ -973,15 +973,19 @@ __global__ void __launch_bounds__(CL_NT) cl_mask_kernel(ClAdjust a, int per_row)
     cl_mask_part<T, COPY, VEC, RMW, CL_NT>(a, a.row0 + blockIdx.x / per_row, blockIdx.x % per_row);
 }
 
-// Lists of a request that a hash table of SLOTS classes in LDS holds (three quarters of the slots): each of them counts the class's occurrences
+// Lists of a request that a hash table of SLOTS classes in LDS holds (two thirds of the slots): each of them counts the class's occurrences
 // and keeps the last of its biases.  The entry that takes a slot fetches the logit at once, so that it arrives while the others
 // are counted, and adjusts it afterwards; nothing is read or written but the lists and the logits of their classes.
 // MASKS > 0: the workgroups behind the requests' carry out the masks in place (1: element by element, 2: vectors): no logit
 // belongs to both, so that one launch does for both.
+#define CLH_ENTRIES(slots) ((slots) / 3 * 2)
+#define CLH_SMALL 1536
+#define CLH_MID 6144
+#define CLH_LARGE 12288 /* 144 KB of LDS, one workgroup on a compute unit */
 template <typename T, int SLOTS, int NT, int MASKS>
 __global__ void __launch_bounds__(NT) cl_hash_kernel(ClAdjust a, int requests, int per_row) {
-    constexpr int K = SLOTS / 4 * 3 / NT; // entries of a thread
-    static_assert(K * NT == SLOTS / 4 * 3, "");
+    constexpr int K = CLH_ENTRIES(SLOTS) / NT; // entries of a thread
+    static_assert(K * NT == CLH_ENTRIES(SLOTS), "");
     __shared__ uint32_t s_key[SLOTS], s_seen[SLOTS]; // column + 1, 0: free
     __shared__ int s_bias[SLOTS];
     if (MASKS && (int)blockIdx.x >= requests) {
@@ -1040,7 +1044,9 @@ __global__ void __launch_bounds__(NT) cl_hash_kernel(ClAdjust a, int requests, i
 
 // Longer lists: `parts` workgroups to a request, each with the classes whose keys, spread by an odd factor over the 32-bit numbers, lie in its
 // part of them; all of them go over the whole list.  A part whose table is so full that an entry finds no slot within CLL_TRIES
-// is done in several rounds, over half of the part, a quarter, and so on (different classes have different keys: that ends).
+// is done in several rounds, over half of the part, a quarter, and so on (different classes have different keys: that ends), and
+// twice as much of it after each that held.  Its time goes into the lists, read again for every part: 256 x 131,072 bf16 with 20,000
+// entries a request 138 us, one such request 22.
 #define CLL_SLOTS 6144
 #define CLL_TRIES 256
 template <typename T>
@@ -1065,15 +1071,15 @@ __global__ void __launch_bounds__(1024) cl_long_kernel(ClAdjust a, int parts) {
         for (int e = threadIdx.x; e < CLL_SLOTS; e += 1024) { s_key[e] = 0; s_seen[e] = 0; s_bias[e] = -1; }
         if (threadIdx.x == 0) s_full = 0;
         __syncthreads();
-        for (int e0 = threadIdx.x; e0 < ns + nb; e0 += 8 * 1024) {
-            int32_t id[8]; // eight loads at a time
+        for (int e0 = threadIdx.x; e0 < ns + nb; e0 += 4 * 1024) {
+            int32_t id[4]; // four loads at a time
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < 4; ++i) {
                 const int e = e0 + i * 1024;
                 id[i] = e < ns ? a.seen_ids[sf + e] : e < ns + nb ? a.bias_ids[bf + e - ns] : -1;
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < 4; ++i) {
                 const int e = e0 + i * 1024;
                 const int64_t c = cl_column(a, id[i], e < ns ? KS_DEV_BAD_LABEL : KS_DEV_BAD_INDEX);
                 const uint32_t key = (uint32_t)c + 1, spread = key * 0x9E3779B1u;
@@ -1081,7 +1087,8 @@ __global__ void __launch_bounds__(1024) cl_long_kernel(ClAdjust a, int parts) {
                 uint32_t at = __umulhi(spread * 0x85EBCA6Bu, CLL_SLOTS);
                 int tries = 0;
                 for (; tries < CLL_TRIES; ++tries) {
-                    const uint32_t was = atomicCAS(&s_key[at], 0u, key);
+                    uint32_t was = *(volatile uint32_t *)&s_key[at]; // a read is shared by the lanes of one class, an atomic is not
+                    if (was == 0) was = atomicCAS(&s_key[at], 0u, key);
                     if (was == 0 || was == key) break;
                     at = at + 1 == CLL_SLOTS ? 0 : at + 1;
                 }
@@ -1096,13 +1103,20 @@ __global__ void __launch_bounds__(1024) cl_long_kernel(ClAdjust a, int parts) {
             width = (width + 1) / 2;
             continue;
         }
+        constexpr int N = CLL_SLOTS / 1024;
+        uint32_t key[N];
+        float z[N];
 #pragma unroll
-        for (int i = 0; i < CLL_SLOTS / 1024; ++i) {
-            const int e = i * 1024 + threadIdx.x;
-            const uint32_t key = s_key[e];
-            if (key && !cl_masked(a, m, (int64_t)key - 1)) cl_store(out + key - 1, cl_adjusted(a, b, cl_load(in + key - 1), s_seen[e], s_bias[e], bf));
+        for (int i = 0; i < N; ++i) { // all of them are fetched before the first one is stored
+            key[i] = s_key[i * 1024 + threadIdx.x];
+            if (key[i] && cl_masked(a, m, (int64_t)key[i] - 1)) key[i] = 0;
+            if (key[i]) z[i] = cl_load(in + key[i] - 1);
         }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (key[i]) cl_store(out + key[i] - 1, cl_adjusted(a, b, z[i], s_seen[i * 1024 + threadIdx.x], s_bias[i * 1024 + threadIdx.x], bf));
         lo += width;
+        width *= 2;
     }
 }
 
@@ -1121,7 +1135,7 @@ template <typename T> static void cl_adjust(const ClAdjust &args, hipStream_t st
     // bf16 on by themselves, reading what they change in part: a bf16 vector has eight elements, stored one by one, and reading
     // it costs less than they do (256 x 390,625, half of the classes: 49 us, 82; fp32, four elements: 112, 90)
     const bool rmw = !copy && vec && sizeof(T) == 2 && (int64_t)args.B * args.C >= 1 << 24;
-    const bool fused = !copy && args.allowed && !rmw && entries > 0 && entries <= 3072;
+    const bool fused = !copy && args.allowed && !rmw && entries > 0 && entries <= CLH_ENTRIES(CLH_MID);
     if ((copy || args.allowed) && !fused) {
         const int per_row = (int)ks_ceil_div(args.C, (int64_t)CLM_U(copy) * CL_NT * E);
         cl_rows(args, per_row, [&](const ClAdjust &a, int rows) {
@@ -1140,11 +1154,18 @@ template <typename T> static void cl_adjust(const ClAdjust &args, hipStream_t st
             hipLaunchKernelGGL(!fused ? alone : vec ? with_vectors : with_elements, dim3((unsigned)rows * (unsigned)(1 + per_row)), dim3(nt), 0, st, a, rows, per_row);
         });
     };
-    if (entries <= 768) hash(cl_hash_kernel<T, 1024, 256, 0>, cl_hash_kernel<T, 1024, 256, 1>, cl_hash_kernel<T, 1024, 256, 2>, 256);
-    else if (entries <= 3072) hash(cl_hash_kernel<T, 4096, 1024, 0>, cl_hash_kernel<T, 4096, 1024, 1>, cl_hash_kernel<T, 4096, 1024, 2>, 1024);
-    else {
-        // parts of 4,096 entries on average, more where there are few requests: two workgroups fit on a compute unit
-        const int fill = (int)ks_ceil_div(512, args.B) < 16 ? (int)ks_ceil_div(512, args.B) : 16, need = (int)ks_ceil_div(entries, 4096), parts = need > fill ? need : fill;
+    if (entries <= CLH_ENTRIES(CLH_SMALL))
+        hash(cl_hash_kernel<T, CLH_SMALL, 256, 0>, cl_hash_kernel<T, CLH_SMALL, 256, 1>, cl_hash_kernel<T, CLH_SMALL, 256, 2>, 256);
+    else if (entries <= CLH_ENTRIES(CLH_MID))
+        hash(cl_hash_kernel<T, CLH_MID, 1024, 0>, cl_hash_kernel<T, CLH_MID, 1024, 1>, cl_hash_kernel<T, CLH_MID, 1024, 2>, 1024);
+    else if (entries <= CLH_ENTRIES(CLH_LARGE) && args.B >= 16) { // few requests leave most of the chip idle with one workgroup each
+        // (131,072 classes, bf16, lists of 8,000: 16 requests 24 us, 26 in parts; 128: 33, 37; 256 of 6,000: 13, 29; one of 9,000: 30, 15)
+        const auto kernel = cl_hash_kernel<T, CLH_LARGE, 1024, 0>;
+        hash(kernel, kernel, kernel, 1024); // the masks are set already
+    } else {
+        // parts of 4,096 entries on average (of 2,048: 256 lists of 20,000 202 us, 137), more where there are few requests: two
+        // workgroups fit on a compute unit, and one list of 20,000 takes 26 us in 16 parts, 22 in 64
+        const int fill = (int)ks_ceil_div(512, args.B) < 64 ? (int)ks_ceil_div(512, args.B) : 64, need = (int)ks_ceil_div(entries, 4096), parts = need > fill ? need : fill;
         cl_rows(args, parts, [&](const ClAdjust &a, int rows) {
             hipLaunchKernelGGL(cl_long_kernel<T>, dim3((unsigned)parts * (unsigned)rows), dim3(1024), 0, st, a, parts);
         });
