@@ -62,12 +62,21 @@ __device__ __forceinline__ int cl_code(float v, double inv, double a) {
     return k;
 }
 // Reductions of N = 1 or 4 values a lane over the wavefront at once.  Of four, every lane passes two on to its neighbour and keeps two, then
-// one and one; lanes of equal number modulo 4 then hold the same value's parts, and go on as in ks_wave_sum: 7 steps for four values
-// instead of 24.  Value i ends up in lane 63, or in lane 60 + i / 2 + i % 2 * 2.
+// one and one; lanes of equal number modulo 4 then hold the same value's parts, and go on four and eight lanes apart, and from row
+// to row by exchange (row_bcast, as in ks_wave_sum, would hand on lane 15's value only): 7 steps for four values instead of 24.
+// Value i ends up in lane 63, or in lane 60 + i / 2 + i % 2 * 2.
 struct ClMaxI {
     typedef int T;
     static __device__ __forceinline__ int op(int a, int b) { return max(a, b); }
     template <int CTRL, int ROWS> static __device__ __forceinline__ int move(int v) { return KS_DPP(0, v, CTRL, ROWS); }
+    static __device__ __forceinline__ int with_row(int v) { // op of the two rows of 16 of a half, in both
+        const auto s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return op((int)s[0], (int)s[1]);
+    }
+    static __device__ __forceinline__ int with_half(int v) { // op of the two halves, in both
+        const auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return op((int)s[0], (int)s[1]);
+    }
     static __device__ __forceinline__ int lane(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
 };
 struct ClSumD {
@@ -75,6 +84,16 @@ struct ClSumD {
     static __device__ __forceinline__ double op(double a, double b) { return a + b; }
     template <int CTRL, int ROWS> static __device__ __forceinline__ double move(double v) {
         return __hiloint2double(KS_DPP(0, __double2hiint(v), CTRL, ROWS), KS_DPP(0, __double2loint(v), CTRL, ROWS));
+    }
+    static __device__ __forceinline__ double with_row(double v) {
+        const auto lo = __builtin_amdgcn_permlane16_swap(__double2loint(v), __double2loint(v), false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap(__double2hiint(v), __double2hiint(v), false, false);
+        return op(__hiloint2double((int)hi[0], (int)lo[0]), __hiloint2double((int)hi[1], (int)lo[1]));
+    }
+    static __device__ __forceinline__ double with_half(double v) {
+        const auto lo = __builtin_amdgcn_permlane32_swap(__double2loint(v), __double2loint(v), false, false);
+        const auto hi = __builtin_amdgcn_permlane32_swap(__double2hiint(v), __double2hiint(v), false, false);
+        return op(__hiloint2double((int)hi[0], (int)lo[0]), __hiloint2double((int)hi[1], (int)lo[1]));
     }
     static __device__ __forceinline__ double lane(double v, int l) {
         return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), l), __builtin_amdgcn_readlane(__double2loint(v), l));
@@ -94,8 +113,7 @@ template <class R, int N> __device__ __forceinline__ void cl_wave_reduce(typenam
     }
     v = R::op(v, R::template move<0x114, 0xf>(v));
     v = R::op(v, R::template move<0x118, 0xf>(v));
-    v = R::op(v, R::template move<0x142, 0xa>(v));
-    v = R::op(v, R::template move<0x143, 0xc>(v));
+    v = R::with_half(R::with_row(v));
 #pragma unroll
     for (int i = 0; i < N; ++i) t[i] = R::lane(v, N == 1 ? 63 : 60 + i / 2 + i % 2 * 2);
 }

@@ -85,6 +85,42 @@ def test_codes(ks, n, D, classes, normalize, dtype):
     assert (np.abs(scale.cpu().numpy() - s) <= 1.0001 * U32 * s).all()
 
 
+def rows_of_gpu(codes, n, D, classes):
+    c = codes.view(-1, (D + 31) // 32, 2, 32, 16).permute(0, 3, 1, 2, 4).reshape(-1, 32, (D + 31) // 32 * 32)
+    c = (c.view(-1, 2, 32, c.shape[2]).transpose(1, 2) if classes else c).reshape(-1, c.shape[2])
+    assert not c[n:].any() and not c[:, D:].any()
+    return c[:n, :D]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("classes,normalize", [(False, False), (True, True), (False, True)])
+@pytest.mark.parametrize("n,D", [(16_353, 33), (16_384, 256), (20_001, 300), (17_000, 512), (33_333, 700), (16_400, 1_024), (16_500, 1_500)])
+def test_codes_of_many_rows(ks, n, D, classes, normalize, dtype):
+    gen = torch.Generator("cuda").manual_seed(n + D)
+    V = torch.randn((n, D), generator=gen, device="cuda") * torch.exp(16 * torch.rand((n, 1), generator=gen, device="cuda") - 8)
+    V[n // 2], V[n - 1, D // 2], V[3, 0] = 0.0, float("nan"), INF
+    V = V.to(dtype)
+    codes, scale = ks.class_quantize_rows(V, classes=classes, normalize=normalize)
+    v = V.double()
+    top = v.abs().amax(1)
+    broken, a = ~torch.isfinite(top), torch.where(torch.isfinite(top) & (top > 0), top, 1.0)
+    assert broken.nonzero().flatten().tolist() == [3, n - 1]
+    q = torch.where((broken | (top == 0))[:, None], 0.0, torch.round(v * 127.0 / a[:, None]))
+    assert torch.equal(rows_of_gpu(codes, n, D, classes).double(), q)
+    s = top / 127.0 / (torch.where(top > 0, (v * v).sum(1).sqrt(), 1.0) if normalize else 1.0)
+    assert torch.equal(scale.isnan(), broken)
+    assert ((scale.double() - s).abs() <= 1.0001 * U32 * s)[~broken].all()
+
+
+@pytest.mark.parametrize("classes", [False, True])
+@pytest.mark.parametrize("n,D,ld,shift", [(16_400, 64, 64, 0), (17_001, 500, 503, 1), (16_390, 1_000, 1_024, 4), (16_384, 1_100, 1_100, 0)])
+def test_bytes_of_many_rows(ks, n, D, ld, shift, classes):
+    gen = torch.Generator("cuda").manual_seed(n + D)
+    V = torch.randint(-128, 128, (n * ld + shift,), generator=gen, device="cuda", dtype=torch.int8)[shift:].view(n, ld)[:, :D]
+    codes, scale = ks.class_quantize_rows(V, classes=classes)
+    assert scale is None and torch.equal(rows_of_gpu(codes, n, D, classes), V)
+
+
 def test_codes_at_the_borders(ks):
     """Halves go to the even code, and values next to a half to their own side: rows whose largest value is 127 * 2^e, and rows of
     any largest value with the fp32 numbers around each border."""
@@ -178,6 +214,34 @@ def test_logits_rows_that_lie_apart(ks, B, C, D, dtype, ld, shift):
     z = ks.class_logits_int8(x, xs, y, ys, -2.5, bias=torch.from_numpy(bias).cuda(), out=mat[:, :C])
     near(z, *plain_logits(q, s, w, t, -2.5, bias), dtype)
     assert (whole[:shift] == 77).all() and (mat[:, C:] == 77).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("apart", [False, True])
+@pytest.mark.parametrize("B,C,D", [
+    (300, 40_001, 64), (1_024, 30_000, 33), (257, 65_537, 128), (1_100, 32_700, 128), (1_024, 32_701, 352), (1_000, 32_001, 512), (900, 65_000, 400),
+    (2_050, 16_130, 290), (1_024, 20_001, 512), (257, 30_011, 256), (129, 90_001, 160), (1_300, 9_999, 192), (700, 30_007, 768), (300, 40_000, 1_152),
+    (600, 20_001, 1_184), (300, 33_000, 4_096), (129, 50_001, 2_500), (2_500, 5_001, 1_300), (64, 70_003, 512), (33, 90_001, 1_024), (20, 200_001, 96),
+    (32, 20_000, 800), (50, 16_000, 1_100)])
+def test_products_of_many_classes(ks, B, C, D, dtype, apart):
+    """Batches, layers and depths on both sides of the sizes at which the work is divided in another way; rows next to each other, and
+    rows of an odd distance, with what lies between them."""
+    gen = torch.Generator("cuda").manual_seed(B + C + D)
+    rand = lambda *n: torch.rand(n, generator=gen, device="cuda")  # noqa: E731
+    q, w = (torch.randint(-127, 128, (n, D), generator=gen, device="cuda", dtype=torch.int8) for n in (B, C))
+    xs, ws, bias = 0.001 + 0.1 * rand(B), 0.001 + 0.1 * rand(C), 9 * rand(C) - 4.5
+    x, y = ks.class_quantize_rows(q)[0], ks.class_quantize_rows(w, classes=True)[0]
+    ld, shift = (C + 5 + C % 2, 3) if apart else (C, 0)
+    whole = torch.full((B * ld + shift,), 77.0, dtype=dtype, device="cuda")
+    mat = whole[shift:].view(B, ld)
+    z = ks.class_logits_int8(x, xs, y, ws, 30.0, bias=bias, out=mat[:, :C])
+    assert (whole[:shift] == 77).all() and (mat[:, C:] == 77).all()
+    for lo in range(0, C, 1 << 14):
+        hi = min(C, lo + (1 << 14))
+        plain = torch.mm(q.double(), w[lo:hi].double().t().contiguous()) * (30.0 * xs.double())[:, None] * ws[None, lo:hi].double()
+        want = plain + bias[None, lo:hi].double()
+        off = (z[:, lo:hi].double() - want).abs() - 1.01 * (U32 * (4 * plain.abs() + want.abs()) + TYPES[dtype] * want.abs())
+        assert off.max() <= 0, (lo, float(off.max()))
 
 
 @pytest.mark.parametrize("B", [1, 40, 200])
@@ -330,7 +394,8 @@ def check_adjust(ks, r, B, C, c0, Cg, a, dtype, in_place, ld, shift=0, extreme=T
     (1, 1, 1, 1, 1, True, 1), (1, 10_000, 1, 300, 20, True, 10_000), (5, 1_000, 1, 40, 0, False, 1_000), (4, 999, 3, 0, 30, True, 1_003),
     (3, 8_193, 2, 500, 3, False, 8_200), (7, 4_133, 1, 0, 0, True, 4_136), (9, 20_001, 4, 3_000, 700, True, 20_001), (2, 100, 1, 9_000, 0, True, 104),
     (3, 40_000, 1, 20_000, 100, True, 40_064), (33, 555, 1, 60, 60, True, 560), (70, 250_001, 1, 100, 20, True, 250_008),
-    (2, 70_000, 1, 50_000, 5_000, True, 70_001)])
+    (2, 70_000, 1, 50_000, 5_000, True, 70_001), (17, 9_001, 1, 5_000, 0, True, 9_008), (20, 12_000, 2, 7_000, 1_100, False, 12_001),
+    (16, 3_001, 1, 4_000, 97, True, 3_002), (300, 60_000, 1, 5, 2, True, 60_000)])
 def test_adjust(ks, B, C, nodes, seen, biases, masks, ld, in_place, dtype):
     r = rng_of(B, C, seen, biases)
     Cg, c0 = C * nodes, C * (nodes // 2)
