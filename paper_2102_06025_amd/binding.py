@@ -841,11 +841,13 @@ def class_logits_int8(x_codes, x_scale, w_codes, w_scale, scale, bias=None, out=
     B, C, dev = x_scale.numel(), w_scale.numel(), x_codes.get_device()
     if B < 1 or C < 1:
         raise ValueError("x_scale [B] and w_scale [C] must not be empty")
-    D = x_codes.numel() // ((B + 31) // 32 * 32)  # a multiple of 32: what lies beyond the rows' own depth is 0
+    D = x_codes.numel() // ((B + 31) // 32 * 32)  # what lies beyond the rows' own depth is 0
     if dev < 0:
         raise TypeError("x_codes must be a device tensor")
-    _list(x_codes, torch.int8, L.class_codes_bytes(B, D, 0), "x_codes (of B feature rows)", dev)
-    _list(w_codes, torch.int8, L.class_codes_bytes(C, D, QUANT_CLASSES), "w_codes (of C class rows of the features' depth)", dev)
+    if D % 32 or D < 32:
+        raise ValueError("x_codes must hold the codes of B rows")
+    _list(x_codes, torch.int8, (B + 31) // 32 * 32 * D, "x_codes (of B feature rows)", dev)
+    _list(w_codes, torch.int8, (C + 63) // 64 * 64 * D, "w_codes (of C class rows of the features' depth)", dev)
     _list(x_scale, torch.float32, B, "x_scale", dev)
     _list(w_scale, torch.float32, C, "w_scale", dev)
     if bias is not None:

@@ -18,48 +18,57 @@ typedef int32_t cl_i32x16 __attribute__((ext_vector_type(16)));
 // ------------------------------------------------------------------------------------------------
 // rows -> codes
 // ------------------------------------------------------------------------------------------------
-template <typename IN> struct ClRow;
+template <typename IN> struct ClRow; // four: elements at byte `at` of a row as a buffer, 0 where it has ended
 template <> struct ClRow<float> {
     static __device__ __forceinline__ float one(const float *p) { return *p; }
-    static __device__ __forceinline__ float4 four(const float *p) { return *(const float4 *)p; }
+    template <int AUX> static __device__ __forceinline__ float4 four(__amdgpu_buffer_rsrc_t row, int at) {
+        return __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(row, at, 0, AUX));
+    }
 };
 template <> struct ClRow<uint16_t> {
     static __device__ __forceinline__ float one(const uint16_t *p) { return ks_bf2f(*p); }
-    static __device__ __forceinline__ float4 four(const uint16_t *p) {
-        const uint2 v = *(const uint2 *)p;
+    template <int AUX> static __device__ __forceinline__ float4 four(__amdgpu_buffer_rsrc_t row, int at) {
+        const uint2 v = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(row, at, 0, AUX));
         return make_float4(ks_bf2f(v.x & 0xFFFFu), ks_bf2f(v.x >> 16), ks_bf2f(v.y & 0xFFFFu), ks_bf2f(v.y >> 16));
     }
 };
 template <> struct ClRow<int8_t> {
     static __device__ __forceinline__ float one(const int8_t *p) { return (float)*p; }
-    static __device__ __forceinline__ float4 four(const int8_t *p) {
-        const uint32_t v = *(const uint32_t *)p;
+    template <int AUX> static __device__ __forceinline__ float4 four(__amdgpu_buffer_rsrc_t row, int at) {
+        const uint32_t v = __builtin_amdgcn_raw_buffer_load_b32(row, at, 0, AUX);
         return make_float4((float)(int8_t)v, (float)(int8_t)(v >> 8), (float)(int8_t)(v >> 16), (float)(int8_t)(v >> 24));
     }
 };
-// elements d .. d + 3 of a row, 0 beyond D
-template <typename IN, bool VEC> __device__ __forceinline__ float4 cl_load4(const IN *row, int d, int D) {
-    if (VEC && d + 4 <= D) return ClRow<IN>::four(row + d);
+// the first `left` of four elements one by one, 0 for the others
+template <typename IN> __device__ __forceinline__ float4 cl_load_few(const IN *p, int left) {
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (d < D) v.x = ClRow<IN>::one(row + d);
-    if (d + 1 < D) v.y = ClRow<IN>::one(row + d + 1);
-    if (d + 2 < D) v.z = ClRow<IN>::one(row + d + 2);
-    if (d + 3 < D) v.w = ClRow<IN>::one(row + d + 3);
+    if (left > 0) v.x = ClRow<IN>::one(p);
+    if (left > 1) v.y = ClRow<IN>::one(p + 1);
+    if (left > 2) v.z = ClRow<IN>::one(p + 2);
+    if (left > 3) v.w = ClRow<IN>::one(p + 3);
     return v;
 }
 
-// 127 v / a to the nearest integer, halves to even.  t = v * (127 / a) in fp64 is off by less than 1e-13; where it lies that close
-// to the middle of two integers, |v| * 254 and (2 k + 1) a, which are exact in fp64 (32 bits each), decide.
-__device__ __forceinline__ int cl_code(float v, double inv, double a) {
-    const double t = (double)v * inv;
-    int k = (int)__builtin_rint(t);
-    if (__builtin_fabs(__builtin_fabs(t - (double)k) - 0.5) < 1e-12) {
-        const int lo = (int)__builtin_fabs(t);
-        const double l = __builtin_fabs((double)v) * 254.0, r = (double)(2 * lo + 1) * a;
-        const int m = l > r || (l == r && (lo & 1)) ? lo + 1 : lo;
-        k = v < 0.f ? -m : m;
-    }
-    return k;
+// 127 v / a to the nearest integer, halves to even, where it is one of t's two neighbours: |v| * 254 and (2 lo + 1) a are exact in F, fp64 for fp32
+// rows (32 bits each), fp32 for bf16 (16; both by 2^-10, which keeps them in range).
+template <typename F> __device__ __forceinline__ uint32_t cl_code(float v, float t, F a) {
+    const int lo = (int)fabsf(t);
+    const F l = (F)fabsf(v) * (F)(254.0 / 1024), r = (F)(2 * lo + 1) * (F)(1.0 / 1024) * a;
+    const int m = l > r || (l == r && (lo & 1)) ? lo + 1 : lo;
+    return (v < 0.f ? -m : m) & 255;
+}
+// Four codes as bytes.  inv, 127 / a rounded to fp32, is off by 2^-24 of itself, so t = v * inv by less than 2^-17 (|t| <= 127); added to 1.5 * 2^23
+// it is rounded once, to an integer in the low bits.  Where t lies within 2^-16 of the middle of two (one fp32 value
+// in 30,000), cl_code decides.
+template <typename F> __device__ __forceinline__ uint32_t cl_codes(float4 v, float inv, F a) {
+    const float whole = 12582912.f;
+    const float r0 = fmaf(v.x, inv, whole), r1 = fmaf(v.y, inv, whole), r2 = fmaf(v.z, inv, whole), r3 = fmaf(v.w, inv, whole);
+    const float d0 = fmaf(v.x, inv, whole - r0), d1 = fmaf(v.y, inv, whole - r1), d2 = fmaf(v.z, inv, whole - r2), d3 = fmaf(v.w, inv, whole - r3);
+    uint32_t q = __builtin_amdgcn_perm(__builtin_amdgcn_perm(__float_as_uint(r3), __float_as_uint(r2), 0x0c0c0400u),
+                                       __builtin_amdgcn_perm(__float_as_uint(r1), __float_as_uint(r0), 0x0c0c0400u), 0x05040100u);
+    if (fmaxf(fmaxf(fabsf(d0), fabsf(d1)), fmaxf(fabsf(d2), fabsf(d3))) > 0.5f - 0x1p-16f)
+        q = cl_code(v.x, v.x * inv, a) | cl_code(v.y, v.y * inv, a) << 8 | cl_code(v.z, v.z * inv, a) << 16 | cl_code(v.w, v.w * inv, a) << 24;
+    return q;
 }
 // Reductions of N = 1 or 4 values a lane over the wavefront at once.  Of four, every lane passes two on to its neighbour and keeps two, then
 // one and one; lanes of equal number modulo 4 then hold the same value's parts, and go on four and eight lanes apart, and from row
@@ -121,18 +130,22 @@ template <class R, int N> __device__ __forceinline__ void cl_wave_reduce(typenam
 // A workgroup takes RB consecutive slots (32: a whole block, or 8) of a block of 32 rows, each of its eight wavefronts RB / 8 of them at
 // the same time, and NP * 256 elements of a row at a time: they stay in registers from the search for the largest to the
 // codes (longer rows are read twice), the codes go through LDS so that RB * 16 bytes in a row are stored.
-// What bounds it: the rows in, the codes out (390,625 x 512 fp32 with norms: 1.0 GB).
+// What bounds it: the rows in, the codes out: 390,625 x 512 fp32 with norms 182 us (1.0 GB at 5.5 TB/s), bf16 135 (0.6 GB at 4.4 TB/s: the ties of
+// values of 8 bits, 8 % of the time, and the sums of squares), int8 69; few rows: the launch and one row's way through it, 3 us.
+// Wavefronts per SIMD: fp32 rows of 257 .. 512 elements do not fit into 64 registers (with 8 of them 192 us, with 6 182).
 #define CLQ_NT 512
 template <int RB, int NP, typename IN, bool VEC>
-__global__ void __launch_bounds__(CLQ_NT)
+__global__ void __launch_bounds__(CLQ_NT, RB * NP < 64 ? 8 : RB * NP > 64 ? 4 : sizeof(IN) == 4 ? 6 : 8)
 cl_quantize_kernel(const IN *__restrict__ V, int64_t n, int D, int64_t ldv, uint32_t flags, int8_t *__restrict__ codes,
-                   float *__restrict__ row_scale, int64_t blk0) { // blk0: the launch's first block
+                   float *__restrict__ row_scale, int64_t blk0, int stream_out) { // blk0: the launch's first block
     constexpr int RW = RB / 8, DC = NP * 256, HALF = RB * 16 + 16; // rows of a wavefront; elements at a time; bytes of a half of a piece and padding that spreads the halves over the banks
     __shared__ __attribute__((aligned(16))) char lds[DC / 16 * HALF];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t blk = blk0 + blockIdx.x / (32 / RB);
     const int slot0 = blockIdx.x % (32 / RB) * RB, kb = (D + 31) / 32;
     constexpr bool RAW = sizeof(IN) == 1;
+    // many rows of more than 1 KB pass by the caches (100,000 x 1,024 fp32: 82 us, 92 through them; but x 128: 75, 71, and rows that are read twice gain by them)
+    constexpr int AUX = RB == 32 && NP > 1 ? 2 : 0;
     const auto row_of = [&](int i) __attribute__((always_inline)) {
         const int slot = slot0 + wave * RW + i;
         return flags & KS_QUANT_CLASSES ? (blk >> 1) * CL_GROUP + 2 * slot + (blk & 1) : blk * 32 + slot;
@@ -143,8 +156,18 @@ cl_quantize_kernel(const IN *__restrict__ V, int64_t n, int D, int64_t ldv, uint
         for (int i = 0; i < RW; ++i) {
             const int64_t row = row_of(i);
             const IN *v = V + (row < n ? row : n - 1) * ldv;
+            const int len = row < n ? D : 0;
+            if (VEC) { // whole fours as a buffer that ends with the last of them, which needs no branch
+                const __amdgpu_buffer_rsrc_t whole = __builtin_amdgcn_make_buffer_rsrc((void *)v, 0, (len & ~3) * (int)sizeof(IN), 0x00020000);
 #pragma unroll
-            for (int e = 0; e < NP; ++e) x[i][e] = cl_load4<IN, VEC>(v, d0 + e * 256 + lane * 4, row < n ? D : 0);
+                for (int e = 0; e < NP; ++e) x[i][e] = ClRow<IN>::template four<AUX>(whole, (d0 + e * 256 + lane * 4) * (int)sizeof(IN));
+            }
+            if (!VEC || (D & 3))
+#pragma unroll
+                for (int e = 0; e < NP; ++e) {
+                    const int d = d0 + e * 256 + lane * 4;
+                    if (!VEC || (d < len && d + 4 > len)) x[i][e] = cl_load_few(v + d, len - d);
+                }
         }
     };
     int top[RW];  // bits of the largest |v|: ordered as the values, NaN above infinity
@@ -178,18 +201,21 @@ cl_quantize_kernel(const IN *__restrict__ V, int64_t n, int D, int64_t ldv, uint
     for (int i = 1; i < RW; ++i)
         if (lane % RW == i) { my_top = top[i]; my_ss = ss[i]; }
     const double my_a = my_top < 0x7F800000 ? (double)__int_as_float(my_top) : 0.0; // not finite: codes 0
-    const double my_inv = my_a > 0.0 ? 127.0 / my_a : 0.0;
+    const float up = my_a < 0x1p-100 ? 0x1p100f : 1.f; // rows of which 127 / a might be no fp32 number
+    const float my_inv = my_a > 0.0 ? (float)(127.0 / (my_a * up)) : 0.f;
     if (!RAW) {
         double scale = my_a / 127.0;
         if ((flags & KS_QUANT_NORMALIZE) && my_a > 0.0) scale /= sqrt(my_ss);
         const int64_t row = row_of(lane % RW);
         if (lane < RW && row < n) row_scale[row] = my_top < 0x7F800000 ? (float)scale : __int_as_float(0x7FC00000);
     }
-    double a[RW], inv[RW];
+    typedef std::conditional_t<sizeof(IN) == 4, double, float> F;
+    F a[RW];
+    float inv[RW];
 #pragma unroll
     for (int i = 0; i < RW; ++i) {
-        a[i] = ClSumD::lane(my_a, i);
-        inv[i] = ClSumD::lane(my_inv, i);
+        a[i] = (F)ClSumD::lane(my_a, i);
+        inv[i] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_inv), i));
     }
     for (int d0 = 0; d0 < D; d0 += DC) {
         if (RAW || D > DC) load(d0);
@@ -199,19 +225,24 @@ cl_quantize_kernel(const IN *__restrict__ V, int64_t n, int D, int64_t ldv, uint
 #pragma unroll
             for (int e = 0; e < NP; ++e) {
                 const int d = e * 256 + lane * 4;
-                const float4 v = x[i][e];
-                int c0 = (int)v.x, c1 = (int)v.y, c2 = (int)v.z, c3 = (int)v.w;
-                if (!RAW) {
-                    if (a[i] > 0.0) { c0 = cl_code(v.x, inv[i], a[i]); c1 = cl_code(v.y, inv[i], a[i]); c2 = cl_code(v.z, inv[i], a[i]); c3 = cl_code(v.w, inv[i], a[i]); }
-                    else c0 = c1 = c2 = c3 = 0;
+                float4 v = x[i][e];
+                F ai = a[i];
+                if (!RAW && ai < (F)0x1p-100) {
+                    v.x *= 0x1p100f; v.y *= 0x1p100f; v.z *= 0x1p100f; v.w *= 0x1p100f;
+                    ai *= (F)0x1p100;
                 }
-                const uint32_t q = (c0 & 255) | (c1 & 255) << 8 | (c2 & 255) << 16 | (uint32_t)c3 << 24;
+                const uint32_t q = RAW ? ((int)v.x & 255) | ((int)v.y & 255) << 8 | ((int)v.z & 255) << 16 | (uint32_t)(int)v.w << 24
+                                       : a[i] > 0 ? cl_codes(v, inv[i], ai) : 0;
                 if (d < len) *(uint32_t *)(lds + (d >> 4) * HALF + (wave * RW + i) * 16 + (d & 15)) = q;
             }
         __syncthreads();
         int8_t *out = codes + (blk * kb + d0 / 32) * CL_PIECE + slot0 * 16;
-        for (int e = threadIdx.x; e < len / 16 * RB; e += CLQ_NT) // 16 bytes each: row e % RB of half-piece e / RB
-            *(uint4 *)(out + (int64_t)(e / RB) * 512 + e % RB * 16) = *(const uint4 *)(lds + e / RB * HALF + e % RB * 16);
+        for (int e = threadIdx.x; e < len / 16 * RB; e += CLQ_NT) { // 16 bytes each: row e % RB of half-piece e / RB
+            const cl_i32x4 q = *(const cl_i32x4 *)(lds + e / RB * HALF + e % RB * 16);
+            cl_i32x4 *const to = (cl_i32x4 *)(out + (int64_t)(e / RB) * 512 + e % RB * 16);
+            if (stream_out) __builtin_nontemporal_store(q, to);
+            else *to = q;
+        }
         if (d0 + DC < D) __syncthreads();
     }
 }
@@ -225,16 +256,22 @@ extern "C" size_t class_codes_bytes(int64_t n, int D, uint32_t flags) {
 template <typename IN, bool VEC>
 static void cl_quantize(const void *V, int64_t n, int D, int64_t ldv, uint32_t flags, int8_t *codes, float *row_scale, hipStream_t st) {
     const int64_t blocks = flags & KS_QUANT_CLASSES ? ks_ceil_div(n, CL_GROUP) * 2 : ks_ceil_div(n, 32);
+    // codes of 4 MB (an XCD's cache) or more pass by the caches (390,625 x 512 int8: 65 us, 98 through them; then its product of fp32
+    // rows and 64 samples: 234 us together, 239)
+    const int stream_out = blocks * ((D + 31) / 32) >= 4096;
     const auto go = [&](auto kernel, int rb) { // a launch's threads are counted in 32 bits
         for (int64_t b0 = 0; b0 < blocks; b0 += 1 << 20)
             hipLaunchKernelGGL(kernel, dim3((unsigned)((blocks - b0 < 1 << 20 ? blocks - b0 : 1 << 20) * (32 / rb))), dim3(CLQ_NT), 0, st, (const IN *)V,
-                               n, D, ldv, flags, codes, row_scale, b0);
+                               n, D, ldv, flags, codes, row_scale, b0, stream_out);
     };
     // whole blocks where there are enough of them and a wavefront holds four rows; else a row a wavefront
     if (blocks >= 512 && D <= 256) go(cl_quantize_kernel<32, 1, IN, VEC>, 32);
     else if (blocks >= 512 && D <= 512) go(cl_quantize_kernel<32, 2, IN, VEC>, 32);
     else if (blocks >= 512 && D <= 1024) go(cl_quantize_kernel<32, 4, IN, VEC>, 32);
+    else if (D <= 256) go(cl_quantize_kernel<8, 1, IN, VEC>, 8);
     else if (D <= 512) go(cl_quantize_kernel<8, 2, IN, VEC>, 8);
+    else if (D <= 1024) go(cl_quantize_kernel<8, 4, IN, VEC>, 8);
+    else if (D <= 2048) go(cl_quantize_kernel<8, 8, IN, VEC>, 8);
     else go(cl_quantize_kernel<8, 16, IN, VEC>, 8);
 }
 template <typename IN>

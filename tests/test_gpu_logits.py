@@ -141,6 +141,20 @@ def test_codes_at_the_borders(ks):
     assert (np.abs(scale.cpu().numpy() - s) <= 1.0001 * U32 * s + 2.0 ** -150).all()
 
 
+@pytest.mark.parametrize("n", [1, 16_400])
+def test_codes_of_every_bf16_value(ks, n):
+    """All bf16 values of the eleven binades up to the largest of the row, both signs: ties among them in every row."""
+    for top in (0x7F7F, 0x7F00, 0x7E81, 0x3F80, 0x3FD5, 0x3F83, 0x2001, 0x0D81, 0x0D7F, 0x0600, 0x0087):
+        bits = np.arange(max(1, top - 11 * 128), top + 1, dtype=np.int64)
+        bits = np.concatenate([bits, bits | 0x8000])
+        row = torch.from_numpy((bits << 16).astype(np.uint32).view(np.float32)).cuda()
+        V = row.to(torch.bfloat16)[None].expand(n, -1).contiguous()
+        codes, scale = ks.class_quantize_rows(V)
+        q, s = plain_codes(row.cpu().numpy()[None])
+        assert torch.equal(rows_of_gpu(codes, n, len(bits), False), torch.from_numpy(q.astype(np.int8)).cuda().expand(n, -1)), hex(top)
+        assert (np.abs(scale.cpu().numpy() - s) <= 1.0001 * U32 * s + 2.0 ** -150).all()
+
+
 def test_codes_of_empty_and_broken_rows(ks):
     V = rng_of(3).standard_normal((9, 70)).astype(np.float32)
     V[1], V[2], V[3, 5], V[4, 69], V[5, 0] = 0.0, -0.0, np.inf, np.nan, -np.inf
@@ -489,7 +503,8 @@ def test_binding_refuses(ks):
     x, xs = ks.class_quantize_rows(V)
     w, ws = ks.class_quantize_rows(V, classes=True)
     for bad in (dict(w_codes=x), dict(bias=torch.ones(5, device="cuda")), dict(out=torch.empty((4, 5), device="cuda")),
-                dict(w_codes=ks.class_quantize_rows(torch.ones((4, 40), device="cuda"), classes=True)[0])):
+                dict(x_codes=x[:512]), dict(x_codes=x[:1000]), dict(x_scale=torch.ones(33, device="cuda")), dict(x_codes=x[:0]),
+                dict(x_codes=x[:512], w_codes=w[:1024]), dict(w_codes=ks.class_quantize_rows(torch.ones((4, 40), device="cuda"), classes=True)[0])):
         with pytest.raises(ValueError):
             ks.class_logits_int8(**{**dict(x_codes=x, x_scale=xs, w_codes=w, w_scale=ws, scale=1.0), **bad})
     with pytest.raises(TypeError):
