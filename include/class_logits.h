@@ -74,8 +74,8 @@ int class_logits_int8(const int8_t *x_codes, const float *x_scale, const int8_t 
  * keeps its logit's bits.  A mask that allows nothing leaves a row of -infinity.
  *
  *   logits [B, C]    in, dtype KS_DTYPE_FP32 or KS_DTYPE_BF16, row i at element i * ldl
- *   out    [B, C]    out, same dtype, row i at element i * ldo; out == logits (then ldo == ldl): in place, where only the logits of
- *                    listed classes are read and only they and the masked ones are written; any other overlap is not allowed
+ *   out    [B, C]    out, same dtype, row i at element i * ldo; out == logits (then ldo == ldl): in place, where only listed and masked
+ *                    classes' logits change; any other overlap is not allowed
  *   C, c0, Cg        the columns are the classes [c0, c0 + C) of a problem with Cg (c0 + C <= Cg).  Lists carry ids of the whole
  *                    problem: another node's classes are passed over, negative ids are empty entries, ids >= Cg set KS_DEV_BAD_LABEL
  *   seen_offsets [B + 1], seen_ids [seen_len]   the list of request i is seen_ids[seen_offsets[i] .. seen_offsets[i + 1]); NULL

@@ -642,21 +642,26 @@ cl_steady_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
         int grp = first + wave;
         if (grp >= last) continue;
         const int block_bytes = kb * CL_PIECE;
-        const auto group_codes = [&](int g) __attribute__((always_inline)) {
-            return __builtin_amdgcn_make_buffer_rsrc((void *)(wq + (int64_t)(g_lo + g) * 2 * block_bytes), 0, 2 * block_bytes, 0x00020000);
+        const auto block_codes = [&](int g, int q) __attribute__((always_inline)) { // of a group's block: 0 beyond the depth
+            return __builtin_amdgcn_make_buffer_rsrc((void *)(wq + ((int64_t)(g_lo + g) * 2 + q) * block_bytes), 0, block_bytes, 0x00020000);
         };
-        const auto codes = [&](__amdgpu_buffer_rsrc_t p, int k, int q) __attribute__((always_inline)) { // beyond the depth: another piece, or 0
-            return __builtin_bit_cast(cl_i32x4, __builtin_amdgcn_raw_buffer_load_b128(p, lane * 16 + k % 4 * CL_PIECE, q * block_bytes + k / 4 * 4 * CL_PIECE, 0));
+        uint32_t at[2] = {0, 0}; // of the four pieces from k - k % 4 on: one register a block, not one for every four
+        const auto codes = [&](__amdgpu_buffer_rsrc_t p, int k, int q) __attribute__((always_inline)) {
+            if (k % 4 == 0) {
+                at[q] = lane * 16 + k * CL_PIECE;
+                asm volatile("" : "+v"(at[q]));
+            }
+            return __builtin_bit_cast(cl_i32x4, __builtin_amdgcn_raw_buffer_load_b128(p, at[q] + k % 4 * CL_PIECE, 0, 0));
         };
         cl_i32x4 w[KB][2], x[4];
         cl_i32x16 acc[2][2];
         {
-            const __amdgpu_buffer_rsrc_t p = group_codes(grp);
+            const __amdgpu_buffer_rsrc_t p[2] = {block_codes(grp, 0), block_codes(grp, 1)};
 #pragma unroll
             for (int k = 0; k < KB; ++k)
 #pragma unroll
                 for (int q = 0; q < 2; ++q) { // in the order in which they are used: the main loop's counted waits hold for these too
-                    w[k][q] = codes(p, k, q);
+                    w[k][q] = codes(p[q], k, q);
                     __builtin_amdgcn_sched_barrier(0);
                 }
         }
@@ -680,7 +685,7 @@ cl_steady_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
             int got = 0;
             if (lane == 0) got = atomicAdd(&s_next, 1);
             const int next = __builtin_amdgcn_readfirstlane(got);
-            const __amdgpu_buffer_rsrc_t p_next = group_codes(next < last ? next : grp);
+            const __amdgpu_buffer_rsrc_t p_next[2] = {block_codes(next < last ? next : grp, 0), block_codes(next < last ? next : grp, 1)};
             const int64_t c0 = (int64_t)(g_lo + grp) * CL_GROUP, c = c0 + 2 * (lane & 31);
             float nsw[2], nb[2];
 #pragma unroll
@@ -704,7 +709,7 @@ cl_steady_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
                     x[k & 3] = *(const cl_i32x4 *)(k + 4 < KB ? xp + (k + 4) * CL_PIECE : xn + (k + 4 - KB) * CL_PIECE);
                     if (reload)
 #pragma unroll
-                        for (int q = 0; q < 2; ++q) w[k][q] = codes(p_next, k, q);
+                        for (int q = 0; q < 2; ++q) w[k][q] = codes(p_next[q], k, q);
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
                         if (r * KB / 16 == k) finish(before, r, f);
@@ -1105,16 +1110,17 @@ __global__ void __launch_bounds__(NT) cl_hash_kernel(ClAdjust a, int requests, i
 #define CLL_SLOTS 6144
 #define CLL_TRIES 256
 template <typename T>
-__global__ void __launch_bounds__(1024) cl_long_kernel(ClAdjust a, int parts) {
+__global__ void __launch_bounds__(1024) cl_long_kernel(ClAdjust a, int per_row, int fill) {
     __shared__ uint32_t s_key[CLL_SLOTS], s_seen[CLL_SLOTS]; // column + 1, 0: free
     __shared__ int s_bias[CLL_SLOTS];
     __shared__ int s_full;
-    const int b = a.row0 + blockIdx.x / parts, part = blockIdx.x % parts;
+    const int b = a.row0 + blockIdx.x / per_row, part = blockIdx.x % per_row;
     int64_t sf = 0, bf = 0;
     const int ns = cl_list(a.seen_offsets, a.seen_len, a.seen_max, b, &sf, a.dev_status);
     const int nb = cl_list(a.bias_offsets, a.bias_len, a.bias_max, b, &bf, a.dev_status);
     const int m = cl_mask_of(a, b);
-    if (ns + nb == 0) return;
+    const int need = (ns + nb + 4095) / 4096, parts = need > fill ? need : fill; // at most per_row, which is for the longest list
+    if (ns + nb == 0 || part >= parts) return;
     const int prompt = a.n_prompt ? a.n_prompt[b] : 0;
     const T *in = (const T *)a.in + b * a.ldl;
     T *out = (T *)a.out + b * a.ldo;
@@ -1222,7 +1228,7 @@ template <typename T> static void cl_adjust(const ClAdjust &args, hipStream_t st
         // workgroups fit on a compute unit, and one list of 20,000 takes 26 us in 16 parts, 22 in 64
         const int fill = (int)ks_ceil_div(512, args.B) < 64 ? (int)ks_ceil_div(512, args.B) : 64, need = (int)ks_ceil_div(entries, 4096), parts = need > fill ? need : fill;
         cl_rows(args, parts, [&](const ClAdjust &a, int rows) {
-            hipLaunchKernelGGL(cl_long_kernel<T>, dim3((unsigned)parts * (unsigned)rows), dim3(1024), 0, st, a, parts);
+            hipLaunchKernelGGL(cl_long_kernel<T>, dim3((unsigned)parts * (unsigned)rows), dim3(1024), 0, st, a, parts, fill);
         });
     }
 }
@@ -1235,7 +1241,7 @@ extern "C" int class_logits_adjust(const void *logits, int64_t ldl, void *out, i
                                    int64_t ld_allowed, int n_masks, const int32_t *mask_row, int32_t *dev_status, void *stream) {
     if (!logits || !out || B < 1 || C < 1 || c0 < 0 || Cg >= (int64_t)1 << 31 || c0 + C > Cg || ldl < C || ldo < C) return KS_INVALID_ARG;
     if (dtype != KS_DTYPE_BF16 && dtype != KS_DTYPE_FP32) return KS_INVALID_ARG;
-    if (((uintptr_t)logits | (uintptr_t)out) % (dtype == KS_DTYPE_FP32 ? 4 : 2) || (logits == out && ldl != ldo)) return KS_INVALID_ARG;
+    if (((uintptr_t)logits | (uintptr_t)out) % (dtype == KS_DTYPE_FP32 ? 4 : 2) || (logits == out && ldl != ldo && B > 1)) return KS_INVALID_ARG;
     if (seen_len < 0 || bias_len < 0 || seen_max < 0 || bias_max < 0 || (int64_t)seen_max + bias_max >= (int64_t)1 << 30) return KS_INVALID_ARG;
     if (seen_offsets && seen_len && !seen_ids) return KS_INVALID_ARG;
     if (bias_offsets && bias_len && (!bias_ids || !bias_values)) return KS_INVALID_ARG;

@@ -434,6 +434,22 @@ def test_adjust_one_kind_at_a_time(ks, seen, biases):
         check_adjust(ks, r, 4, 30_000, 0, 30_000, a, torch.float32, True, 30_000, seen_max=seen, bias_max=biases)
 
 
+def test_adjust_lists_far_shorter_than_the_array(ks):
+    """Many requests without word of their longest list: what the array holds is all that is known."""
+    r = rng_of(5)
+    for B, most in ((60, 400), (300, 90), (7, 6_000)):
+        check_adjust(ks, r, B, 5_001, 0, 5_001, adjust_case(r, B, 5_001, 5_001, most, 9, True), torch.float32, True, 5_001)
+
+
+def test_adjust_one_row_in_place_by_another_view(ks):
+    z = torch.randn((1, 64), generator=torch.Generator().manual_seed(2)).cuda()
+    want = z.clone()
+    want[0, 5] = -INF
+    allowed = torch.tensor([[~(1 << 5), -1]], dtype=torch.int32, device="cuda")
+    ks.class_logits_adjust(z, out=z.as_strided((1, 64), (100, 1)), allowed=allowed)
+    assert torch.equal(z, want)
+
+
 def test_adjust_the_same_class_again_and_again(ks):
     """One class all along a list, once in the prompt and then behind it; of a class named twice among the biases the last one counts."""
     for n in (5, 3_000, 20_000):
