@@ -1036,8 +1036,9 @@ __global__ void __launch_bounds__(CL_NT) cl_mask_kernel(ClAdjust a, int per_row)
 // Lists of a request that a hash table of SLOTS classes in LDS holds (two thirds of the slots): each of them counts the class's occurrences
 // and keeps the last of its biases.  The entry that takes a slot fetches the logit at once, so that it arrives while the others
 // are counted, and adjusts it afterwards; nothing is read or written but the lists and the logits of their classes.
-// MASKS > 0: the workgroups behind the requests' carry out the masks in place (1: element by element, 2: vectors): no logit
-// belongs to both, so that one launch does for both.
+// MASKS 1, 2: the workgroups behind the requests' carry out the masks in place (1: element by element, 2: vectors): no logit
+// belongs to both, so that one launch does for both.  3, 4: the same, but into another matrix: a request's workgroup copies its
+// short row first.
 #define CLH_ENTRIES(slots) ((slots) / 3 * 2)
 #define CLH_SMALL 1536
 #define CLH_MID 6144
@@ -1048,7 +1049,7 @@ __global__ void __launch_bounds__(NT) cl_hash_kernel(ClAdjust a, int requests, i
     static_assert(K * NT == CLH_ENTRIES(SLOTS), "");
     __shared__ uint32_t s_key[SLOTS], s_seen[SLOTS]; // column + 1, 0: free
     __shared__ int s_bias[SLOTS];
-    if (MASKS && (int)blockIdx.x >= requests) {
+    if ((MASKS == 1 || MASKS == 2) && (int)blockIdx.x >= requests) {
         const int i = blockIdx.x - requests;
         cl_mask_part<T, false, MASKS == 2, false, NT>(a, a.row0 + i / per_row, i % per_row);
         return;
@@ -1058,6 +1059,8 @@ __global__ void __launch_bounds__(NT) cl_hash_kernel(ClAdjust a, int requests, i
     const int ns = cl_list(a.seen_offsets, a.seen_len, a.seen_max, b, &sf, a.dev_status);
     const int nb = cl_list(a.bias_offsets, a.bias_len, a.bias_max, b, &bf, a.dev_status);
     const int m = cl_mask_of(a, b);
+    if (MASKS > 2)
+        for (int part = 0; part < per_row; ++part) cl_mask_part<T, true, MASKS == 4, false, NT>(a, b, part);
     if (ns + nb == 0) return;
     const int prompt = a.n_prompt ? a.n_prompt[b] : 0;
     for (int e = threadIdx.x; e < SLOTS; e += NT) { s_key[e] = 0; s_seen[e] = 0; s_bias[e] = -1; }
@@ -1096,6 +1099,7 @@ __global__ void __launch_bounds__(NT) cl_hash_kernel(ClAdjust a, int requests, i
         else if (e < prompt) atomicOr(&s_seen[at], 1u);
         else atomicAdd(&s_seen[at], 2u);
     }
+    if (MASKS > 2) __builtin_amdgcn_s_waitcnt(0x0F70); // vmcnt(0): the row is copied before a logit of it changes
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < K; ++i)
@@ -1196,8 +1200,12 @@ template <typename T> static void cl_adjust(const ClAdjust &args, hipStream_t st
     // bf16 on by themselves, reading what they change in part: a bf16 vector has eight elements, stored one by one, and reading
     // it costs less than they do (256 x 390,625, half of the classes: 49 us, 82; fp32, four elements: 112, 90)
     const bool rmw = !copy && vec && sizeof(T) == 2 && (int64_t)args.B * args.C >= 1 << 24;
+    // short rows into another matrix: a workgroup each copies and changes its own, if three rounds of 1,024 threads do for the copy (1 x
+    // 10,000 fp32: 5.4 us, 7.9 in two launches; x 24,000: 7.4, 8.7; x 32,000: 8.2, 8.3) and there is one for every compute unit at most
+    // (2,048 x 1,000 with long lists: 38, 28)
+    const bool whole = copy && entries > 0 && entries <= CLH_ENTRIES(CLH_MID) && args.B <= 256 && ks_ceil_div(args.C, (int64_t)CLM_U(true) * 1024 * E) <= 3;
     const bool fused = !copy && args.allowed && !rmw && entries > 0 && entries <= CLH_ENTRIES(CLH_MID);
-    if ((copy || args.allowed) && !fused) {
+    if ((copy || args.allowed) && !fused && !whole) {
         const int per_row = (int)ks_ceil_div(args.C, (int64_t)CLM_U(copy) * CL_NT * E);
         cl_rows(args, per_row, [&](const ClAdjust &a, int rows) {
             const dim3 grid((unsigned)per_row * (unsigned)rows);
@@ -1209,20 +1217,22 @@ template <typename T> static void cl_adjust(const ClAdjust &args, hipStream_t st
         });
     }
     if (entries == 0) return;
-    const auto hash = [&](auto alone, auto with_elements, auto with_vectors, int nt) {
-        const int per_row = fused ? (int)ks_ceil_div(args.C, (int64_t)CLM_U(false) * nt * E) : 0;
-        cl_rows(args, 1 + per_row, [&](const ClAdjust &a, int rows) {
-            hipLaunchKernelGGL(!fused ? alone : vec ? with_vectors : with_elements, dim3((unsigned)rows * (unsigned)(1 + per_row)), dim3(nt), 0, st, a, rows, per_row);
+    const auto hash = [&](auto kernel, int nt) {
+        const int per_row = fused || whole ? (int)ks_ceil_div(args.C, (int64_t)CLM_U(whole) * nt * E) : 0;
+        cl_rows(args, fused ? 1 + per_row : 1, [&](const ClAdjust &a, int rows) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)rows * (unsigned)(fused ? 1 + per_row : 1)), dim3(nt), 0, st, a, rows, per_row);
         });
     };
-    if (entries <= CLH_ENTRIES(CLH_SMALL))
-        hash(cl_hash_kernel<T, CLH_SMALL, 256, 0>, cl_hash_kernel<T, CLH_SMALL, 256, 1>, cl_hash_kernel<T, CLH_SMALL, 256, 2>, 256);
+    if (entries <= CLH_ENTRIES(CLH_SMALL) && whole)
+        hash(vec ? cl_hash_kernel<T, CLH_SMALL, 1024, 4> : cl_hash_kernel<T, CLH_SMALL, 1024, 3>, 1024);
+    else if (entries <= CLH_ENTRIES(CLH_SMALL))
+        hash(!fused ? cl_hash_kernel<T, CLH_SMALL, 256, 0> : vec ? cl_hash_kernel<T, CLH_SMALL, 256, 2> : cl_hash_kernel<T, CLH_SMALL, 256, 1>, 256);
     else if (entries <= CLH_ENTRIES(CLH_MID))
-        hash(cl_hash_kernel<T, CLH_MID, 1024, 0>, cl_hash_kernel<T, CLH_MID, 1024, 1>, cl_hash_kernel<T, CLH_MID, 1024, 2>, 1024);
+        hash(whole ? (vec ? cl_hash_kernel<T, CLH_MID, 1024, 4> : cl_hash_kernel<T, CLH_MID, 1024, 3>)
+             : !fused ? cl_hash_kernel<T, CLH_MID, 1024, 0> : vec ? cl_hash_kernel<T, CLH_MID, 1024, 2> : cl_hash_kernel<T, CLH_MID, 1024, 1>, 1024);
     else if (entries <= CLH_ENTRIES(CLH_LARGE) && args.B >= 16) { // few requests leave most of the chip idle with one workgroup each
         // (131,072 classes, bf16, lists of 8,000: 16 requests 24 us, 26 in parts; 128: 33, 37; 256 of 6,000: 13, 29; one of 9,000: 30, 15)
-        const auto kernel = cl_hash_kernel<T, CLH_LARGE, 1024, 0>;
-        hash(kernel, kernel, kernel, 1024); // the masks are set already
+        hash(cl_hash_kernel<T, CLH_LARGE, 1024, 0>, 1024); // the masks are set already
     } else {
         // parts of 4,096 entries on average (of 2,048: 256 lists of 20,000 202 us, 137), more where there are few requests: two
         // workgroups fit on a compute unit, and one list of 20,000 takes 26 us in 16 parts, 22 in 64

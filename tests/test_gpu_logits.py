@@ -409,7 +409,8 @@ def check_adjust(ks, r, B, C, c0, Cg, a, dtype, in_place, ld, shift=0, extreme=T
     (3, 8_193, 2, 500, 3, False, 8_200), (7, 4_133, 1, 0, 0, True, 4_136), (9, 20_001, 4, 3_000, 700, True, 20_001), (2, 100, 1, 9_000, 0, True, 104),
     (3, 40_000, 1, 20_000, 100, True, 40_064), (33, 555, 1, 60, 60, True, 560), (70, 250_001, 1, 100, 20, True, 250_008),
     (2, 70_000, 1, 50_000, 5_000, True, 70_001), (17, 9_001, 1, 5_000, 0, True, 9_008), (20, 12_000, 2, 7_000, 1_100, False, 12_001),
-    (16, 3_001, 1, 4_000, 97, True, 3_002), (300, 60_000, 1, 5, 2, True, 60_000)])
+    (16, 3_001, 1, 4_000, 97, True, 3_002), (300, 60_000, 1, 5, 2, True, 60_000), (256, 24_576, 1, 900, 100, True, 24_576),
+    (3, 24_577, 1, 900, 100, True, 24_584), (257, 1_000, 2, 2_000, 10, True, 1_000), (2, 6_143, 1, 3_000, 90, False, 6_143), (4, 49_152, 1, 1_000, 24, True, 49_160)])
 def test_adjust(ks, B, C, nodes, seen, biases, masks, ld, in_place, dtype):
     r = rng_of(B, C, seen, biases)
     Cg, c0 = C * nodes, C * (nodes // 2)
