@@ -624,3 +624,36 @@ def test_two_calls_at_once(ks):
     torch.cuda.synchronize()
     for pair in got:
         assert all(torch.equal(g, w) for g, w in zip(pair, want))
+
+
+@pytest.mark.parametrize("B,C,D,seen,dtype", [(300, 66_000, 128, 5_000, torch.bfloat16), (300, 33_000, 1_200, 9_000, torch.float32),
+                                              (256, 20_000, 512, 700, torch.bfloat16)])
+def test_large_answers_captured_and_replayed(ks, B, C, D, seen, dtype):
+    """The kernels of large batches and long lists, with the weights' codes made inside the graph; eager calls between the replays."""
+    gen = torch.Generator("cuda").manual_seed(B + C + D)
+    weights = [torch.randn((C, D), generator=gen, device="cuda") for _ in range(2)]
+    batches = [torch.randn((B, D), generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2)]
+    a = to_gpu(adjust_case(rng_of(B, C), B, C, C, seen, 30, True))
+    a.update(seen_max=seen, bias_max=30, dev_status=torch.zeros(1, dtype=torch.int32, device="cuda"))
+
+    def whole(W, X, out, copy):
+        W8, ws = ks.class_quantize_rows(W, classes=True, normalize=True)
+        x, xs = ks.class_quantize_rows(X)
+        z = ks.class_logits_int8(x, xs, W8, ws, 30.0, out=out)
+        ks.class_logits_adjust(z, out=copy, **a)
+        return ks.class_logits_adjust(z, **a)
+
+    new = lambda: torch.empty((B, (C + 63) // 64 * 64), dtype=dtype, device="cuda")[:, :C]  # noqa: E731
+    W, X, out, copy = weights[0].clone(), batches[0].clone(), new(), new()
+    want = [whole(weights[k], batches[k], new(), new()).clone() for k in range(2)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        whole(W, X, out, copy)
+    for k in (1, 0, 1):
+        W.copy_(weights[k])
+        X.copy_(batches[k])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[k]) and torch.equal(copy, want[k]) and int(a["dev_status"]) == 0
+        assert torch.equal(whole(weights[k], batches[k], new(), new()), want[k])
