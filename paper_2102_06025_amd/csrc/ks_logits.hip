@@ -739,17 +739,19 @@ cl_steady_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
 }
 
 // Deeper rows: as in cl_resident_kernel, but the samples pass through LDS in chunks of eight k-steps, which eight wavefronts with 64
-// classes each read at the same time: three buffers, a barrier a chunk (2,048 x 131,072 x 4,096: 1,069 us = 2.06 POP/s, with
-// chunks of four 1,092; the matrix pipes are busy for 56 % of the time at 1.9 GHz, what holds them up are the loads, 20 KB for 64
-// instructions, which wait for the L2 just as long: 907 us with codes of 0, which cost little power.  A tile of 256 x 256 with both sides in LDS and one wavefront a SIMD came to 1,118).  While chunk t is multiplied, the fragments are read one k-step ahead (the
-// last ones from chunk t + 1, which is there since the barrier), chunk t + 2 is written to LDS from registers and those are
-// requested anew for chunk t + 3.  The chunks run on from one tile of 512 classes by 128 samples to the next.
+// classes each read at the same time: three buffers, a barrier a chunk.  2,048 x 131,072 x 4,096: 1,043 us = 2.11 POP/s, the matrix
+// pipes 56 % busy at 1.9 GHz (codes of 0, which cost little power: 907).  What holds them up is the operands' way into the registers, for 64
+// instructions 32 KB from LDS and 20 KB through the caches: neither weights six k-steps ahead (1,054) nor 256 classes by 256 samples, which
+// need 16 KB of the L2 instead of 20 (1,110), nor both sides in LDS and one wavefront a SIMD (1,118) were faster.
+// While chunk t is multiplied, a fragment is read for the next k-step when it has been used (the last ones from chunk t + 1, which is
+// there since the barrier), and chunk t + 2 is written to LDS from registers, each half of it half a chunk after it was requested.
+// The chunks run on from one tile of 512 classes by 128 samples to the next.
 template <typename OUT>
 __global__ void __launch_bounds__(CLX_NT, 2)
 cl_staged_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, const int8_t *__restrict__ wq,
                  const float *__restrict__ ws, const float *__restrict__ bias, int64_t C, int kb, int B, float scale,
                  OUT *__restrict__ out, int64_t ldl, int vec) {
-    constexpr int NW = CLX_NT / 64, R = 8, RW = 4 /* k-steps of weights ahead */, CHUNK = R * 4 * CL_PIECE;
+    constexpr int NW = CLX_NT / 64, R = 8, RW = 4 /* k-steps of weights ahead */, H = R / 4, CHUNK = R * 4 * CL_PIECE;
     __shared__ __attribute__((aligned(16))) char s_x[3 * CHUNK];
     __shared__ __attribute__((aligned(16))) float s_f[NW][128];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -764,12 +766,12 @@ cl_staged_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
     const int step_c = per_xcd / n_sb, step_s = per_xcd % n_sb; // from one of this workgroup's tiles to its next
     int ct = c_lo + j / n_sb, sb = j % n_sb;
 
-    // samples: this wavefront moves four of a chunk's 32 pieces, k-step `wave` of the four sample blocks
+    // samples: this wavefront moves 2 H of a chunk's 32 pieces, half of them at a time; piece 4 k + s is k-step k of sample block s
     int64_t r_left = left;
     int r_sb = sb, r_c = 0; // chunk that is requested next
     const auto request = [&](int i) __attribute__((always_inline)) {
-        const int blk = r_sb * 4 + i < xblocks ? r_sb * 4 + i : xblocks - 1;
-        const int k = (r_c < chunks - 1 ? r_c * R : kb - R) + wave;
+        const int bi = r_sb * 4 + ((wave * 2 * H + i) & 3), blk = bi < xblocks ? bi : xblocks - 1;
+        const int k = (r_c < chunks - 1 ? r_c * R : kb - R) + ((wave * 2 * H + i) >> 2);
         return *(const cl_i32x4 *)(xq + ((int64_t)blk * kb + k) * CL_PIECE + lane * 16);
     };
     const auto requested = [&]() __attribute__((always_inline)) { // behind the last tile: the same again, read by nobody
@@ -784,8 +786,9 @@ cl_staged_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
     };
     // chunk c: one that is short begins R before the end, with zeros for what the one before had
     const auto place = [&](cl_i32x4 v, int i, int c, char *to) __attribute__((always_inline)) {
-        if (c == chunks - 1 && kb - R + wave < c * R) v = cl_i32x4{0, 0, 0, 0};
-        *(cl_i32x4 *)(to + (wave * 4 + i) * CL_PIECE + lane * 16) = v;
+        const int id = wave * 2 * H + i;
+        if (c == chunks - 1 && kb - R + (id >> 2) < c * R) v = cl_i32x4{0, 0, 0, 0};
+        *(cl_i32x4 *)(to + id * CL_PIECE + lane * 16) = v;
     };
     const int block_bytes = kb * CL_PIECE;
     const auto weights = [&](int tile) __attribute__((always_inline)) { // of this wavefront's classes in a tile; beyond the last group: that one
@@ -793,18 +796,17 @@ cl_staged_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
         return wq + (int64_t)(g < groups ? g : groups - 1) * 2 * block_bytes;
     };
     char *b0 = s_x, *b1 = s_x + CHUNK, *b2 = s_x + 2 * CHUNK; // chunks t, t + 1, t + 2
-    cl_i32x4 held[4];
+    cl_i32x4 held[H];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) place(request(i), i, r_c, t ? b1 : b0);
+        for (int i = 0; i < 2 * H; ++i) place(request(i), i, r_c, t ? b1 : b0);
         requested();
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) held[i] = request(i);
+    for (int i = 0; i < H; ++i) held[i] = request(i);
     int p_c = r_c; // its chunk
-    requested();
-    cl_i32x4 w[RW][2], x[2][4];
+    cl_i32x4 w[RW][2], x[4];
     const int8_t *p = weights(ct);
 #pragma unroll
     for (int kk = 0; kk < RW; ++kk)
@@ -815,7 +817,7 @@ cl_staged_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
         }
     cl_barrier();
 #pragma unroll
-    for (int s = 0; s < 4; ++s) x[0][s] = *(const cl_i32x4 *)(b0 + s * CL_PIECE + lane * 16);
+    for (int s = 0; s < 4; ++s) x[s] = *(const cl_i32x4 *)(b0 + s * CL_PIECE + lane * 16);
     for (; left > 0; left -= per_xcd) {
         int next_ct = ct + step_c, next_sb = sb + step_s;
         if (next_sb >= n_sb) { next_sb -= n_sb; ++next_ct; }
@@ -834,24 +836,25 @@ cl_staged_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
             cl_barrier(); // chunk t + 1 is whole, and nobody reads chunk t - 1 any more
 #pragma unroll
             for (int kk = 0; kk < R; ++kk) {
+                if (kk == R / 2) requested();
 #pragma unroll
-                for (int s = 0; s < 4; ++s) x[kk + 1 & 1][s] = *(const cl_i32x4 *)((kk < R - 1 ? b0 + (kk + 1) * 4 * CL_PIECE : b1) + s * CL_PIECE + lane * 16);
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
+                for (int s = 0; s < 4; ++s) {
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) acc[s][q] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[kk & 1][s], w[kk % RW][q], acc[s][q], 0, 0, 0);
+                    for (int q = 0; q < 2; ++q) acc[s][q] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[s], w[kk % RW][q], acc[s][q], 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
-                    w[kk % RW][q] = *(const cl_i32x4 *)((kk < RW ? (q == 0 ? pc : pc1) : (q == 0 ? p : p1)) + kk % RW * CL_PIECE + lane * 16);
-                    if (kk == 1 || kk == 4) {
-                        const int i = kk == 1 ? q : 2 + q;
-                        place(held[i], i, p_c, b2);
-                        held[i] = request(i);
+                    x[s] = *(const cl_i32x4 *)((kk < R - 1 ? b0 + (kk + 1) * 4 * CL_PIECE : b1) + s * CL_PIECE + lane * 16);
+                    if (s == 3)
+#pragma unroll
+                        for (int q = 0; q < 2; ++q)
+                            w[kk % RW][q] = *(const cl_i32x4 *)(kk + RW < R ? (q == 0 ? pc : pc1) + kk * CL_PIECE + lane * 16 : (q == 0 ? p : p1) + (kk + RW - R) * CL_PIECE + lane * 16);
+                    if ((kk == 2 || kk == R / 2 + 2) && s < H) {
+                        place(held[s], (kk == 2 ? 0 : H) + s, p_c, b2);
+                        held[s] = request((kk == 2 ? H : 0) + s);
                     }
                 }
             }
             p_c = r_c;
-            requested();
             char *const b = b0;
             b0 = b1;
             b1 = b2;
