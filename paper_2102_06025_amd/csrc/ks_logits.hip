@@ -518,8 +518,8 @@ struct ClShare {
 #define CLX_NT 512
 // Batches of more than 64 samples, D <= 32 CLX_KB: a workgroup keeps the codes of 128 samples in LDS and its wavefronts, each on its own, go
 // over groups of 64 classes: 8 matrix instructions on 2 pieces of weights, which come straight from memory a chunk of R
-// k-steps ahead, also across the end of a group.  What bounds it are codes in and logits out (512 x 390,625 x 512 bf16: 119 us for 0.6 GB,
-// 152 with codes that no cache holds; 256: 68 and 95).
+// k-steps ahead, also across the end of a group.  What bounds it are codes in and logits out (512 x 390,625 x 512 fp32: 169 us for 1.0 GB,
+// 226 with codes that no cache holds; 256, bf16: 74 and 95).
 template <int R, typename OUT>
 __global__ void __launch_bounds__(CLX_NT, 2)
 cl_resident_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, const int8_t *__restrict__ wq,
@@ -888,11 +888,15 @@ static void cl_logits(const int8_t *xq, const float *xs, const int8_t *wq, const
     if (B <= 64 || waves <= 1280 || (waves <= 2048 && kb <= 8) || (kb < 4 && !vec))
         return waves <= 320 && kb >= 24 ? direct(cl_direct_kernel<2, 4, OUT>, 64, 1) : direct(cl_direct_kernel<2, 1, OUT>, 64, 4);
     // Registers hold 64 classes' codes while samples stream, or LDS holds samples while codes stream: the former is ahead for thin
-    // rows (390,625 x 64, batch 1,024: 162 us, 176) and for large products (x 512: 214, 229; 1,024 x 120,000 x 512: 75, 71), if
-    // the wavefronts' last round of groups is well filled.
+    // rows (390,625 x 64, batch 1,024: 162 us, 176) and for deep ones and more than one tile of samples (x 512, batch 1,024 bf16: 219,
+    // 235, and 260, 310 where no cache holds the codes, which it reads half as often; batch 256: 88, 80; fp32, more than two tiles: 512
+    // samples 181, 169), if the wavefronts' last round of groups is well filled.  In between it is behind by 5 %, but where bf16 logits
+    // leave codes as the larger part and the caches rarely hold them ahead by 16 % (390,625 x 256, batch 1,024: 175, 166, and 217, 259
+    // from memory; 200,000 x 256, from a cache: 94, 88).
     const int xblocks = (B + 31) / 32, tiles = (xblocks + 7) / 8, tile = ((xblocks + tiles - 1) / tiles + 1) / 2 * 2;
     const int64_t sets = 32 / (tiles < 8 ? tiles : 8) * 64, rounds = ks_ceil_div(groups, sets);
-    if (vec && (kb < 4 || ((kb == 4 || (kb > 8 && kb <= 16 && tiles >= 4)) && groups * 100 >= rounds * sets * 85)))
+    const bool thin_out = sizeof(OUT) == 2 && kb > 6 && groups * kb >= 32768; // 64 MB of codes
+    if (vec && (kb < 4 || ((kb == 4 || (tiles >= (sizeof(OUT) == 2 ? 2 : 3) && kb <= 16 && (kb > 8 || thin_out))) && groups * 100 >= rounds * sets * 85)))
         hipLaunchKernelGGL((kb <= 4 ? cl_steady_kernel<4, OUT> : kb <= 12 ? cl_steady_kernel<12, OUT> : cl_steady_kernel<16, OUT>), dim3(256), dim3(CLX_NT),
                            0, st, xq, xs, wq, ws, bias, C, kb, B, scale, out, ldl, tile);
     else if (kb <= CLX_KB)

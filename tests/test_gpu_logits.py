@@ -236,7 +236,7 @@ def test_logits_rows_that_lie_apart(ks, B, C, D, dtype, ld, shift):
     (300, 40_001, 64), (1_024, 30_000, 33), (257, 65_537, 128), (1_100, 32_700, 128), (1_024, 32_701, 352), (1_000, 32_001, 512), (900, 65_000, 400),
     (2_050, 16_130, 290), (1_024, 20_001, 512), (257, 30_011, 256), (129, 90_001, 160), (1_300, 9_999, 192), (700, 30_007, 768), (300, 40_000, 1_152),
     (600, 20_001, 1_184), (300, 33_000, 4_096), (129, 50_001, 2_500), (2_500, 5_001, 1_300), (64, 70_003, 512), (33, 90_001, 1_024), (20, 200_001, 96),
-    (32, 20_000, 800), (50, 16_000, 1_100)])
+    (32, 20_000, 800), (50, 16_000, 1_100), (400, 65_500, 320), (500, 65_535, 512), (257, 262_200, 256)])
 def test_products_of_many_classes(ks, B, C, D, dtype, apart):
     """Batches, layers and depths on both sides of the sizes at which the work is divided in another way; rows next to each other, and
     rows of an odd distance, with what lies between them."""
