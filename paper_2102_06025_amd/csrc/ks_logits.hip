@@ -8,9 +8,6 @@
 typedef int32_t cl_i32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t cl_i32x16 __attribute__((ext_vector_type(16)));
 
-#define CL_GPTR(p) ((const void __attribute__((address_space(1))) *)(p))
-#define CL_LPTR(p) ((void __attribute__((address_space(3))) *)(p))
-
 #define CL_NT 256
 #define CL_PIECE 1024 /* bytes of a piece: 32 rows x 32 codes, the operand of one 32x32x32 matrix instruction */
 #define CL_GROUP 64   /* classes whose two blocks of codes lie next to each other, every other class in each */
