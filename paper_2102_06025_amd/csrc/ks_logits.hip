@@ -321,12 +321,13 @@ __device__ __forceinline__ void cl_store1(__amdgpu_buffer_rsrc_t to, uint32_t of
 __device__ __forceinline__ void cl_store1(__amdgpu_buffer_rsrc_t to, uint32_t off, float v, const uint16_t *) {
     __builtin_amdgcn_raw_buffer_store_b16((uint16_t)ks_f2bf(v), to, off, 0, 0);
 }
-// Logits of 32 samples from m0 on by the 64 classes from c0 on as a buffer that ends with the last sample's row: what lies behind its
-// end (samples that do not exist, and classes: CL_NO_CLASS) the hardware leaves out, so that every row is one store on every
-// way.  32 rows are less than 2^31 bytes (cl_logits sees to that).
-template <typename OUT> __device__ __forceinline__ __amdgpu_buffer_rsrc_t cl_rows_of(OUT *out, int64_t ldl, int m0, int64_t c0, int B) {
-    const int rows = B - m0 < 32 ? B - m0 : 32;
-    return __builtin_amdgcn_make_buffer_rsrc(out + (int64_t)m0 * ldl + c0, 0, rows > 0 ? (int)((rows - 1) * (uint32_t)(ldl * sizeof(OUT)) + CL_GROUP * sizeof(OUT)) : 0, 0x00020000);
+// Logits of 32 samples from m0 on by the 64 classes from c0 on as a buffer that ends with the last class of the last sample: what lies
+// behind its end (samples that do not exist, and classes: CL_NO_CLASS) the hardware leaves out, so that every row is one store on
+// every way.  It ends with a whole pair, which is within the row since ldl is even here; so also where ldl < 64 the rows behind
+// the last sample, from rows * ldl on, lie behind the end.  32 rows are less than 2^31 bytes (cl_logits sees to both).
+template <typename OUT> __device__ __forceinline__ __amdgpu_buffer_rsrc_t cl_rows_of(OUT *out, int64_t ldl, int m0, int64_t c0, int64_t C, int B) {
+    const int rows = B - m0 < 32 ? B - m0 : 32, classes = C - c0 < CL_GROUP ? (int)(C - c0) + 1 & ~1 : CL_GROUP;
+    return __builtin_amdgcn_make_buffer_rsrc(out + (int64_t)m0 * ldl + c0, 0, rows > 0 ? (int)((rows - 1) * (uint32_t)(ldl * sizeof(OUT)) + classes * (uint32_t)sizeof(OUT)) : 0, 0x00020000);
 }
 #define CL_NO_CLASS 0x80000000u
 
@@ -360,7 +361,7 @@ __device__ __forceinline__ void cl_finish(const cl_i32x16 (&acc)[S][2], const fl
 #pragma unroll
                 for (int r4 = 0; r4 < 4; ++r4) f4[s + 1 & 1][r4] = *(const float4 *)(f + half4 + (s + 1) * 32 + r4 * 8);
             __builtin_amdgcn_sched_barrier(0);
-            const __amdgpu_buffer_rsrc_t to = cl_rows_of(out, ldl, m0 + s * 32, c0, B);
+            const __amdgpu_buffer_rsrc_t to = cl_rows_of(out, ldl, m0 + s * 32, c0, C, B);
             uint32_t off = off0;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -374,7 +375,7 @@ __device__ __forceinline__ void cl_finish(const cl_i32x16 (&acc)[S][2], const fl
         const uint32_t row_bytes = (uint32_t)(ldl * sizeof(OUT)), off0 = c + 1 == C ? half4 * row_bytes + 2 * (lane & 31) * (uint32_t)sizeof(OUT) : CL_NO_CLASS;
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-            const __amdgpu_buffer_rsrc_t to = cl_rows_of(out, ldl, m0 + s * 32, c0, B);
+            const __amdgpu_buffer_rsrc_t to = cl_rows_of(out, ldl, m0 + s * 32, c0, C, B);
             uint32_t off = off0;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -715,7 +716,7 @@ cl_steady_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
                     for (int r = 0; r < 16; ++r)
                         if (r * KB / 16 == k) finish(before, r, f);
                 }
-                to = cl_rows_of(out, ldl, (sb * tile + blk) * 32, c0, B);
+                to = cl_rows_of(out, ldl, (sb * tile + blk) * 32, c0, C, B);
                 off = off0;
 #pragma unroll
                 for (int q = 0; q < 2; ++q) { sw[q] = nsw[q]; b[q] = nb[q]; }

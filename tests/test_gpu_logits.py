@@ -265,6 +265,39 @@ def test_the_largest_sum(ks, B):
     near(ks.class_logits_int8(x, xs, y, ys, 1.0), *plain_logits(q, s, w, t, 1.0, None), torch.float32)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B", [1, 3, 31, 33, 65])
+@pytest.mark.parametrize("D", [33, 200, 800])
+def test_few_classes_in_tight_rows(ks, B, D, dtype):
+    """Rows of fewer than 64 classes next to each other: the rows behind the last sample are not the call's."""
+    for C in (1, 2, 9, 10, 31, 32, 40, 61, 62, 63, 64, 65, 70):
+        q, s, w, t, x, xs, y, ys, bias = product_case(ks, B, C, D, 3)
+        for ld in (C, C + 1, C + 2):
+            mat = torch.full((B + 70, ld), 77.0, dtype=dtype, device="cuda")
+            z = ks.class_logits_int8(x, xs, y, ys, 30.0, bias=torch.from_numpy(bias).cuda(), out=mat[:B, :C])
+            assert (mat[B:] == 77).all() and (mat[:, C:] == 77).all(), (C, ld)
+            near(z, *plain_logits(q, s, w, t, 30.0, bias), dtype, (C, ld))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,C,D,ld", [(131_100, 10, 64, 10), (131_075, 41, 33, 42), (82_000, 40, 512, 40), (81_985, 63, 300, 64), (82_010, 62, 1_200, 62),
+                                      (82_017, 9, 1_184, 10), (82_017, 9, 1_184, 9)])
+def test_few_classes_of_a_large_batch_in_tight_rows(ks, B, C, D, ld, dtype):
+    """The same for the kernels that large batches take."""
+    gen = torch.Generator("cuda").manual_seed(B + C + D)
+    rand = lambda *n: torch.rand(n, generator=gen, device="cuda")  # noqa: E731
+    q, w = (torch.randint(-127, 128, (n, D), generator=gen, device="cuda", dtype=torch.int8) for n in (B, C))
+    xs, ws, bias = 0.001 + 0.1 * rand(B), 0.001 + 0.1 * rand(C), 9 * rand(C) - 4.5
+    x, y = ks.class_quantize_rows(q)[0], ks.class_quantize_rows(w, classes=True)[0]
+    mat = torch.full((B + 300, ld), 77.0, dtype=dtype, device="cuda")
+    z = ks.class_logits_int8(x, xs, y, ws, 30.0, bias=bias, out=mat[:B, :C])
+    assert (mat[B:] == 77).all() and (mat[:, C:] == 77).all()
+    plain = torch.mm(q.double(), w.double().t().contiguous()) * (30.0 * xs.double())[:, None] * ws[None].double()
+    want = plain + bias[None].double()
+    off = (z.double() - want).abs() - 1.01 * (U32 * (4 * plain.abs() + want.abs()) + TYPES[dtype] * want.abs())
+    assert off.max() <= 0, float(off.max())
+
+
 def test_codes_and_logits_beyond_32_bits(ks):
     """Weights of more than 4 GB of codes, and rows of logits more than 2^31 elements apart."""
     D, C, B, ld = 4_352, 1_000_064, 3, 1_200_000_000
