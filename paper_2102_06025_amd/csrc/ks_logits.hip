@@ -1197,8 +1197,11 @@ __global__ void __launch_bounds__(1024) cl_long_kernel(ClAdjust a, int per_row, 
 #define CL_MAX_GRID (1 << 21) /* workgroups of a launch: threads are counted in 32 bits */
 // launch(a, rows) for stretches of rows from a.row0 on that fit into a launch, per_row workgroups each
 template <class F> static void cl_rows(ClAdjust a, int per_row, F launch) {
-    const int rows = per_row < CL_MAX_GRID ? CL_MAX_GRID / per_row : 1, B = a.B;
-    for (a.row0 = 0; a.row0 < B; a.row0 += rows) launch(a, rows < B - a.row0 ? rows : B - a.row0);
+    const int rows = per_row < CL_MAX_GRID ? CL_MAX_GRID / per_row : 1;
+    for (int64_t row0 = 0; row0 < a.B; row0 += rows) { // the row behind the last stretch may be no int
+        a.row0 = (int)row0;
+        launch(a, (int)(rows < a.B - row0 ? rows : a.B - row0));
+    }
 }
 
 template <typename T> static void cl_adjust(const ClAdjust &args, hipStream_t st) {

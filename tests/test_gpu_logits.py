@@ -475,6 +475,19 @@ def test_adjust_lists_far_shorter_than_the_array(ks):
         check_adjust(ks, r, B, 5_001, 0, 5_001, adjust_case(r, B, 5_001, 5_001, most, 9, True), torch.float32, True, 5_001)
 
 
+def test_adjust_the_largest_batch(ks):
+    """2^31 - 1 rows of one class: the row behind the last launch's rows is no 32-bit number."""
+    B = 2 ** 31 - 1
+    z, row = torch.zeros((B, 1), dtype=torch.bfloat16, device="cuda"), torch.full((B,), -1, dtype=torch.int32, device="cuda")
+    at = [0, 1, 2 ** 21 - 1, 2 ** 21, B - 2 ** 21, B - 2, B - 1]
+    row[at] = 0
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ks.class_logits_adjust(z, allowed=torch.zeros((1, 1), dtype=torch.int32, device="cuda"), mask_row=row, dev_status=status)
+    assert int(status) == 0 and z.flatten()[at].isneginf().all()
+    z.view(-1)[at] = 0
+    assert not z.any()
+
+
 def test_adjust_one_row_in_place_by_another_view(ks):
     z = torch.randn((1, 64), generator=torch.Generator().manual_seed(2)).cuda()
     want = z.clone()
