@@ -1261,7 +1261,7 @@ extern "C" int class_logits_adjust(const void *logits, int64_t ldl, void *out, i
                                    const float *frequency, const int64_t *bias_offsets, const int32_t *bias_ids,
                                    const float *bias_values, int64_t bias_len, int bias_max, const uint32_t *allowed,
                                    int64_t ld_allowed, int n_masks, const int32_t *mask_row, int32_t *dev_status, void *stream) {
-    if (!logits || !out || B < 1 || C < 1 || c0 < 0 || Cg >= (int64_t)1 << 31 || c0 + C > Cg || ldl < C || ldo < C) return KS_INVALID_ARG;
+    if (!logits || !out || B < 1 || C < 1 || c0 < 0 || Cg >= (int64_t)1 << 31 || C > Cg || c0 > Cg - C || ldl < C || ldo < C) return KS_INVALID_ARG;
     if (dtype != KS_DTYPE_BF16 && dtype != KS_DTYPE_FP32) return KS_INVALID_ARG;
     if (((uintptr_t)logits | (uintptr_t)out) % (dtype == KS_DTYPE_FP32 ? 4 : 2) || (logits == out && ldl != ldo && B > 1)) return KS_INVALID_ARG;
     if (seen_len < 0 || bias_len < 0 || seen_max < 0 || bias_max < 0 || (int64_t)seen_max + bias_max >= (int64_t)1 << 30) return KS_INVALID_ARG;

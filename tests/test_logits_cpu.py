@@ -78,3 +78,10 @@ def test_binding_refuses_host_tensors(ks):
         ks.class_logits_int8(torch.zeros(1024, dtype=torch.int8), torch.zeros(1), torch.zeros(4096, dtype=torch.int8), torch.zeros(1), 1.0)
     with pytest.raises(TypeError):
         ks.class_logits_adjust(torch.zeros(2, 8))
+
+
+def test_adjust_refuses_a_first_class_near_the_largest_number(ks):
+    L, p = ks.lib(), 256
+    for c0, Cg in (((1 << 63) - 1, 100), ((1 << 63) - 50, 100), (0, -(1 << 63)), (1 << 62, 1 << 30)):
+        assert L.class_logits_adjust(p, 100, p, 100, 1, 100, c0, Cg, 2, None, None, 0, 0, None, None, None, None, None, None, None, 0, 0, None, 4, 2,
+                                     None, None, None) == ks.KS_INVALID_ARG, (c0, Cg)
