@@ -40,7 +40,8 @@ extern "C" {
  *              Block b holds rows 32 b + r, with KS_QUANT_CLASSES rows 64 (b / 2) + 2 r + b % 2.  What lies beyond row n or
  *              element D is 0.
  * A zero row has codes 0 and scale 0.  A row that holds an infinity or a NaN has codes 0 and scale NaN: all its logits are NaN.
- * Requires n >= 1, 1 <= D <= KS_MAX_INT8_D (KS_UNSUPPORTED beyond); KS_QUANT_NORMALIZE not with KS_DTYPE_INT8.
+ * Requires 1 <= n < 2^31, 1 <= D <= KS_MAX_INT8_D (KS_UNSUPPORTED beyond); KS_QUANT_NORMALIZE not with KS_DTYPE_INT8.
+ * class_codes_bytes is 0 for sizes that are refused.
  * ---------------------------------------------------------------------------------------------------- */
 size_t class_codes_bytes(int64_t n, int D, uint32_t flags);
 int class_quantize_rows(const void *V, int dtype, int64_t n, int D, int64_t ldv, uint32_t flags, int8_t *codes, float *row_scale,

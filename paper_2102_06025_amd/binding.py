@@ -764,6 +764,7 @@ def grad_topk_select(g, plan: GradTopkPlan, out_idx=None, out_val=None, ws=None,
 QUANT_CLASSES, QUANT_NORMALIZE = 1, 2  # KS_QUANT_*
 _ROW_CODES = {torch.bfloat16: 0, torch.float32: 1, torch.int8: 2}
 _LOGIT_CODES, _WORD_CODES = {torch.bfloat16: 0, torch.float32: 1}, {torch.int32: 0}
+_MAX_INT8_D, _MAX_INT8_B, _INT_MAX = 65536, 4194240, (1 << 31) - 1  # KS_MAX_INT8_*; a C int takes the low 32 bits of what is passed for it
 
 
 def _at(t):
@@ -807,7 +808,8 @@ def _launch(dev, stream, call):
 
 
 def class_codes_bytes(n, D, classes=False) -> int:
-    return int(lib().class_codes_bytes(n, D, QUANT_CLASSES if classes else 0))
+    """Bytes of the codes of n rows of D elements, 0 for sizes that are refused."""
+    return int(lib().class_codes_bytes(n, D, QUANT_CLASSES if classes else 0)) if 0 < n <= _INT_MAX and 0 < D <= _MAX_INT8_D else 0
 
 
 def class_quantize_rows(V, classes=False, normalize=False, codes=None, row_scale=None, stream=None):
@@ -818,6 +820,8 @@ def class_quantize_rows(V, classes=False, normalize=False, codes=None, row_scale
     code, n, D, ldv = _rows(V, _ROW_CODES, "V")
     if code == 2 and (normalize or row_scale is not None):
         raise ValueError("int8 rows are taken as they are: no normalize, no row_scale")
+    if D > _MAX_INT8_D:
+        raise KsError("class_quantize_rows", KS_UNSUPPORTED)
     dev, flags = V.get_device(), (QUANT_CLASSES if classes else 0) | (QUANT_NORMALIZE if normalize else 0)
     need = L.class_codes_bytes(n, D, flags)
     if codes is not None:
@@ -846,6 +850,8 @@ def class_logits_int8(x_codes, x_scale, w_codes, w_scale, scale, bias=None, out=
         raise TypeError("x_codes must be a device tensor")
     if D % 32 or D < 32:
         raise ValueError("x_codes must hold the codes of B rows")
+    if D > _MAX_INT8_D or B > _MAX_INT8_B:
+        raise KsError("class_logits_int8", KS_UNSUPPORTED)
     _list(x_codes, torch.int8, (B + 31) // 32 * 32 * D, "x_codes (of B feature rows)", dev)
     _list(w_codes, torch.int8, (C + 63) // 64 * 64 * D, "w_codes (of C class rows of the features' depth)", dev)
     _list(x_scale, torch.float32, B, "x_scale", dev)
@@ -876,6 +882,8 @@ def class_logits_adjust(logits, seen=None, seen_max=None, n_prompt=None, repetit
     >= ceil(C / 32)] words of bits; mask_row int32 [B]; dev_status int32 [1], None: nothing is reported."""
     code, B, C, ldl = _rows(logits, _LOGIT_CODES, "logits")
     dev = logits.get_device()
+    if B > _INT_MAX:
+        raise ValueError("logits must have fewer than 2^31 rows")
     if out is None or out is logits:
         out, ldo = logits, ldl
     else:
@@ -913,13 +921,19 @@ def class_logits_adjust(logits, seen=None, seen_max=None, n_prompt=None, repetit
         _, n_masks, words, lda = _rows(allowed, _WORD_CODES, "allowed", dev)
         if words < (C + 31) // 32 or n_masks < 1 or (mask_row is None and n_masks < B):
             raise ValueError("allowed must be [n_masks, >= ceil(C / 32)], a mask per request without mask_row")
+    n_masks = min(n_masks, _INT_MAX)  # no mask_row names one beyond
+    s_max = s_len if seen_max is None or seen_max > s_len else seen_max
+    b_max = b_len if bias_max is None or bias_max > b_len else bias_max
+    if Cg is None:
+        Cg = c0 + C
+    if not (0 <= s_max <= _INT_MAX and 0 <= b_max <= _INT_MAX and 0 <= c0 <= Cg <= _INT_MAX):
+        raise KsError("class_logits_adjust", KS_INVALID_ARG)
 
     def call(raw):
         return lib().class_logits_adjust(
-            logits.data_ptr(), ldl, out.data_ptr(), ldo, code, C, c0, c0 + C if Cg is None else Cg, B, _at(s_off), _at(s_ids), s_len,
-            s_len if seen_max is None or seen_max > s_len else seen_max, _at(n_prompt), _at(repetition), _at(presence), _at(frequency),
-            _at(b_off), _at(b_ids), _at(b_val), b_len, b_len if bias_max is None or bias_max > b_len else bias_max, _at(allowed), lda, n_masks,
-            _at(mask_row), _at(dev_status), raw)
+            logits.data_ptr(), ldl, out.data_ptr(), ldo, code, C, c0, Cg, B, _at(s_off), _at(s_ids), s_len, s_max, _at(n_prompt), _at(repetition),
+            _at(presence), _at(frequency), _at(b_off), _at(b_ids), _at(b_val), b_len, b_max, _at(allowed), lda, n_masks, _at(mask_row),
+            _at(dev_status), raw)
 
     _check("class_logits_adjust", _launch(dev, stream, call))
     return out

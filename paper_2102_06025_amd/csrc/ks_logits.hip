@@ -245,7 +245,7 @@ cl_quantize_kernel(const IN *__restrict__ V, int64_t n, int D, int64_t ldv, uint
 }
 
 extern "C" size_t class_codes_bytes(int64_t n, int D, uint32_t flags) {
-    if (n < 1 || D < 1 || D > KS_MAX_INT8_D) return 0;
+    if (n < 1 || n >= (int64_t)1 << 31 || D < 1 || D > KS_MAX_INT8_D) return 0;
     const int64_t rows = flags & KS_QUANT_CLASSES ? ks_ceil_div(n, CL_GROUP) * CL_GROUP : ks_ceil_div(n, 32) * 32;
     return (size_t)rows * ((D + 31) / 32 * 32);
 }

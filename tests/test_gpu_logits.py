@@ -583,6 +583,32 @@ def test_binding_refuses(ks):
         ks.class_logits_adjust(z, c0=1, Cg=40, allowed=m)
 
 
+def test_binding_refuses_sizes_beyond_a_c_int(ks):
+    """What is passed for a C int is taken by its low 32 bits: such sizes are refused before.  Nothing here is ever read."""
+    new = lambda *n, dtype=torch.int8: torch.empty(n, dtype=dtype, device="cuda")  # noqa: E731
+    for D in (65_537, 2 ** 32 + 8):
+        with pytest.raises(ks.KsError) as e:
+            ks.class_quantize_rows(new(1, D))
+        assert e.value.code == ks.KS_UNSUPPORTED
+    B = 4_194_241
+    with pytest.raises(ks.KsError) as e:
+        ks.class_logits_int8(new((B + 31) // 32 * 1024), new(B, dtype=torch.float32), new(64 * 32), new(1, dtype=torch.float32), 1.0)
+    assert e.value.code == ks.KS_UNSUPPORTED
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        ks.class_logits_adjust(new(2 ** 32 + 1, 1, dtype=torch.bfloat16), allowed=new(1, 1, dtype=torch.int32), dev_status=status)
+    z, none = torch.ones((2, 40), device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda")
+    few, many = torch.zeros(9, dtype=torch.int32, device="cuda"), new(2 ** 32 + 5, dtype=torch.int32)
+    for bad in (dict(seen=(few, none), seen_max=5 - 2 ** 32), dict(seen=(many, none)), dict(seen=(many, none), seen_max=2 ** 32 + 2),
+                dict(bias=(few, few.float(), none), bias_max=5 - 2 ** 32), dict(seen=(few, none), c0=2 ** 64), dict(seen=(few, none), Cg=2 ** 64 + 40),
+                dict(seen=(few, none), c0=-2 ** 64)):
+        with pytest.raises(ks.KsError) as e:
+            ks.class_logits_adjust(z, presence=torch.ones(2, device="cuda"), dev_status=status, **bad)
+        assert e.value.code == ks.KS_INVALID_ARG
+    ks.class_logits_adjust(z, seen=(many, none), seen_max=5, presence=torch.ones(2, device="cuda"), dev_status=status)  # short lists of a large array
+    assert int(status) == 0 and (z == 1).all()
+
+
 # ---------------------------------------------------------------------------------------------------- together
 def answer(ks, X, W8, ws, bias, adjust, stream=None, **args):
     x, xs = ks.class_quantize_rows(X, stream=stream)

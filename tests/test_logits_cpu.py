@@ -85,3 +85,9 @@ def test_adjust_refuses_a_first_class_near_the_largest_number(ks):
     for c0, Cg in (((1 << 63) - 1, 100), ((1 << 63) - 50, 100), (0, -(1 << 63)), (1 << 62, 1 << 30)):
         assert L.class_logits_adjust(p, 100, p, 100, 1, 100, c0, Cg, 2, None, None, 0, 0, None, None, None, None, None, None, None, 0, 0, None, 4, 2,
                                      None, None, None) == ks.KS_INVALID_ARG, (c0, Cg)
+
+
+def test_bytes_of_sizes_beyond_a_c_int(ks):
+    """Sizes that no call takes have no codes, not the codes of their low 32 bits."""
+    assert [ks.class_codes_bytes(*a) for a in ((8, (1 << 32) + 8), (8, 8 - (1 << 32)), (1 << 31, 8), (1 << 62, 65_536), ((1 << 64) + 8, 8))] == [0] * 5
+    assert ks.class_codes_bytes((1 << 31) - 1, 8) == (1 << 31) * 32
