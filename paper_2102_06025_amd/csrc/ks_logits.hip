@@ -1038,8 +1038,14 @@ __device__ __forceinline__ void cl_mask_part(const ClAdjust &a, int b, int part)
 }
 
 template <typename T, bool COPY, bool VEC, bool RMW>
-__global__ void __launch_bounds__(CL_NT) cl_mask_kernel(ClAdjust a, int per_row) {
-    cl_mask_part<T, COPY, VEC, RMW, CL_NT>(a, a.row0 + blockIdx.x / per_row, blockIdx.x % per_row);
+__global__ void __launch_bounds__(CL_NT) cl_mask_kernel(ClAdjust a, int per_row, int check) { // check: lists that may hold nothing are looked at here
+    const int b = a.row0 + blockIdx.x / per_row, part = blockIdx.x % per_row;
+    if (check && part == 0) {
+        int64_t first;
+        cl_list(a.seen_offsets, a.seen_len, a.seen_max, b, &first, a.dev_status);
+        cl_list(a.bias_offsets, a.bias_len, a.bias_max, b, &first, a.dev_status);
+    }
+    cl_mask_part<T, COPY, VEC, RMW, CL_NT>(a, b, part);
 }
 
 // Lists of a request that a hash table of SLOTS classes in LDS holds (two thirds of the slots): each of them counts the class's occurrences
@@ -1217,18 +1223,20 @@ template <typename T> static void cl_adjust(const ClAdjust &args, hipStream_t st
     // (2,048 x 1,000 with long lists: 38, 28)
     const bool whole = copy && entries > 0 && entries <= CLH_ENTRIES(CLH_MID) && args.B <= 256 && ks_ceil_div(args.C, (int64_t)CLM_U(true) * 1024 * E) <= 3;
     const bool fused = !copy && args.allowed && !rmw && entries > 0 && entries <= CLH_ENTRIES(CLH_MID);
+    // lists that may hold nothing change no logit, but one that holds something is reported
+    const int check = entries == 0 && args.dev_status && (args.seen_offsets || args.bias_offsets);
     if ((copy || args.allowed) && !fused && !whole) {
         const int per_row = (int)ks_ceil_div(args.C, (int64_t)CLM_U(copy) * CL_NT * E);
         cl_rows(args, per_row, [&](const ClAdjust &a, int rows) {
             const dim3 grid((unsigned)per_row * (unsigned)rows);
-            if (copy && vec) hipLaunchKernelGGL((cl_mask_kernel<T, true, true, false>), grid, dim3(CL_NT), 0, st, a, per_row);
-            else if (copy) hipLaunchKernelGGL((cl_mask_kernel<T, true, false, false>), grid, dim3(CL_NT), 0, st, a, per_row);
-            else if (sizeof(T) == 2 && rmw) hipLaunchKernelGGL((cl_mask_kernel<T, false, true, sizeof(T) == 2>), grid, dim3(CL_NT), 0, st, a, per_row);
-            else if (vec) hipLaunchKernelGGL((cl_mask_kernel<T, false, true, false>), grid, dim3(CL_NT), 0, st, a, per_row);
-            else hipLaunchKernelGGL((cl_mask_kernel<T, false, false, false>), grid, dim3(CL_NT), 0, st, a, per_row);
+            if (copy && vec) hipLaunchKernelGGL((cl_mask_kernel<T, true, true, false>), grid, dim3(CL_NT), 0, st, a, per_row, check);
+            else if (copy) hipLaunchKernelGGL((cl_mask_kernel<T, true, false, false>), grid, dim3(CL_NT), 0, st, a, per_row, check);
+            else if (sizeof(T) == 2 && rmw) hipLaunchKernelGGL((cl_mask_kernel<T, false, true, sizeof(T) == 2>), grid, dim3(CL_NT), 0, st, a, per_row, check);
+            else if (vec) hipLaunchKernelGGL((cl_mask_kernel<T, false, true, false>), grid, dim3(CL_NT), 0, st, a, per_row, check);
+            else hipLaunchKernelGGL((cl_mask_kernel<T, false, false, false>), grid, dim3(CL_NT), 0, st, a, per_row, check);
         });
     }
-    if (entries == 0) return;
+    if (entries == 0 && (!check || copy || args.allowed)) return;
     const auto hash = [&](auto kernel, int nt) {
         const int per_row = fused || whole ? (int)ks_ceil_div(args.C, (int64_t)CLM_U(whole) * nt * E) : 0;
         cl_rows(args, fused ? 1 + per_row : 1, [&](const ClAdjust &a, int rows) {
@@ -1268,7 +1276,8 @@ extern "C" int class_logits_adjust(const void *logits, int64_t ldl, void *out, i
     if (seen_offsets && seen_len && !seen_ids) return KS_INVALID_ARG;
     if (bias_offsets && bias_len && (!bias_ids || !bias_values)) return KS_INVALID_ARG;
     if (allowed && (ld_allowed < (C + 31) / 32 || n_masks < 1 || (!mask_row && n_masks < B))) return KS_INVALID_ARG;
-    if (logits == out && !allowed && !(seen_offsets && seen_max) && !(bias_offsets && bias_max)) return KS_OK; // nothing changes
+    const auto lists = [&](const int64_t *offsets, int most) { return offsets && (most || dev_status); };
+    if (logits == out && !allowed && !lists(seen_offsets, seen_max) && !lists(bias_offsets, bias_max)) return KS_OK; // nothing changes or is reported
     const ClAdjust a = {logits, out, ldl, ldo, C, c0, Cg, seen_offsets, bias_offsets, seen_ids, bias_ids, n_prompt, mask_row, bias_values,
                         repetition, presence, frequency, allowed, seen_len, bias_len, ld_allowed, B, seen_max, bias_max, n_masks, 0, dev_status};
     if (dtype == KS_DTYPE_FP32) cl_adjust<float>(a, (hipStream_t)stream);

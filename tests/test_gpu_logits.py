@@ -553,6 +553,27 @@ def test_adjust_reports_what_it_cannot_use(ks):
             assert int(status) == bit, (args, int(status))
 
 
+@pytest.mark.parametrize("B,C,dtype", [(3, 64, torch.float32), (3, 6_000_000, torch.bfloat16), (3, 100_001, torch.float32), (300, 1_000, torch.bfloat16)])
+def test_adjust_reports_lists_where_none_may_hold_anything(ks, B, C, dtype):
+    z0 = torch.randn((B, C), generator=torch.Generator("cuda").manual_seed(4), device="cuda").to(dtype)
+    off = torch.zeros(B + 1, dtype=torch.int64, device="cuda")
+    full = off.clone()
+    full[2:] = 5  # the second request's list
+    ids, words = torch.zeros(5, dtype=torch.int32, device="cuda"), torch.full((1, (C + 31) // 32), -2, dtype=torch.int32, device="cuda")
+    none, masked = ids[:0], z0.clone()
+    masked[:, ::32] = -INF
+    masks = dict(allowed=words, mask_row=torch.zeros(B, dtype=torch.int32, device="cuda"))
+    for lists in (lambda o: dict(seen=(none, o)), lambda o: dict(bias=(none, none.float(), o)), lambda o: dict(seen=(ids, o), seen_max=0),
+                  lambda o: dict(bias=(ids, ids.float(), o), bias_max=0), lambda o: dict(seen=(none, off), bias=(none, none.float(), o))):
+        for args, want in (({}, z0), (masks, masked)):
+            for offsets, bit in ((off, 0), (full, ks.KS_DEV_BAD_COUNT)):
+                for out in (None, torch.empty_like(z0)):
+                    z, status = z0.clone(), torch.zeros(1, dtype=torch.int32, device="cuda")
+                    got = ks.class_logits_adjust(z, out=out, dev_status=status, **lists(offsets), **args)
+                    assert torch.equal(got, want) and int(status) == bit
+                    assert torch.equal(ks.class_logits_adjust(z0.clone(), **lists(offsets), **args), want)
+
+
 def test_binding_refuses(ks):
     V = torch.ones((4, 8), device="cuda")
     with pytest.raises(TypeError):
