@@ -258,6 +258,45 @@ def test_products_of_many_classes(ks, B, C, D, dtype, apart):
         assert off.max() <= 0, (lo, float(off.max()))
 
 
+@pytest.mark.parametrize("C,B,D", [(64, 81_920, 512), (1_000, 5_120, 512), (64, 131_072, 128), (500, 10_240, 1_024)])
+def test_large_batches_of_few_classes_fill_the_chip(ks, C, B, D):
+    """Twice the batch, on the other side of the batch sizes that go to other kernels where there are many classes: about twice the time
+    (with the chip left nearly empty it was ten to eighty times)."""
+    def least(n):
+        x, xs = torch.zeros(ks.class_codes_bytes(n, D), dtype=torch.int8, device="cuda"), torch.ones(n, device="cuda")
+        w, ws = torch.zeros(ks.class_codes_bytes(C, D, True), dtype=torch.int8, device="cuda"), torch.ones(C, device="cuda")
+        z, times = torch.empty((n, (C + 63) // 64 * 64), device="cuda")[:, :C], []
+        for _ in range(4):
+            ends = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+            torch.cuda.synchronize()
+            ends[0].record()
+            for _ in range(10):
+                ks.class_logits_int8(x, xs, w, ws, 1.0, out=z)
+            ends[1].record()
+            torch.cuda.synchronize()
+            times.append(ends[0].elapsed_time(ends[1]))
+        return min(times)
+    assert least(2 * B) < 5 * least(B)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,C,D", [(4_500, 8_191, 64), (1_500, 8_257, 320), (700, 8_192, 1_152), (3_000, 2_048, 1_184), (3_000, 2_049, 1_200), (7_000, 1_999, 31)])
+def test_products_on_both_sides_of_few_classes(ks, B, C, D, dtype):
+    gen = torch.Generator("cuda").manual_seed(B + C + D)
+    rand = lambda *n: torch.rand(n, generator=gen, device="cuda")  # noqa: E731
+    q, w = (torch.randint(-127, 128, (n, D), generator=gen, device="cuda", dtype=torch.int8) for n in (B, C))
+    xs, ws, bias = 0.001 + 0.1 * rand(B), 0.001 + 0.1 * rand(C), 9 * rand(C) - 4.5
+    x, y = ks.class_quantize_rows(q)[0], ks.class_quantize_rows(w, classes=True)[0]
+    plain = torch.mm(q.double(), w.double().t().contiguous()) * (30.0 * xs.double())[:, None] * ws[None].double()
+    want = plain + bias[None].double()
+    for ld in (C, C + 1):
+        mat = torch.full((B + 9, ld), 77.0, dtype=dtype, device="cuda")
+        z = ks.class_logits_int8(x, xs, y, ws, 30.0, bias=bias, out=mat[:B, :C])
+        assert (mat[B:] == 77).all() and (mat[:, C:] == 77).all()
+        off = (z.double() - want).abs() - 1.01 * (U32 * (4 * plain.abs() + want.abs()) + TYPES[dtype] * want.abs())
+        assert off.max() <= 0, (ld, float(off.max()))
+
+
 @pytest.mark.parametrize("B", [1, 40, 200])
 def test_the_largest_sum(ks, B):
     """-128 everywhere at the largest depth: 2^14 * 2^16 = 2^30."""
