@@ -1042,10 +1042,11 @@ __device__ __forceinline__ void cl_mask_part(const ClAdjust &a, int b, int part)
     }
 }
 
-template <typename T, bool COPY, bool VEC, bool RMW>
-__global__ void __launch_bounds__(CL_NT) cl_mask_kernel(ClAdjust a, int per_row, int check) { // check: lists that may hold nothing are looked at here
+// CHECK: lists that may hold nothing are looked at here (an instance of its own: 256 x 390,625 bf16 1 us longer with the question in all)
+template <typename T, bool CHECK, bool COPY, bool VEC, bool RMW>
+__global__ void __launch_bounds__(CL_NT) cl_mask_kernel(ClAdjust a, int per_row) {
     const int b = a.row0 + blockIdx.x / per_row, part = blockIdx.x % per_row;
-    if (check && part == 0) {
+    if (CHECK && part == 0) {
         int64_t first;
         cl_list(a.seen_offsets, a.seen_len, a.seen_max, b, &first, a.dev_status);
         cl_list(a.bias_offsets, a.bias_len, a.bias_max, b, &first, a.dev_status);
@@ -1229,16 +1230,18 @@ template <typename T> static void cl_adjust(const ClAdjust &args, hipStream_t st
     const bool whole = copy && entries > 0 && entries <= CLH_ENTRIES(CLH_MID) && args.B <= 256 && ks_ceil_div(args.C, (int64_t)CLM_U(true) * 1024 * E) <= 3;
     const bool fused = !copy && args.allowed && !rmw && entries > 0 && entries <= CLH_ENTRIES(CLH_MID);
     // lists that may hold nothing change no logit, but one that holds something is reported
-    const int check = entries == 0 && args.dev_status && (args.seen_offsets || args.bias_offsets);
+    const bool check = entries == 0 && args.dev_status && (args.seen_offsets || args.bias_offsets);
     if ((copy || args.allowed) && !fused && !whole) {
         const int per_row = (int)ks_ceil_div(args.C, (int64_t)CLM_U(copy) * CL_NT * E);
         cl_rows(args, per_row, [&](const ClAdjust &a, int rows) {
-            const dim3 grid((unsigned)per_row * (unsigned)rows);
-            if (copy && vec) hipLaunchKernelGGL((cl_mask_kernel<T, true, true, false>), grid, dim3(CL_NT), 0, st, a, per_row, check);
-            else if (copy) hipLaunchKernelGGL((cl_mask_kernel<T, true, false, false>), grid, dim3(CL_NT), 0, st, a, per_row, check);
-            else if (sizeof(T) == 2 && rmw) hipLaunchKernelGGL((cl_mask_kernel<T, false, true, sizeof(T) == 2>), grid, dim3(CL_NT), 0, st, a, per_row, check);
-            else if (vec) hipLaunchKernelGGL((cl_mask_kernel<T, false, true, false>), grid, dim3(CL_NT), 0, st, a, per_row, check);
-            else hipLaunchKernelGGL((cl_mask_kernel<T, false, false, false>), grid, dim3(CL_NT), 0, st, a, per_row, check);
+            const auto masks = [&](auto checking, auto plain) {
+                hipLaunchKernelGGL((check ? checking : plain), dim3((unsigned)per_row * (unsigned)rows), dim3(CL_NT), 0, st, a, per_row);
+            };
+            if (copy && vec) masks(cl_mask_kernel<T, true, true, true, false>, cl_mask_kernel<T, false, true, true, false>);
+            else if (copy) masks(cl_mask_kernel<T, true, true, false, false>, cl_mask_kernel<T, false, true, false, false>);
+            else if (sizeof(T) == 2 && rmw) masks(cl_mask_kernel<T, true, false, true, sizeof(T) == 2>, cl_mask_kernel<T, false, false, true, sizeof(T) == 2>);
+            else if (vec) masks(cl_mask_kernel<T, true, false, true, false>, cl_mask_kernel<T, false, false, true, false>);
+            else masks(cl_mask_kernel<T, true, false, false, false>, cl_mask_kernel<T, false, false, false, false>);
         });
     }
     if (entries == 0 && (!check || copy || args.allowed)) return;
