@@ -23,7 +23,7 @@ extern "C" {
 #define KS_QUANT_CLASSES 1u   /* the rows are class weights: codes in the order of the product's class side */
 #define KS_QUANT_NORMALIZE 2u /* scales of the L2-normalised rows: row_scale is divided by the row's norm */
 
-#define KS_MAX_INT8_D 65536   /* largest depth: the integer sums stay below 2^30 */
+#define KS_MAX_INT8_D 65536   /* largest depth: the integer sums are at most 2^30 */
 #define KS_MAX_INT8_B 4194240 /* largest batch of one class_logits_int8 call */
 
 /* ------------------------------------------------------------------------------------------------------
@@ -39,7 +39,7 @@ extern "C" {
  *              (h * 32 + r) * 16 + j  is the code of element 32 p + 16 h + j of the block's row r (h = 0, 1; j = 0 .. 15).
  *              Block b holds rows 32 b + r, with KS_QUANT_CLASSES rows 64 (b / 2) + 2 r + b % 2.  What lies beyond row n or
  *              element D is 0.
- * A zero row has codes 0 and scale 0.  A row that holds an infinity or a NaN has codes 0 and scale NaN: all its logits are NaN.
+ * The codes must not overlap V.  A zero row has codes 0 and scale 0.  A row that holds an infinity or a NaN has codes 0 and scale NaN: all its logits are NaN.
  * Requires 1 <= n < 2^31, 1 <= D <= KS_MAX_INT8_D (KS_UNSUPPORTED beyond); KS_QUANT_NORMALIZE not with KS_DTYPE_INT8.
  * class_codes_bytes is 0 for sizes that are refused.
  * ---------------------------------------------------------------------------------------------------- */
@@ -51,14 +51,15 @@ int class_quantize_rows(const void *V, int dtype, int64_t n, int D, int64_t ldv,
  * class_logits_int8 -- the fc forward of Section 3.2 over all classes of the shard, in 8-bit integers:
  *     logits[i, c] = scale * x_scale[i] * w_scale[c] * sum_d qx[i, d] qw[c, d]  (+ bias[c])
  * The sum is exact; it is converted to fp32, multiplied by fp32(scale * x_scale[i]) and by w_scale[c], the bias added, in fp32
- * (at most five roundings of 2^-24), and rounded to the type of the logits.
+ * (at most five roundings of 2^-24 while these stay within fp32's normal range), and rounded to the type of the logits.
  *
  *   x_codes  codes of the features [B, D] (class_quantize_rows without KS_QUANT_CLASSES), x_scale [B]
  *   w_codes  codes of the class weights [C, D] (with KS_QUANT_CLASSES), w_scale [C]
  *   bias     [C] fp32, may be NULL
  *   logits   [B, C] out, dtype KS_DTYPE_FP32 or KS_DTYPE_BF16; row i begins at element i * ldl (ldl >= C; elements between C and ldl
  *            are not touched, so that a node of a sharded layer may write its columns of a larger matrix).  Aligned to its
- *            elements is enough; rows that begin on whole 128-byte lines are written fastest, an odd ldl slowest
+ *            elements is enough; rows that begin on whole 128-byte lines are written fastest.  With batches of more than 64 others
+ *            take up to two and a half times as long (1,024 x 390,625 x 512 bf16: 260 us, ldl = 390,626 680, ldl = 390,625 490)
  * Requires 1 <= B <= KS_MAX_INT8_B, 1 <= C < 2^31, 1 <= D <= KS_MAX_INT8_D (KS_UNSUPPORTED beyond the maxima).
  * ---------------------------------------------------------------------------------------------------- */
 int class_logits_int8(const int8_t *x_codes, const float *x_scale, const int8_t *w_codes, const float *w_scale, const float *bias,
@@ -84,8 +85,8 @@ int class_logits_int8(const int8_t *x_codes, const float *x_scale, const int8_t 
  *                    not read
  *   n_prompt [B]     entries of the list that count for `repetition` alone (clamped to the list); NULL: none
  *   repetition, presence, frequency [B]         fp32; NULL: no such penalty.  repetition > 0 (1: no effect)
- *   bias_offsets [B + 1], bias_ids, bias_values [bias_len], bias_max   lists of single classes' biases, likewise; of a class that is
- *                    named twice the later entry counts
+ *   bias_offsets [B + 1], bias_ids, bias_values [bias_len], bias_max   lists of single classes' biases, likewise, but that ids >= Cg
+ *                    set KS_DEV_BAD_INDEX; of a class that is named twice the later entry counts
  *   allowed [n_masks, ld_allowed] uint32        masks: bit c % 32 of word c / 32 set: column c (class c0 + c) is allowed;
  *                    ld_allowed >= ceil(C / 32); bits beyond C are ignored.  NULL: no masks
  *   mask_row [B]     mask of request i, negative: everything is allowed; an index >= n_masks sets KS_DEV_BAD_INDEX and counts as
