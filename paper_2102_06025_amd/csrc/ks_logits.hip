@@ -517,7 +517,9 @@ struct ClShare {
 // Batches of more than 64 samples, D <= 32 CLX_KB: a workgroup keeps the codes of 128 samples in LDS and its wavefronts, each on its own, go
 // over groups of 64 classes: 8 matrix instructions on 2 pieces of weights, which come straight from memory a chunk of R
 // k-steps ahead, also across the end of a group.  What bounds it are codes in and logits out (512 x 390,625 x 512 fp32: 169 us for 1.0 GB,
-// 226 with codes that no cache holds; 256, bf16: 74 and 95).
+// 226 with codes that no cache holds; 256, bf16: 74 and 95), of deep rows and large batches the codes, read again for every tile of 128
+// samples, and the products (codes that no cache holds: 256 x 390,625 x 768 bf16 115 us, x 1,152 152; 1,024 samples 373 and 467, which
+// is 1.6 and 2.0 POP/s; fp32 525 and 615).  Where a wavefront has no group of its own, it is idle: 77 x 50,021 x 333, 782 groups for 2,048 wavefronts, 10.3 us.
 template <int R, typename OUT>
 __global__ void __launch_bounds__(CLX_NT, 2)
 cl_resident_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, const int8_t *__restrict__ wq,
@@ -738,7 +740,7 @@ cl_steady_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
 
 // Deeper rows: as in cl_resident_kernel, but the samples pass through LDS in chunks of eight k-steps, which eight wavefronts with 64
 // classes each read at the same time: three buffers, a barrier a chunk.  2,048 x 131,072 x 4,096: 1,043 us = 2.11 POP/s, the matrix
-// pipes 56 % busy at 1.9 GHz (codes of 0, which cost little power: 907).  What holds them up is the operands' way into the registers, for 64
+// pipes 56 % busy at 1.9 GHz (codes of 0, which cost little power: 907; a bare loop of the instruction over random codes: 2.7 to 2.9 POP/s, 785 us).  What holds them up is the operands' way into the registers, for 64
 // instructions 32 KB from LDS and 20 KB through the caches: neither weights six k-steps ahead (1,054) nor 256 classes by 256 samples, which
 // need 16 KB of the L2 instead of 20 (1,110), nor both sides in LDS and one wavefront a SIMD (1,118) were faster.
 // While chunk t is multiplied, a fragment is read for the next k-step when it has been used (the last ones from chunk t + 1, which is
@@ -876,6 +878,9 @@ static void cl_logits(const int8_t *xq, const float *xs, const int8_t *wq, const
         hipLaunchKernelGGL(kernel, dim3((unsigned)ks_ceil_div(groups, per_workgroup), (unsigned)ks_ceil_div(B, samples)), dim3(CL_NT), 0, st, xq, xs,
                            wq, ws, bias, C, kb, B, scale, out, ldl, vec);
     };
+    // vec: pairs of classes in one store; 64 MB from row to row and more, whose offsets are no 32 bits, go element by element (8 x 390,625 x 512 bf16:
+    // 42 us, 41 with rows next to each other).  Pairs in rows that begin beside the 128-byte lines: 1,024 x 390,625 x 512 bf16 680 us, elements
+    // 490, on the lines 260.
     // Few samples: the codes of the weights are what moves, and every wavefront reads its own.  Few wavefronts in all (a kernel of
     // 256 workgroups that keep the samples would leave most idle: 10,000 x 512, batch 256: 5.9 us, 8.0 in 128-sample tiles; 50,000
     // x 512, 128: 11.3 and 9.3; x 256: 6.8 and 8.4): the same for any batch.  Where they are deep, four wavefronts divide each group's depth (10,000 x
