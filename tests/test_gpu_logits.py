@@ -279,6 +279,19 @@ def test_large_batches_of_few_classes_fill_the_chip(ks, C, B, D):
     assert least(2 * B) < 5 * least(B)
 
 
+@pytest.mark.parametrize("C,ld", [(3, 3), (10, 10), (9, 10)])
+def test_product_of_the_largest_batch(ks, C, ld):
+    B, D = 4_194_240, 20
+    gen = torch.Generator("cuda").manual_seed(C)
+    q, w = (torch.randint(-127, 128, (n, D), generator=gen, device="cuda", dtype=torch.int8) for n in (B, C))
+    xs, ws = (0.001 + 0.1 * torch.rand(n, generator=gen, device="cuda") for n in (B, C))
+    mat = torch.full((B + 70, ld), 77.0, device="cuda")
+    z = ks.class_logits_int8(ks.class_quantize_rows(q)[0], xs, ks.class_quantize_rows(w, classes=True)[0], ws, 2.0, out=mat[:B, :C])
+    assert (mat[B:] == 77).all() and (mat[:, C:] == 77).all()
+    want = torch.mm(q.double(), w.double().t().contiguous()) * (2.0 * xs.double())[:, None] * ws[None].double()
+    assert ((z.double() - want).abs() <= 4.1 * U32 * want.abs()).all()
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("B,C,D", [(4_500, 8_191, 64), (1_500, 8_257, 320), (700, 8_192, 1_152), (3_000, 2_048, 1_184), (3_000, 2_049, 1_200), (7_000, 1_999, 31)])
 def test_products_on_both_sides_of_few_classes(ks, B, C, D, dtype):
