@@ -39,7 +39,8 @@ extern "C" {
  *              (h * 32 + r) * 16 + j  is the code of element 32 p + 16 h + j of the block's row r (h = 0, 1; j = 0 .. 15).
  *              Block b holds rows 32 b + r, with KS_QUANT_CLASSES rows 64 (b / 2) + 2 r + b % 2.  What lies beyond row n or
  *              element D is 0.
- * The codes must not overlap V.  A zero row has codes 0 and scale 0.  A row that holds an infinity or a NaN has codes 0 and scale NaN: all its logits are NaN.
+ * The codes must not overlap V.  A zero row has codes 0 and scale 0.  A row that holds an infinity or a NaN has codes 0 and scale NaN:
+ * all its logits are NaN.
  * Requires 1 <= n < 2^31, 1 <= D <= KS_MAX_INT8_D (KS_UNSUPPORTED beyond); KS_QUANT_NORMALIZE not with KS_DTYPE_INT8.
  * class_codes_bytes is 0 for sizes that are refused.
  * ---------------------------------------------------------------------------------------------------- */

@@ -519,7 +519,7 @@ struct ClShare {
 // k-steps ahead, also across the end of a group.  What bounds it are codes in and logits out (512 x 390,625 x 512 fp32: 169 us for 1.0 GB,
 // 226 with codes that no cache holds; 256, bf16: 74 and 95), of deep rows and large batches the codes, read again for every tile of 128
 // samples, and the products (codes that no cache holds: 256 x 390,625 x 768 bf16 115 us, x 1,152 152; 1,024 samples 373 and 467, which
-// is 1.6 and 2.0 POP/s; fp32 525 and 615).  Where a wavefront has no group of its own, it is idle: 77 x 50,021 x 333, 782 groups for 2,048 wavefronts, 10.3 us.
+// is 1.6 and 2.0 POP/s; fp32 525 and 615).  A wavefront that gets no group is idle: 77 x 50,021 x 333, 782 groups for 2,048 of them, 10.3 us.
 template <int R, typename OUT>
 __global__ void __launch_bounds__(CLX_NT, 2)
 cl_resident_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, const int8_t *__restrict__ wq,
@@ -740,9 +740,10 @@ cl_steady_kernel(const int8_t *__restrict__ xq, const float *__restrict__ xs, co
 
 // Deeper rows: as in cl_resident_kernel, but the samples pass through LDS in chunks of eight k-steps, which eight wavefronts with 64
 // classes each read at the same time: three buffers, a barrier a chunk.  2,048 x 131,072 x 4,096: 1,043 us = 2.11 POP/s, the matrix
-// pipes 56 % busy at 1.9 GHz (codes of 0, which cost little power: 907; a bare loop of the instruction over random codes: 2.7 to 2.9 POP/s, 785 us).  What holds them up is the operands' way into the registers, for 64
-// instructions 32 KB from LDS and 20 KB through the caches: neither weights six k-steps ahead (1,054) nor 256 classes by 256 samples, which
-// need 16 KB of the L2 instead of 20 (1,110), nor both sides in LDS and one wavefront a SIMD (1,118) were faster.
+// pipes 56 % busy at 1.9 GHz (codes of 0, which cost little power: 907; a bare loop of the instruction over random codes, 2.7 to 2.9 POP/s,
+// would take 785).  What holds them up is the operands' way into the registers, for 64 instructions 32 KB from LDS and 20 KB through the
+// caches: neither weights six k-steps ahead (1,054) nor 256 classes by 256 samples, which need 16 KB of the L2 instead of 20 (1,110),
+// nor both sides in LDS and one wavefront a SIMD (1,118) were faster.
 // While chunk t is multiplied, a fragment is read for the next k-step when it has been used (the last ones from chunk t + 1, which is
 // there since the barrier), and chunk t + 2 is written to LDS from registers, each half of it half a chunk after it was requested.
 // The chunks run on from one tile of 512 classes by 128 samples to the next.
