@@ -888,11 +888,11 @@ static void cl_logits(const int8_t *xq, const float *xs, const int8_t *wq, const
     // 4,096, one sample: 39 us, 13; 64: 44, 16; 50,000 x 2,048, one: 25, 20; but 64 samples, whose sums take 320 registers, only
     // where a compute unit would have a wavefront or so: 50,000 x 768: 12 us, 21).
     // Few groups of classes leave them idle too, whatever the batch: at most eight tiles of samples at a time take the groups, each with
-    // 256 wavefronts (x 512, batch 82,000: C = 64 574 us, 17 by wavefronts of their own; batch 10,242: C = 1,000 81, 16; batch 2,564: C =
-    // 8,000 22, 21; but C = 16,000, batch 1,284: 20, 36).  Deep rows, whose groups share their samples: x 2,048, batch 10,242: C = 1,000 78, 54;
-    // C = 2,000 76, 77; C = 4,000, batch 5,124: 57, 73.
+    // 256 wavefronts (x 512, batch 82,000: C = 64 574 us, 17 by wavefronts of their own; batch 10,242: C = 1,000 81, 16; batch 1,666: C =
+    // 6,000 16, 14; but C = 8,000 x 1,152, batch 1,282: 24, 25, and C = 16,000, batch 1,284: 20, 36).  Deep rows, whose groups share their
+    // samples: x 2,048, batch 10,242: C = 1,000 78, 54; C = 2,000 76, 77; C = 4,000, batch 5,124: 57, 73.
     const int64_t waves = groups * ks_ceil_div(B, 64);
-    const bool few_groups = groups <= (kb <= CLX_KB ? 128 : 32);
+    const bool few_groups = groups <= (kb <= CLX_KB ? 96 : 32);
     if (B <= 32) return waves <= 1024 && kb >= 24 ? direct(cl_direct_kernel<1, 4, OUT>, 32, 1) : direct(cl_direct_kernel<1, 1, OUT>, 32, 4);
     if (B <= 64 || waves <= 1280 || few_groups || (waves <= 2048 && kb <= 8) || (kb < 4 && !vec))
         return waves <= 320 && kb >= 24 ? direct(cl_direct_kernel<2, 4, OUT>, 64, 1) : direct(cl_direct_kernel<2, 1, OUT>, 64, 4);
