@@ -28,7 +28,8 @@ EXPORTS = ("ks_version", "knn_graph_build_workspace", "knn_graph_build", "knn_gr
            "knn_softmax_selected_next_workspace", "knn_softmax_fwd_bwd_update_selected_next",
            "knn_softmax_split_next_workspace", "knn_softmax_bwd_from_stats_next",
            "ks_peak_mfma", "ks_peak_copy", "grad_topk_plan", "grad_topk_workspace", "grad_topk_select",
-           "class_codes_bytes", "class_quantize_rows", "class_logits_int8", "class_logits_adjust")
+           "class_codes_bytes", "class_quantize_rows", "class_logits_int8", "class_logits_adjust",
+           "class_mxfp4_bytes", "class_quantize_mxfp4", "class_dequantize_mxfp4", "class_logits_mxfp4")
 
 
 class KsError(RuntimeError):
@@ -52,7 +53,7 @@ def lib():
         L = ct.CDLL(path)
         L.ks_version.restype = ct.c_char_p
         for name in EXPORTS:
-            if name.endswith(("_workspace", "_codes_bytes")):
+            if name.endswith(("_workspace", "_bytes")):
                 getattr(L, name).restype = ct.c_size_t
             elif name == "grad_topk_plan":
                 L.grad_topk_plan.restype = ct.c_int64
@@ -64,6 +65,10 @@ def lib():
         L.class_quantize_rows.argtypes = (p, i, i64, i, i64, u32, p, p, p)
         L.class_logits_int8.argtypes = (p, p, p, p, p, i64, i, i, f, p, i, i64, p)
         L.class_logits_adjust.argtypes = (p, i64, p, i64, i, i64, i64, i64, i, p, p, i64, i, p, p, p, p, p, p, p, i64, i, p, i64, i, p, p, p)
+        L.class_mxfp4_bytes.argtypes = (i64, i, u32)
+        L.class_quantize_mxfp4.argtypes = (p, i, i64, i, i64, u32, p, p)
+        L.class_dequantize_mxfp4.argtypes = (p, i64, i, u32, p, i, i64, p)
+        L.class_logits_mxfp4.argtypes = (p, p, p, i64, i, i, f, p, i, i64, p)
         _LIB = L
     return _LIB
 
@@ -937,3 +942,87 @@ def class_logits_adjust(logits, seen=None, seen_max=None, n_prompt=None, repetit
 
     _check("class_logits_adjust", _launch(dev, stream, call))
     return out
+
+
+# ---- answering in 4 bits (include/class_mxfp4.h) ----
+MXFP4_CLASSES = 1
+_MAX_MXFP4_D, _MAX_MXFP4_B = 65536, 4194240  # KS_MAX_MXFP4_*
+
+
+def class_mxfp4_bytes(n, D, classes=False) -> int:
+    """Bytes of the 4-bit codes and exponents of n rows of D elements, 0 for sizes that are refused."""
+    return int(lib().class_mxfp4_bytes(n, D, MXFP4_CLASSES if classes else 0)) if 0 < n <= _INT_MAX and 0 < D <= _MAX_MXFP4_D else 0
+
+
+def class_quantize_mxfp4(V, classes=False, codes=None, stream=None):
+    """Rows of V [n, D] (bf16 or fp32; the rows may lie apart) as 4-bit codes with a power of two per 32 elements, in the order that
+    class_logits_mxfp4 reads, class weights with classes=True.  Returns uint8 [class_mxfp4_bytes]; `codes` is used as the output when
+    given."""
+    L = lib()
+    code, n, D, ldv = _rows(V, _LOGIT_CODES, "V")
+    if D > _MAX_MXFP4_D:
+        raise KsError("class_quantize_mxfp4", KS_UNSUPPORTED)
+    dev, flags = V.get_device(), MXFP4_CLASSES if classes else 0
+    need = class_mxfp4_bytes(n, D, classes)
+    if codes is not None:
+        _list(codes, torch.uint8, need, "codes", dev)
+
+    def call(raw):
+        c = codes if codes is not None else torch.empty(need, dtype=torch.uint8, device=V.device)
+        _check("class_quantize_mxfp4", L.class_quantize_mxfp4(V.data_ptr(), code, n, D, ldv, flags, c.data_ptr(), raw))
+        return c
+
+    return _launch(dev, stream, call)
+
+
+def class_dequantize_mxfp4(codes, n, D, classes=False, out=None, dtype=torch.bfloat16, stream=None):
+    """The values that the codes of n rows of D elements stand for, as rows [n, D] (bf16 or fp32, exact in both).  `out` (its rows may lie
+    apart) is used as the output when given, else the result is of `dtype`."""
+    L = lib()
+    if not (0 < n <= _INT_MAX and 0 < D <= _MAX_MXFP4_D):
+        raise KsError("class_dequantize_mxfp4", KS_UNSUPPORTED if D > _MAX_MXFP4_D and 0 < n <= _INT_MAX else KS_INVALID_ARG)
+    if not codes.is_cuda:
+        raise TypeError("codes must be a device tensor")
+    dev = codes.get_device()
+    _list(codes, torch.uint8, class_mxfp4_bytes(n, D, classes), "codes (of n rows of D elements)", dev)
+    if out is None and dtype not in _LOGIT_CODES:
+        raise TypeError("dtype must be torch.bfloat16 or torch.float32")
+
+    def call(raw):
+        v = out if out is not None else torch.empty((n, D), dtype=dtype, device=codes.device)
+        code, rows, d, ldv = _rows(v, _LOGIT_CODES, "out", dev)
+        if rows != n or d != D:
+            raise ValueError("out must be [n, D]")
+        _check("class_dequantize_mxfp4", L.class_dequantize_mxfp4(codes.data_ptr(), n, D, MXFP4_CLASSES if classes else 0, v.data_ptr(), code, ldv, raw))
+        return v
+
+    return _launch(dev, stream, call)
+
+
+def class_logits_mxfp4(x_codes, w_codes, B, C, D, scale, bias=None, out=None, dtype=torch.float32, stream=None):
+    """Logits [B, C] of B feature rows against all C classes, all of depth D, from the codes of class_quantize_mxfp4 (w_codes made with
+    classes=True).  Without `out` (bf16 or fp32, rows may lie apart) the result is of `dtype` and its rows lie on 128-byte lines."""
+    L = lib()
+    if not (0 < B <= _INT_MAX and 0 < C <= _INT_MAX and 0 < D <= _INT_MAX):
+        raise KsError("class_logits_mxfp4", KS_INVALID_ARG)
+    if D > _MAX_MXFP4_D or B > _MAX_MXFP4_B:
+        raise KsError("class_logits_mxfp4", KS_UNSUPPORTED)
+    if not x_codes.is_cuda:
+        raise TypeError("x_codes must be a device tensor")
+    dev = x_codes.get_device()
+    _list(x_codes, torch.uint8, class_mxfp4_bytes(B, D), "x_codes (of B feature rows of D elements)", dev)
+    _list(w_codes, torch.uint8, class_mxfp4_bytes(C, D, True), "w_codes (of C class rows of D elements)", dev)
+    if bias is not None:
+        _list(bias, torch.float32, C, "bias", dev)
+    if out is None and dtype not in _LOGIT_CODES:
+        raise TypeError("dtype must be torch.bfloat16 or torch.float32")
+
+    def call(raw):
+        z = out if out is not None else torch.empty((B, (C + 63) // 64 * 64), dtype=dtype, device=x_codes.device)[:, :C]
+        code, n, d, ldl = _rows(z, _LOGIT_CODES, "out", dev)
+        if n != B or d != C:
+            raise ValueError("out must be [B, C]")
+        _check("class_logits_mxfp4", L.class_logits_mxfp4(x_codes.data_ptr(), w_codes.data_ptr(), _at(bias), C, D, B, scale, z.data_ptr(), code, ldl, raw))
+        return z
+
+    return _launch(dev, stream, call)
