@@ -29,7 +29,8 @@ EXPORTS = ("ks_version", "knn_graph_build_workspace", "knn_graph_build", "knn_gr
            "knn_softmax_split_next_workspace", "knn_softmax_bwd_from_stats_next",
            "ks_peak_mfma", "ks_peak_copy", "grad_topk_plan", "grad_topk_workspace", "grad_topk_select",
            "class_codes_bytes", "class_quantize_rows", "class_logits_int8", "class_logits_adjust",
-           "class_mxfp4_bytes", "class_quantize_mxfp4", "class_dequantize_mxfp4", "class_logits_mxfp4")
+           "class_mxfp4_bytes", "class_quantize_mxfp4", "class_dequantize_mxfp4", "class_logits_mxfp4",
+           "class_sample_workspace", "class_sample")
 
 
 class KsError(RuntimeError):
@@ -69,6 +70,8 @@ def lib():
         L.class_quantize_mxfp4.argtypes = (p, i, i64, i, i64, u32, p, p)
         L.class_dequantize_mxfp4.argtypes = (p, i64, i, u32, p, i, i64, p)
         L.class_logits_mxfp4.argtypes = (p, p, p, i64, i, i, f, p, i, i64, p)
+        L.class_sample_workspace.argtypes = (i64, i)
+        L.class_sample.argtypes = (p, i64, i, i64, i, p, p, p, p, p, p, p, p, ct.c_size_t, p)
         _LIB = L
     return _LIB
 
@@ -1024,5 +1027,48 @@ def class_logits_mxfp4(x_codes, w_codes, B, C, D, scale, bias=None, out=None, dt
             raise ValueError("out must be [B, C]")
         _check("class_logits_mxfp4", L.class_logits_mxfp4(x_codes.data_ptr(), w_codes.data_ptr(), _at(bias), C, D, B, scale, z.data_ptr(), code, ldl, raw))
         return z
+
+    return _launch(dev, stream, call)
+
+
+# ---- drawing a class from its logits (include/class_sample.h) ----
+def class_sample_workspace(C, B) -> int:
+    """Bytes of workspace, 0 for sizes that are refused."""
+    return int(lib().class_sample_workspace(C, B)) if 0 < C <= _INT_MAX and 0 < B <= _INT_MAX else 0
+
+
+def class_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, ids=None, logprob=None, ws=None, stream=None):
+    """One class per row of logits [B, C] (bf16 or fp32; rows may lie apart) by the random numbers u fp32 [B] in [0, 1): of the top_k [B] int32
+    (<= 0: all) largest the shortest beginning with a share top_p [B] of the weights exp(z / temperature [B]), of these the ones that weigh
+    at least min_p [B] times the largest; all fp32, None: 1, all, 1, 0.  temperature 0: the largest logit's class.  Returns (ids int32
+    [B], -1 for a row without a class; logprob fp32 [B]); `ids` / `logprob` are used as the outputs when given."""
+    L = lib()
+    code, B, C, ldl = _rows(logits, _LOGIT_CODES, "logits")
+    dev = logits.get_device()
+    if not (0 < B <= _INT_MAX and 0 < C <= _INT_MAX):
+        raise KsError("class_sample", KS_INVALID_ARG)
+    _list(u, torch.float32, B, "u", dev)
+    if temperature is not None:
+        _list(temperature, torch.float32, B, "temperature", dev)
+    if top_k is not None:
+        _list(top_k, torch.int32, B, "top_k", dev)
+    if top_p is not None:
+        _list(top_p, torch.float32, B, "top_p", dev)
+    if min_p is not None:
+        _list(min_p, torch.float32, B, "min_p", dev)
+    if ids is not None:
+        _list(ids, torch.int32, B, "ids", dev)
+    if logprob is not None:
+        _list(logprob, torch.float32, B, "logprob", dev)
+    if ws is not None and (ws.get_device() != dev or not ws.is_contiguous()):
+        raise TypeError("ws must be a contiguous tensor on the logits' device")
+
+    def call(raw):
+        i = ids if ids is not None else torch.empty(B, dtype=torch.int32, device=logits.device)
+        lp = logprob if logprob is not None else torch.empty(B, dtype=torch.float32, device=logits.device)
+        w = ws if ws is not None else _ws(L.class_sample_workspace(C, B), logits.device)
+        _check("class_sample", L.class_sample(logits.data_ptr(), ldl, code, C, B, u.data_ptr(), _at(temperature), _at(top_k), _at(top_p), _at(min_p),
+                                              i.data_ptr(), lp.data_ptr(), w.data_ptr(), w.numel() * w.element_size(), raw))
+        return i, lp
 
     return _launch(dev, stream, call)
