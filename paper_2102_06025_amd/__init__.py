@@ -17,4 +17,4 @@ from .binding import (KS_DEV_RANGE, FLAG_UNIT_ROWS, FLAG_PAD_RANDOM, FLAG_TRUSTE
                       ks_version, lib, lib_path, GradTopkPlan, grad_topk_plan, grad_topk_select,
                       QUANT_CLASSES, QUANT_NORMALIZE, class_codes_bytes, class_logits_adjust, class_logits_int8, class_quantize_rows,
                       MXFP4_CLASSES, class_dequantize_mxfp4, class_logits_mxfp4, class_mxfp4_bytes, class_quantize_mxfp4,
-                      class_sample, class_sample_workspace)
+                      class_sample, class_sample_workspace, class_distill_fwd_bwd, class_distill_workspace)

@@ -30,7 +30,8 @@ EXPORTS = ("ks_version", "knn_graph_build_workspace", "knn_graph_build", "knn_gr
            "ks_peak_mfma", "ks_peak_copy", "grad_topk_plan", "grad_topk_workspace", "grad_topk_select",
            "class_codes_bytes", "class_quantize_rows", "class_logits_int8", "class_logits_adjust",
            "class_mxfp4_bytes", "class_quantize_mxfp4", "class_dequantize_mxfp4", "class_logits_mxfp4",
-           "class_sample_workspace", "class_sample")
+           "class_sample_workspace", "class_sample",
+           "class_distill_workspace", "class_distill_fwd_bwd")
 
 
 class KsError(RuntimeError):
@@ -72,6 +73,8 @@ def lib():
         L.class_logits_mxfp4.argtypes = (p, p, p, i64, i, i, f, p, i, i64, p)
         L.class_sample_workspace.argtypes = (i64, i)
         L.class_sample.argtypes = (p, i64, i, i64, i, p, p, p, p, p, p, p, p, ct.c_size_t, p)
+        L.class_distill_workspace.argtypes = (i64, i, i)
+        L.class_distill_fwd_bwd.argtypes = (p, i64, i, i64, i, p, p, i, i, f, f, p, p, p, i64, p, ct.c_size_t, p, p)
         _LIB = L
     return _LIB
 
@@ -1070,5 +1073,61 @@ def class_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None
         _check("class_sample", L.class_sample(logits.data_ptr(), ldl, code, C, B, u.data_ptr(), _at(temperature), _at(top_k), _at(top_p), _at(min_p),
                                               i.data_ptr(), lp.data_ptr(), w.data_ptr(), w.numel() * w.element_size(), raw))
         return i, lp
+
+    return _launch(dev, stream, call)
+
+
+# ---- learning from a teacher's top logits (include/class_distill.h) ----
+_MAX_DISTILL_K = 4096  # KS_MAX_DISTILL_K
+
+
+def class_distill_workspace(C, B, K) -> int:
+    """Bytes of workspace, 0 for sizes that are refused."""
+    return int(lib().class_distill_workspace(C, B, K)) if 0 < C <= _INT_MAX and 0 < B <= _INT_MAX and 0 < K <= _MAX_DISTILL_K else 0
+
+
+def class_distill_fwd_bwd(logits, teacher_ids, teacher_logits, temperature=1.0, grad_scale=1.0, out=None, ws=None, dev_status=None, stream=None):
+    """Loss and gradient of logits [B, C] (bf16 or fp32; rows may lie apart) that learn from a teacher's logits [B, K] (bf16 or fp32) of the
+    classes teacher_ids [B, K] int32 (negative: an empty entry).  Returns dict(loss_per_sample, loss_mean, dlogits, dev_status); `out`, a
+    dict of the first three, is used as the outputs when given, and its dlogits may be the logits themselves: in place."""
+    L = lib()
+    code, B, C, ldl = _rows(logits, _LOGIT_CODES, "logits")
+    dev = logits.get_device()
+    if teacher_ids.dim() != 2 or teacher_ids.shape[0] != B or teacher_logits.shape != teacher_ids.shape:
+        raise ValueError("teacher_ids and teacher_logits must be [B, K]")
+    K = teacher_ids.shape[1]
+    if not (0 < B <= _INT_MAX and 0 < C <= _INT_MAX and 0 < K <= _INT_MAX):
+        raise KsError("class_distill_fwd_bwd", KS_INVALID_ARG)
+    if K > _MAX_DISTILL_K:
+        raise KsError("class_distill_fwd_bwd", KS_UNSUPPORTED)
+    _list(teacher_ids, torch.int32, B * K, "teacher_ids", dev)
+    if teacher_logits.dtype not in _LOGIT_CODES:
+        raise TypeError("teacher_logits must be torch.bfloat16 or torch.float32")
+    _list(teacher_logits, teacher_logits.dtype, B * K, "teacher_logits", dev)
+    if dev_status is not None:
+        _list(dev_status, torch.int32, 1, "dev_status", dev)
+    if ws is not None and (ws.get_device() != dev or not ws.is_contiguous()):
+        raise TypeError("ws must be a contiguous tensor on the logits' device")
+
+    def call(raw):
+        o = out
+        if o is None:
+            ld = (C + 63) // 64 * 64
+            o = dict(loss_per_sample=torch.empty(B, dtype=torch.float32, device=logits.device),
+                     loss_mean=torch.empty(1, dtype=torch.float32, device=logits.device),
+                     dlogits=torch.empty((B, ld), dtype=logits.dtype, device=logits.device)[:, :C])
+        _list(o["loss_per_sample"], torch.float32, B, "loss_per_sample", dev)
+        _list(o["loss_mean"], torch.float32, 1, "loss_mean", dev)
+        d = o["dlogits"]
+        other, n, c, ldd = _rows(d, _LOGIT_CODES, "dlogits", dev)
+        if other != code or n != B or c != C:
+            raise ValueError("dlogits must have the logits' type and shape")
+        o["dev_status"] = _status(logits.device, dev_status)
+        w = ws if ws is not None else _ws(L.class_distill_workspace(C, B, K), logits.device)
+        _check("class_distill_fwd_bwd", L.class_distill_fwd_bwd(
+            logits.data_ptr(), ldl, code, C, B, teacher_ids.data_ptr(), teacher_logits.data_ptr(), _LOGIT_CODES[teacher_logits.dtype], K, temperature,
+            grad_scale, o["loss_per_sample"].data_ptr(), o["loss_mean"].data_ptr(), d.data_ptr(), ldd, w.data_ptr(), w.numel() * w.element_size(),
+            o["dev_status"].data_ptr(), raw))
+        return o
 
     return _launch(dev, stream, call)
