@@ -35,8 +35,8 @@ extern "C" {
  *   temperature, top_p, min_p [B] fp32, top_k [B] int32      each may be NULL: 1, 1, 0, 0 for all rows
  *   ids [B]         out: the drawn class, -1 where a row has no class to draw (all of it -infinity or NaN)
  *   logprob [B]     out, fp32, may be NULL: the logarithm of its weight's share of what is kept; -infinity where ids is -1
- * Requires B >= 1, 1 <= C < 2^31.  Workspace: class_sample_workspace, 12 bytes for 512 classes of a row (more classes than 2^21: for more
- * of them); 0 for sizes that are refused.
+ * Requires B >= 1, 1 <= C < 2^31.  Workspace: class_sample_workspace, 12 bytes for each of up to 4,096 parts of a row; 0 for sizes that
+ * are refused.
  * ---------------------------------------------------------------------------------------------------- */
 size_t class_sample_workspace(int64_t C, int B);
 int class_sample(const void *logits, int64_t ldl, int dtype, int64_t C, int B, const float *u, const float *temperature,

@@ -1,23 +1,23 @@
 // Drawing one class per request from its row of the logits (paper Section 3.2: the softmax over the classes): temperature, top-k, top-p and
 // min-p, by given random numbers.
 //
-// The first launch reads the logits once, all compute units sharing the rows: the largest logit of every segment of 512 classes, and where it
-// is needed the segment's weight.  The second has a workgroup per row, which learns from the segments which of them can hold a kept class
-// and reads only those: with k classes to keep, the segments down to the k-th largest of their maxima hold them all; with a share p of
-// the weight, segments that hold less than that do not.  A flat distribution, of which most is kept, leaves all segments: the same
-// steps over the whole row.
+// The first launch reads the logits once, all compute units sharing the rows: the largest logit of every granule of 8 to 512 classes (at most
+// 4,096 granules a row), and where it is needed the granule's weight.  The second has a workgroup per row, which learns from the granules
+// which of them can hold a kept class and reads only those: with k classes to keep, the granules down to the k-th largest of their maxima
+// hold them all; with a share p of the weight, granules that hold less than that do not.  What may be kept is put in order in LDS.  Rows of
+// which more is kept than LDS holds (a flat distribution) are left to a third launch.
 #include "../../include/class_sample.h"
 #include "ks_common.h"
 
 #define SP_NT 1024
 #define SP_WAVES (SP_NT / 64)
 #define SP_CHUNK 512     /* classes that a wavefront takes at a time: eight consecutive ones a lane */
-#define SP_SEGS 4096     /* most segments of a row */
+#define SP_GRANULES 4096 /* most granules of a row */
+#define SP_PER (SP_GRANULES / SP_NT) /* most granules of a thread */
 #define SP_BINS 2048     /* of the weights: 32 to a factor of two */
 #define SP_PER_BINADE 32
-#define SP_CAND 4096     /* classes of one bin that are put in order in LDS */
+#define SP_CAND 8192     /* classes that are put in order in LDS */
 #define SP_NO_BIN (1 << 20)
-#define SP_PER (SP_SEGS / SP_NT) /* most segments of a thread */
 
 // of one type: min() and max() of the runtime's headers go through double for 64-bit numbers
 template <typename T> static __device__ __forceinline__ T sp_min(T a, T b) { return b < a ? b : a; }
@@ -25,12 +25,13 @@ template <typename T> static __device__ __forceinline__ T sp_max(T a, T b) { ret
 
 struct SpArgs {
     const void *logits;
-    int64_t ldl, C, seg; // classes of a segment, a multiple of SP_CHUNK
-    int nseg, bits, row0;
+    int64_t ldl, C, gran; // classes of a granule: 8 << lg, beyond 512 a multiple of that
+    int lg, ngr, bits, row0;
     const float *u, *temperature, *top_p, *min_p;
     const int32_t *top_k;
-    float *seg_max;  // [B, nseg]
-    double *seg_sum; // [B, nseg]: sum of exp((z - seg_max) / T)
+    float *g_max;  // [B, ngr]
+    double *g_sum; // [B, ngr]: sum of exp((z - g_max) / T)
+    int32_t *many; // [B]: the row is left to the third launch
     int32_t *ids;
     float *logprob;
 };
@@ -41,7 +42,7 @@ struct SpRule {
     int64_t k;           // 0: all
     double p;
     float m;
-    bool greedy, use_k, use_p, use_m, sums; // sums: the segments' weights are needed
+    bool greedy, use_k, use_p, use_m, sums; // sums: the granules' weights are needed
     __device__ __forceinline__ SpRule(const SpArgs &a, int row) {
         const float t = a.temperature ? a.temperature[row] : 1.f;
         greedy = !(t > 0.f);
@@ -133,22 +134,32 @@ template <typename T> __device__ __forceinline__ const T *sp_row(const SpArgs &a
     vec = (uintptr_t)p % 16 == 0;
     return p;
 }
-__device__ __forceinline__ double sp_wave_sum(double v) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+// op over groups of 2^LG lanes, in all of them
+template <int CTRL> __device__ __forceinline__ float sp_move(float v) { return KS_DPP_F(v, v, CTRL, 0xf); }
+template <int CTRL> __device__ __forceinline__ double sp_move(double v) {
+    const int lo = __double2loint(v), hi = __double2hiint(v);
+    return __hiloint2double(KS_DPP(hi, hi, CTRL, 0xf), KS_DPP(lo, lo, CTRL, 0xf));
+}
+template <int LG, typename V, typename OP> __device__ __forceinline__ V sp_lanes(V v, OP op) {
+    if (LG > 0) v = op(v, sp_move<0xB1>(v));  // quad_perm [1, 0, 3, 2]
+    if (LG > 1) v = op(v, sp_move<0x4E>(v));  // quad_perm [2, 3, 0, 1]
+    if (LG > 2) v = op(v, sp_move<0x141>(v)); // row_half_mirror
+    if (LG > 3) v = op(v, sp_move<0x140>(v)); // row_mirror
+    if (LG > 4) v = op(v, (V)__shfl_xor(v, 16));
+    if (LG > 5) v = op(v, (V)__shfl_xor(v, 32));
     return v;
 }
 
-// A wavefront per segment.
-template <typename T>
+// A wavefront per 512 classes, or per granule of more.
+template <int LG, typename T>
 __global__ void __launch_bounds__(256)
-sp_segments_kernel(SpArgs a) {
-    const int lane = threadIdx.x & 63, s = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = a.row0 + blockIdx.y;
-    if (s >= a.nseg) return;
+sp_granules_kernel(SpArgs a) {
+    const int lane = threadIdx.x & 63, wave = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = a.row0 + blockIdx.y;
+    const int64_t span = LG < 6 ? SP_CHUNK : a.gran, first = wave * span, last = sp_min(first + span, a.C);
+    if (first >= a.C) return;
     const SpRule rule(a, row);
     bool vec;
     const T *const z = sp_row<T>(a, row, vec);
-    const int64_t first = s * a.seg, last = sp_min(first + a.seg, a.C);
     float top = -INFINITY;
     float v[8];
     for (int64_t e = first; e < last; e += SP_CHUNK) {
@@ -156,19 +167,20 @@ sp_segments_kernel(SpArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) top = fmaxf(top, v[i]);
     }
-    top = ks_wave_max(top);
+    top = sp_lanes<LG>(top, [](float x, float y) __attribute__((always_inline)) { return fmaxf(x, y); });
+    const int64_t g = LG < 6 ? (first >> (LG + 3)) + (lane >> LG) : wave;
+    const bool writes = (lane & ((1 << LG) - 1)) == 0 && g < a.ngr;
+    if (writes) a.g_max[(int64_t)row * a.ngr + g] = top;
+    if (!rule.sums) return;
     double sum = 0.0;
-    if (rule.sums && top > -INFINITY)
+    if (top > -INFINITY)
         for (int64_t e = first; e < last; e += SP_CHUNK) {
-            if (a.seg > SP_CHUNK) sp_load(z, vec, e + lane * 8, a.C, v); // else they are there
+            if (LG == 6 && a.gran > SP_CHUNK) sp_load(z, vec, e + lane * 8, a.C, v); // else they are there
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum += sp_exp2(sp_log2w(v[i], top, rule.c));
         }
-    sum = sp_wave_sum(sum);
-    if (lane == 0) {
-        a.seg_max[(int64_t)row * a.nseg + s] = top;
-        if (rule.sums) a.seg_sum[(int64_t)row * a.nseg + s] = sum;
-    }
+    sum = sp_lanes<LG>(sum, [](double x, double y) __attribute__((always_inline)) { return x + y; });
+    if (writes) a.g_sum[(int64_t)row * a.ngr + g] = sum;
 }
 
 // inclusive sum over the wavefront
@@ -182,49 +194,38 @@ __device__ __forceinline__ uint64_t sp_wave_scan(uint64_t v) {
     return v;
 }
 
-struct SpShared {
-    uint32_t n[SP_BINS];   // of the bins: classes (at first: segments), and their weight
-    uint64_t w[SP_BINS];
-    union {
-        uint64_t cand[SP_CAND]; // places of the classes of one bin
-        struct {
-            uint32_t n[SP_BINS];
-            uint64_t w[SP_BINS];
-        } sub;                  // parts of a bin that has too many
-    };
-    uint64_t seg_w[SP_SEGS]; // kept weight of the listed segments
-    int32_t list[SP_SEGS];
-    uint64_t wave_w[SP_WAVES + 1], wave_v[SP_WAVES + 1];
-    uint32_t wave_n[SP_WAVES + 1];
-    uint64_t found_w, found_place;
-    uint32_t found_n, fill;
-    int found, n_list;
+struct SpScan {
+    uint64_t w[SP_WAVES], v[SP_WAVES];
+    uint32_t n[SP_WAVES];
+    uint64_t found_w;
+    uint32_t found_n;
+    int found;
 };
 
 // exclusive sums over the workgroup of a weight and a number a thread, and their totals
-__device__ __forceinline__ void sp_scan(SpShared &sh, uint64_t w, uint32_t n, uint64_t &w0, uint32_t &n0, uint64_t &w_all, uint32_t &n_all) {
+__device__ __forceinline__ void sp_scan(SpScan &sh, uint64_t w, uint32_t n, uint64_t &w0, uint32_t &n0, uint64_t &w_all, uint32_t &n_all) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint64_t wi = sp_wave_scan(w);
     const uint32_t ni = (uint32_t)ks_wave_iscan((int)n);
     __syncthreads();
-    if (lane == 63) { sh.wave_w[wave] = wi; sh.wave_n[wave] = ni; }
+    if (lane == 63) { sh.w[wave] = wi; sh.n[wave] = ni; }
     __syncthreads();
     w0 = wi - w; n0 = ni - n; w_all = 0; n_all = 0;
 #pragma unroll
     for (int i = 0; i < SP_WAVES; ++i) {
-        if (i < wave) { w0 += sh.wave_w[i]; n0 += sh.wave_n[i]; }
-        w_all += sh.wave_w[i];
-        n_all += sh.wave_n[i];
+        if (i < wave) { w0 += sh.w[i]; n0 += sh.n[i]; }
+        w_all += sh.w[i];
+        n_all += sh.n[i];
     }
 }
-__device__ __forceinline__ float sp_block_max(SpShared &sh, float v) {
+__device__ __forceinline__ float sp_block_max(SpScan &sh, float v) {
     v = ks_wave_max(v);
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh.wave_n[threadIdx.x >> 6] = __float_as_uint(v);
+    if ((threadIdx.x & 63) == 0) sh.n[threadIdx.x >> 6] = __float_as_uint(v);
     __syncthreads();
-    v = __uint_as_float(sh.wave_n[0]);
+    v = __uint_as_float(sh.n[0]);
 #pragma unroll
-    for (int i = 1; i < SP_WAVES; ++i) v = fmaxf(v, __uint_as_float(sh.wave_n[i]));
+    for (int i = 1; i < SP_WAVES; ++i) v = fmaxf(v, __uint_as_float(sh.n[i]));
     return v;
 }
 __device__ __forceinline__ void sp_clear(uint32_t *n, uint64_t *w) {
@@ -234,7 +235,7 @@ __device__ __forceinline__ void sp_clear(uint32_t *n, uint64_t *w) {
 }
 // The first bin at which the running number (by_n) or weight reaches `target` >= 1: found (-1: none does), and what lies before it;
 // the totals.
-__device__ __forceinline__ void sp_find(SpShared &sh, const uint32_t *n, const uint64_t *w, bool by_n, uint64_t target, uint64_t &w_all, uint32_t &n_all) {
+__device__ __forceinline__ void sp_find(SpScan &sh, const uint32_t *n, const uint64_t *w, bool by_n, uint64_t target, uint64_t &w_all, uint32_t &n_all) {
     __syncthreads();
     if (threadIdx.x == 0) sh.found = -1;
     constexpr int EACH = SP_BINS / SP_NT;
@@ -254,127 +255,57 @@ __device__ __forceinline__ void sp_find(SpShared &sh, const uint32_t *n, const u
     __syncthreads();
 }
 
-// f(z, id) for the eight classes a lane of all listed segments
-template <typename T, typename F> __device__ __forceinline__ void sp_over_list(const SpArgs &a, const T *z, bool vec, const SpShared &sh, F f) {
-    const int lane = threadIdx.x & 63;
-    for (int i = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < sh.n_list; i += SP_WAVES) {
-        const int64_t first = sh.list[i] * a.seg, last = sp_min(first + a.seg, a.C);
-        for (int64_t e = first; e < last; e += SP_CHUNK) {
-            float v[8];
-            sp_load(z, vec, e + lane * 8, a.C, v);
+// granules of a workgroup's threads, SP_PER consecutive ones each
+struct SpMine {
+    float top[SP_PER], row_top;
+    int first, n; // of the thread
+    __device__ __forceinline__ SpMine(const SpArgs &a, int row, SpScan &sh) {
+        const int per = (a.ngr + SP_NT - 1) / SP_NT;
+        first = threadIdx.x * per;
+        n = sp_max(0, sp_min(per, a.ngr - first));
+        row_top = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f(v[j], (uint32_t)(e + lane * 8 + j));
+        for (int i = 0; i < SP_PER; ++i) {
+            top[i] = i < n ? a.g_max[(int64_t)row * a.ngr + first + i] : -INFINITY;
+            row_top = fmaxf(row_top, top[i]);
         }
+        row_top = sp_block_max(sh, row_top);
     }
+    // weight of granule i
+    __device__ __forceinline__ uint64_t weight(const SpArgs &a, int row, const SpRule &rule, int i) const {
+        return top[i] > -INFINITY ? (uint64_t)(a.g_sum[(int64_t)row * a.ngr + first + i] * sp_exp2(sp_log2w(top[i], row_top, rule.c) + a.bits) + 0.5) : 0;
+    }
+};
+__device__ __forceinline__ float sp_c32(const SpRule &rule) { return (float)(rule.c * SP_PER_BINADE); }
+__device__ __forceinline__ int sp_limit(const SpArgs &a) { return (a.bits + 1) * SP_PER_BINADE; } // from this bin on weights are 0
+__device__ __forceinline__ int sp_bin_m(const SpArgs &a, const SpRule &rule) { // last bin with weights of m or more
+    return rule.use_m ? (int)fminf(-log2f(rule.m) * SP_PER_BINADE + 2.f, (float)(sp_limit(a) - 1)) : sp_limit(a) - 1;
+}
+__device__ __forceinline__ uint64_t sp_floor(const SpArgs &a, const SpRule &rule) {
+    return rule.use_m ? sp_max((uint64_t)ceil((double)rule.m * (double)((uint64_t)1 << a.bits)), (uint64_t)1) : 0;
+}
+__device__ __forceinline__ uint64_t sp_share(double p, uint64_t w) { return sp_max((uint64_t)ceil(p * (double)w), (uint64_t)1); } // the weight that is p of w
+__device__ __forceinline__ uint64_t sp_target(const SpArgs &a, int row, uint64_t w) { // the running weight that the drawn class exceeds: u of w
+    const double share = fmax((double)a.u[row], 0.0) * (double)w;
+    return share >= (double)w ? w - 1 : sp_min((uint64_t)share, w - 1);
+}
+__device__ __forceinline__ void sp_result(const SpArgs &a, int row, int id, float z, float top, double c, uint64_t w) {
+    a.ids[row] = id;
+    if (a.logprob) a.logprob[row] = (float)((sp_log2w(z, top, c) - (log2((double)w) - a.bits)) * 0.6931471805599453); // log of 2^(c (z - top)) / (w 2^-bits)
 }
 
-// Of the listed classes of bin `bin`, which are sh.n[bin]: the place of the one at which the running number or weight reaches `target`, in
-// the order; `weight`: their weight up to it.  Too many for LDS (a bin of equal logits) are cut into parts of equal ranges of places first.
-template <typename T>
-__device__ uint64_t sp_refine(const SpArgs &a, const T *z, bool vec, SpShared &sh, float top, double c, float c32, int bin, bool by_n, uint64_t target,
-                              uint64_t &weight) {
-    uint64_t lo = 0, hi = ~0ull, before = 0;
-    uint32_t n = sh.n[bin];
-    while (n > SP_CAND) {
-        uint64_t least = ~0ull, most = 0;
-        sp_over_list(a, z, vec, sh, [&](float v, uint32_t id) __attribute__((always_inline)) {
-            if (sp_bin(v, top, c32) != bin) return;
-            const uint64_t place = sp_place(v, id);
-            if (place < lo || place > hi) return;
-            least = sp_min(least, place);
-            most = sp_max(most, place);
-        });
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            least = sp_min(least, (uint64_t)__shfl_xor((unsigned long long)least, d));
-            most = sp_max(most, (uint64_t)__shfl_xor((unsigned long long)most, d));
-        }
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) { sh.wave_w[threadIdx.x >> 6] = least; sh.wave_v[threadIdx.x >> 6] = most; }
-        __syncthreads();
-        for (int i = 0; i < SP_WAVES; ++i) { least = sp_min(least, sh.wave_w[i]); most = sp_max(most, sh.wave_v[i]); }
-        int shift = 0;
-        while ((most - least) >> shift >= SP_BINS) ++shift;
-        sp_clear(sh.sub.n, sh.sub.w);
-        sp_over_list(a, z, vec, sh, [&](float v, uint32_t id) __attribute__((always_inline)) {
-            if (sp_bin(v, top, c32) != bin) return;
-            const uint64_t place = sp_place(v, id);
-            if (place < least || place > most) return;
-            const int part = (int)((place - least) >> shift);
-            atomicAdd(&sh.sub.n[part], 1u);
-            atomicAdd((unsigned long long *)&sh.sub.w[part], (unsigned long long)sp_weight(v, top, c, a.bits));
-        });
-        uint64_t w_all;
-        uint32_t n_all;
-        sp_find(sh, sh.sub.n, sh.sub.w, by_n, target, w_all, n_all);
-        const int part = sh.found; // there is one: the target lies within the bin
-        lo = least + ((uint64_t)part << shift);
-        hi = sp_min(most, lo + (((uint64_t)1 << shift) - 1));
-        n = sh.sub.n[part];
-        target -= by_n ? sh.found_n : sh.found_w;
-        before += sh.found_w;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) { sh.fill = 0; sh.found_place = 0; sh.found_w = 0; }
-    int size = 64;
-    while (size < (int)n) size <<= 1;
-    for (int i = n + threadIdx.x; i < size; i += SP_NT) sh.cand[i] = ~0ull;
-    __syncthreads();
-    sp_over_list(a, z, vec, sh, [&](float v, uint32_t id) __attribute__((always_inline)) {
-        if (sp_bin(v, top, c32) != bin) return;
-        const uint64_t place = sp_place(v, id);
-        if (place >= lo && place <= hi) {
-            const uint32_t at = atomicAdd(&sh.fill, 1u);
-            if (at < n) sh.cand[at] = place;
-        }
-    });
-    __syncthreads();
-    for (int k = 2; k <= size; k <<= 1) // bitonic sort
-        for (int j = k >> 1; j > 0; j >>= 1) {
-            for (int i = threadIdx.x; i < size / 2; i += SP_NT) {
-                const int x = i / j * 2 * j + i % j, y = x + j;
-                const uint64_t p = sh.cand[x], q = sh.cand[y];
-                if ((p > q) == ((x & k) == 0)) { sh.cand[x] = q; sh.cand[y] = p; }
-            }
-            __syncthreads();
-        }
-    // SP_CAND / SP_NT consecutive candidates a thread
-    constexpr int EACH = SP_CAND / SP_NT;
-    uint64_t w[EACH], mine = 0, w0, w_all;
-    uint32_t unused, unused_all;
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        const int at = threadIdx.x * EACH + i;
-        w[i] = at < (int)n ? sp_weight(sp_place_z(sh.cand[at]), top, c, a.bits) : 0;
-        mine += w[i];
-    }
-    sp_scan(sh, mine, 0, w0, unused, w_all, unused_all);
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        const int at = threadIdx.x * EACH + i;
-        if (at < (int)n && (by_n ? at + 1 == (int)target : w0 < target && target <= w0 + w[i])) {
-            sh.found_place = sh.cand[at];
-            sh.found_w = w0 + w[i];
-        }
-        w0 += w[i];
-    }
-    __syncthreads();
-    weight = before + sh.found_w;
-    return sh.found_place;
-}
-
-// One wavefront: of the classes of segment s that are kept, the one at which the running weight exceeds `target`; if rounding left less
+// One wavefront: of the classes [first, last) that are kept, the one at which the running weight exceeds `target`; if rounding left less
 // weight than that the last that is kept.  -> its id and logit
 template <typename T>
-__device__ void sp_pick(const SpArgs &a, const T *z, bool vec, int s, uint64_t target, float top, double c, uint64_t cut, uint64_t floor_w, int &id, float &logit) {
+__device__ __forceinline__ void sp_pick(const SpArgs &a, const T *z, bool vec, int64_t first, int64_t last, uint64_t target, float top, double c, uint64_t cut,
+                                        uint64_t floor_w, int &id, float &logit) {
     const int lane = threadIdx.x & 63;
-    const int64_t first = s * a.seg, last = sp_min(first + a.seg, a.C);
     id = -1;
     logit = -INFINITY;
     for (int64_t e = first; e < last; e += SP_CHUNK) {
         float v[8];
         uint64_t w[8], mine = 0;
-        sp_load(z, vec, e + lane * 8, a.C, v);
+        sp_load(z, vec, e + lane * 8, last, v);
         int my_last = -1;
         float my_z = -INFINITY;
 #pragma unroll
@@ -396,8 +327,7 @@ __device__ void sp_pick(const SpArgs &a, const T *z, bool vec, int s, uint64_t t
                 if (got < 0 && run <= target && target < run + w[i]) { got = (int)(e + lane * 8 + i); got_z = v[i]; }
                 run += w[i];
             }
-            const uint64_t who = __ballot(got >= 0);
-            const int l = __ffsll((unsigned long long)who) - 1;
+            const int l = __ffsll((unsigned long long)__ballot(got >= 0)) - 1;
             id = __shfl(got, l);
             logit = __shfl(got_z, l);
             return;
@@ -410,6 +340,88 @@ __device__ void sp_pick(const SpArgs &a, const T *z, bool vec, int s, uint64_t t
         }
     }
 }
+// the first class of [first, last) with logit `top`
+template <typename T> __device__ __forceinline__ int sp_first(const SpArgs &a, const T *z, bool vec, int64_t first, int64_t last, float top) {
+    const int lane = threadIdx.x & 63;
+    for (int64_t e = first; e < last; e += SP_CHUNK) {
+        float v[8];
+        sp_load(z, vec, e + lane * 8, last, v);
+        int got = -1;
+#pragma unroll
+        for (int i = 7; i >= 0; --i)
+            if (v[i] == top) got = (int)(e + lane * 8 + i);
+        const uint64_t who = __ballot(got >= 0);
+        if (who) return __shfl(got, __ffsll((unsigned long long)who) - 1);
+    }
+    return -1;
+}
+
+// f(z, id) for eight classes a thread of the n listed granules; all lanes of a wavefront call it together
+template <typename T, typename F> __device__ __forceinline__ void sp_over_list(const SpArgs &a, const T *z, bool vec, const int32_t *list, int n, F f) {
+    if (a.gran <= SP_CHUNK) {
+        const int lanes = 1 << a.lg, at_once = SP_NT >> a.lg, sub = threadIdx.x & (lanes - 1);
+        for (int i0 = 0; i0 < n; i0 += at_once) {
+            const int i = i0 + (threadIdx.x >> a.lg);
+            float v[8];
+            const int64_t e = i < n ? list[i] * a.gran + sub * 8 : a.C;
+            sp_load(z, vec, e, a.C, v);
+            f(v, (uint32_t)e);
+        }
+    } else {
+        const int lane = threadIdx.x & 63;
+        for (int i = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < n; i += SP_WAVES) {
+            const int64_t first = list[i] * a.gran, last = sp_min(first + a.gran, a.C);
+            for (int64_t e = first + lane * 8; e - lane * 8 < last; e += SP_CHUNK) {
+                float v[8];
+                sp_load(z, vec, e, a.C, v);
+                f(v, (uint32_t)e);
+            }
+        }
+    }
+}
+// the granules whose largest logit lies in bin b0 or before, in order: list, and how many
+__device__ __forceinline__ int sp_list(const SpMine &mine, SpScan &sh, float c32, int b0, int32_t *list) {
+    bool in[SP_PER];
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < SP_PER; ++i) {
+        in[i] = sp_bin(mine.top[i], mine.row_top, c32) <= b0;
+        n += in[i];
+    }
+    uint64_t w0, w_all;
+    uint32_t at, all;
+    sp_scan(sh, 0, (uint32_t)n, w0, at, w_all, all);
+#pragma unroll
+    for (int i = 0; i < SP_PER; ++i)
+        if (in[i]) list[at++] = mine.first + i;
+    __syncthreads();
+    return (int)all;
+}
+
+// p[0 .. size) into ascending order (bitonic), size a power of two, at least 64.  A wavefront's 64 pairs lie within 128 numbers where they are at
+// most 64 apart: only wider steps, and the first one after them, wait for the other wavefronts.
+__device__ __forceinline__ void sp_sort(uint64_t *p, int size) {
+    for (int k = 2; k <= size; k <<= 1)
+        for (int j = k >> 1; j > 0; j >>= 1) {
+            if (j >= 64) __syncthreads();
+            else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            for (int i = threadIdx.x; i < size / 2; i += SP_NT) {
+                const int x = ((i & ~(j - 1)) << 1) | (i & (j - 1)), y = x + j;
+                const uint64_t u = p[x], v = p[y];
+                if ((u > v) == ((x & k) == 0)) { p[x] = v; p[y] = u; }
+            }
+        }
+    __syncthreads();
+}
+
+struct SpShared {
+    SpScan scan;
+    uint32_t n[SP_BINS];   // of the bins: granules, and their weight; then of ranges of ids
+    uint64_t w[SP_BINS];
+    uint64_t cand[SP_CAND]; // places of classes that may be kept
+    int32_t list[SP_CAND > SP_GRANULES ? SP_CAND : SP_GRANULES]; // granules; then candidates of one range of ids
+    uint32_t fill;
+};
 
 // A workgroup per row.
 template <typename T>
@@ -420,19 +432,9 @@ sp_draw_kernel(SpArgs a) {
     const SpRule rule(a, row);
     bool vec;
     const T *const z = sp_row<T>(a, row, vec);
-    const float *const seg_max = a.seg_max + (int64_t)row * a.nseg;
-    const double *const seg_sum = a.seg_sum + (int64_t)row * a.nseg;
-    // up to SP_PER consecutive segments a thread
-    const int per = (a.nseg + SP_NT - 1) / SP_NT;
-    float my_max[SP_PER];
-    float top = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < SP_PER; ++i) {
-        const int s = threadIdx.x * per + i;
-        my_max[i] = i < per && s < a.nseg ? seg_max[s] : -INFINITY;
-        top = fmaxf(top, my_max[i]);
-    }
-    top = sp_block_max(sh, top);
+    const SpMine mine(a, row, sh.scan);
+    const float top = mine.row_top;
+    if (threadIdx.x == 0) a.many[row] = 0;
     if (!(top > -INFINITY)) {
         if (threadIdx.x == 0) {
             a.ids[row] = -1;
@@ -441,227 +443,483 @@ sp_draw_kernel(SpArgs a) {
         return;
     }
     const double c = rule.c;
-    const float c32 = (float)(c * SP_PER_BINADE);
-    const int limit = (a.bits + 1) * SP_PER_BINADE; // from this bin on weights are 0
-    const auto seg_mass = [&](int i) __attribute__((always_inline)) -> uint64_t {
-        const int s = threadIdx.x * per + i;
-        return my_max[i] > -INFINITY ? (uint64_t)(seg_sum[s] * sp_exp2(sp_log2w(my_max[i], top, c) + a.bits) + 0.5) : 0;
-    };
-
-    uint64_t cut = ~0ull, floor_w = 0, all_w = 0;
-    uint32_t unused_n, unused_all;
-    uint64_t my_w[SP_PER] = {}, w0;
-    const bool plain = !rule.greedy && !rule.use_k && !rule.use_p && !rule.use_m;
+    uint64_t w0, w_all;
+    uint32_t n0, n_all;
     if (rule.greedy) { // the first class with the largest logit: the only one that is kept
-        if (threadIdx.x == 0) { sh.fill = 0x7FFFFFFF; sh.n_list = 1; }
+        if (threadIdx.x == 0) sh.fill = 0x7FFFFFFF;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < SP_PER; ++i)
-            if (my_max[i] == top) atomicMin(&sh.fill, (uint32_t)(threadIdx.x * per + i));
+            if (mine.top[i] == top) atomicMin(&sh.fill, (uint32_t)(mine.first + i));
         __syncthreads();
         if (wave == 0) {
-            const int64_t first = (int64_t)sh.fill * a.seg, last = sp_min(first + a.seg, a.C);
-            for (int64_t e = first; e < last; e += SP_CHUNK) {
-                float v[8];
-                sp_load(z, vec, e + lane * 8, a.C, v);
-                int got = -1;
-#pragma unroll
-                for (int i = 7; i >= 0; --i)
-                    if (v[i] == top) got = (int)(e + lane * 8 + i);
-                const uint64_t who = __ballot(got >= 0);
-                if (who) {
-                    const int id = __shfl(got, __ffsll((unsigned long long)who) - 1);
-                    if (lane == 0) {
-                        a.ids[row] = id;
-                        if (a.logprob) a.logprob[row] = 0.f;
-                    }
-                    break;
-                }
+            const int64_t first = sh.fill * a.gran;
+            const int id = sp_first(a, z, vec, first, sp_min(first + a.gran, a.C), top);
+            if (lane == 0) {
+                a.ids[row] = id;
+                if (a.logprob) a.logprob[row] = 0.f;
             }
         }
         return;
     }
-    if (plain) { // all classes: the segments' weights say where to look
+    if (!rule.use_k && !rule.use_p && !rule.use_m) { // all classes: the granules' weights say where to look
+        uint64_t w[SP_PER], sum = 0;
 #pragma unroll
-        for (int i = 0; i < SP_PER; ++i) my_w[i] = seg_mass(i);
-    } else {
-        // 1  down to which bin segments and classes have to be looked at
-        const int bin_m = rule.use_m ? (int)fminf(-log2f(rule.m) * SP_PER_BINADE + 2.f, (float)(limit - 1)) : limit - 1;
-        int b0 = bin_m;
-        uint64_t target_p = 0;
-        if (rule.use_k || rule.use_p) {
-            sp_clear(sh.n, sh.w);
-            uint64_t mine = 0;
-#pragma unroll
-            for (int i = 0; i < SP_PER; ++i) {
-                const int b = sp_bin(my_max[i], top, c32);
-                if (b >= limit) continue;
-                atomicAdd(&sh.n[b], 1u);
-                if (!rule.use_k) {
-                    const uint64_t w = seg_mass(i);
-                    mine += w;
-                    atomicAdd((unsigned long long *)&sh.w[b], (unsigned long long)w);
-                }
-            }
-            uint64_t w_all;
-            uint32_t n_all;
-            if (!rule.use_k) {
-                sp_scan(sh, mine, 0, w0, unused_n, w_all, unused_all);
-                target_p = sp_max((uint64_t)ceil(rule.p * (double)w_all), (uint64_t)1);
-            }
-            sp_find(sh, sh.n, sh.w, rule.use_k, rule.use_k ? (uint64_t)rule.k : target_p, w_all, n_all);
-            const int found = sh.found < 0 ? limit - 1 : sh.found;
-            b0 = rule.use_k ? (rule.use_p ? found : sp_min(found, bin_m)) : sp_min(found + SP_PER_BINADE, bin_m);
+        for (int i = 0; i < SP_PER; ++i) {
+            w[i] = mine.weight(a, row, rule, i);
+            sum += w[i];
         }
-        // 2  numbers and weights of the bins down to there; more of them while a share of the weight is not reached
+        sp_scan(sh.scan, sum, 0, w0, n0, w_all, n_all);
+        const uint64_t target = sp_target(a, row, w_all);
+#pragma unroll
+        for (int i = 0; i < SP_PER; ++i) {
+            if (w0 <= target && target < w0 + w[i]) { sh.scan.found = mine.first + i; sh.scan.found_w = target - w0; }
+            w0 += w[i];
+        }
+        __syncthreads();
+        if (wave == 0) {
+            int id;
+            float logit;
+            const int64_t first = sh.scan.found * a.gran;
+            sp_pick(a, z, vec, first, sp_min(first + a.gran, a.C), sh.scan.found_w, top, c, ~(uint64_t)0, 0, id, logit);
+            if (lane == 0) sp_result(a, row, id, logit, top, c, w_all);
+        }
+        return;
+    }
+    // 1  down to which bin granules and classes have to be looked at
+    const float c32 = sp_c32(rule);
+    const int limit = sp_limit(a), bin_m = sp_bin_m(a, rule);
+    int b0 = bin_m;
+    uint64_t target_p = 0;
+    if (rule.use_k || rule.use_p) {
+        sp_clear(sh.n, sh.w);
+        uint64_t sum = 0;
+#pragma unroll
+        for (int i = 0; i < SP_PER; ++i) {
+            const int b = sp_bin(mine.top[i], top, c32);
+            if (b >= limit) continue;
+            atomicAdd(&sh.n[b], 1u);
+            if (!rule.use_k) {
+                const uint64_t w = mine.weight(a, row, rule, i);
+                sum += w;
+                atomicAdd((unsigned long long *)&sh.w[b], (unsigned long long)w);
+            }
+        }
+        if (!rule.use_k) {
+            sp_scan(sh.scan, sum, 0, w0, n0, w_all, n_all);
+            target_p = sp_share(rule.p, w_all);
+        }
+        sp_find(sh.scan, sh.n, sh.w, rule.use_k, rule.use_k ? (uint64_t)rule.k : target_p, w_all, n_all);
+        const int found = sh.scan.found < 0 ? limit - 1 : sh.scan.found;
+        b0 = rule.use_k ? (rule.use_p ? found : sp_min(found, bin_m)) : sp_min(found + SP_PER_BINADE / 2, bin_m);
+    }
+    // 2  the classes down to there in order, and their running weight; more of them while a share of the weight is not reached
+    constexpr int EACH = SP_CAND / SP_NT;
+    int n;
+    uint64_t w[EACH];
+    for (;;) {
+        if (rule.use_k && rule.k > SP_CAND) { // b0 has more than k
+            n = SP_CAND + 1;
+        } else {
+            if (threadIdx.x == 0) sh.fill = 0;
+            const int n_list = sp_list(mine, sh.scan, c32, b0, sh.list);
+            sp_over_list(a, z, vec, sh.list, n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const bool in = sp_bin(v[i], top, c32) <= b0;
+                    const uint64_t who = __ballot(in);
+                    if (who == 0) continue;
+                    uint32_t at = 0;
+                    const int leader = __ffsll((unsigned long long)who) - 1;
+                    if (lane == leader) at = atomicAdd(&sh.fill, (uint32_t)__popcll(who));
+                    at = __builtin_amdgcn_readlane(at, leader) + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+                    if (in && at < SP_CAND) sh.cand[at] = sp_place(v[i], id + i);
+                }
+            });
+            __syncthreads();
+            n = (int)sh.fill;
+        }
+        if (n > SP_CAND) { // more than LDS holds
+            if (threadIdx.x == 0) a.many[row] = 1;
+            return;
+        }
+        int size = 64;
+        while (size < n) size <<= 1;
+        for (int i = n + threadIdx.x; i < size; i += SP_NT) sh.cand[i] = ~(uint64_t)0;
+        __syncthreads();
+        sp_sort(sh.cand, size);
+        uint64_t sum = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int at = threadIdx.x * EACH + i;
+            w[i] = at < n ? sp_weight(sp_place_z(sh.cand[at]), top, c, a.bits) : 0;
+            sum += w[i];
+        }
+        sp_scan(sh.scan, sum, 0, w0, n0, w_all, n_all);
+        if (!rule.use_p || rule.use_k || w_all >= target_p || b0 >= bin_m) break;
+        b0 = sp_min(b0 + 2 * SP_PER_BINADE, bin_m);
+    }
+    // 3  how many of them top-k, then top-p and min-p keep, and their weight
+    int keep = rule.use_k && rule.k < n ? (int)rule.k : n;
+    if (rule.use_p) {
+        if (rule.use_k) { // the share is one of the weight that top-k keeps
+            uint64_t run = w0;
+            __syncthreads();
+            if (threadIdx.x == 0) sh.scan.found_w = w_all;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                run += w[i];
+                if (threadIdx.x * EACH + i == keep - 1) sh.scan.found_w = run;
+            }
+            __syncthreads();
+            target_p = sp_share(rule.p, sh.scan.found_w);
+        }
+        uint64_t run = w0;
+        __syncthreads();
+        if (threadIdx.x == 0) sh.scan.found = n;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            if (run < target_p && target_p <= run + w[i]) sh.scan.found = threadIdx.x * EACH + i + 1;
+            run += w[i];
+        }
+        __syncthreads();
+        keep = sp_min(keep, sh.scan.found);
+    }
+    const uint64_t floor_w = sp_floor(a, rule);
+    uint64_t kept = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (threadIdx.x * EACH + i >= keep || w[i] < floor_w) w[i] = 0;
+        kept += w[i];
+    }
+    // 4  by id: the range of ids, then the class, at which the running weight exceeds the target
+    int shift = 0;
+    while ((a.C - 1) >> shift >= SP_BINS) ++shift;
+    sp_clear(sh.n, sh.w);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+        if (w[i]) atomicAdd((unsigned long long *)&sh.w[(uint32_t)sh.cand[threadIdx.x * EACH + i] >> shift], (unsigned long long)w[i]);
+    sp_scan(sh.scan, kept, 0, w0, n0, w_all, n_all);
+    const uint64_t target = sp_target(a, row, w_all);
+    uint64_t unused;
+    sp_find(sh.scan, sh.n, sh.w, false, target + 1, unused, n_all);
+    const uint64_t rest = target - sh.scan.found_w;
+    const uint32_t range = (uint32_t)sh.scan.found;
+    if (threadIdx.x == 0) sh.fill = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+        if (w[i] && (uint32_t)sh.cand[threadIdx.x * EACH + i] >> shift == range) {
+            const uint32_t at = atomicAdd(&sh.fill, 1u);
+            sh.list[at] = threadIdx.x * EACH + i;
+        }
+    __syncthreads();
+    const int members = (int)sh.fill;
+    for (int i = threadIdx.x; i < members; i += SP_NT) {
+        const uint64_t place = sh.cand[sh.list[i]];
+        uint64_t before = 0;
+        for (int j = 0; j < members; ++j) {
+            const uint64_t other = sh.cand[sh.list[j]];
+            if ((uint32_t)other < (uint32_t)place) before += sp_weight(sp_place_z(other), top, c, a.bits);
+        }
+        const float logit = sp_place_z(place);
+        if (before <= rest && rest < before + sp_weight(logit, top, c, a.bits)) sp_result(a, row, (int)(uint32_t)place, logit, top, c, w_all);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// rows of which more may be kept than LDS holds
+// ------------------------------------------------------------------------------------------------
+struct SpMany {
+    SpScan scan;
+    uint32_t n[SP_BINS];   // of the bins: classes (at first: granules), and their weight
+    uint64_t w[SP_BINS];
+    union {
+        uint64_t cand[SP_GRANULES]; // places of the classes of one bin
+        struct {
+            uint32_t n[SP_BINS];
+            uint64_t w[SP_BINS];
+        } sub;                      // parts of a bin that has too many
+    };
+    uint64_t g_w[SP_GRANULES]; // kept weight of the listed granules
+    int32_t list[SP_GRANULES];
+    int n_list;
+    uint32_t fill;
+    uint64_t place;
+};
+#define SP_MANY_CAND SP_GRANULES
+
+// Of the listed classes of bin `bin`, which are sh.n[bin]: the place of the one at which the running number or weight reaches `target`, in
+// the order; `weight`: their weight up to it.  Too many for LDS (a bin of equal logits) are cut into parts of equal ranges of places first.
+template <typename T>
+__device__ __forceinline__ uint64_t sp_refine(const SpArgs &a, const T *z, bool vec, SpMany &sh, float top, double c, float c32, int bin, bool by_n, uint64_t target,
+                                           uint64_t &weight) {
+    uint64_t lo = 0, hi = ~(uint64_t)0, before = 0;
+    uint32_t n = sh.n[bin];
+    while (n > SP_MANY_CAND) {
+        uint64_t least = ~(uint64_t)0, most = 0;
+        sp_over_list(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint64_t place = sp_place(v[i], id + i);
+                if (sp_bin(v[i], top, c32) != bin || place < lo || place > hi) continue;
+                least = sp_min(least, place);
+                most = sp_max(most, place);
+            }
+        });
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            least = sp_min(least, (uint64_t)__shfl_xor((unsigned long long)least, d));
+            most = sp_max(most, (uint64_t)__shfl_xor((unsigned long long)most, d));
+        }
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) { sh.scan.w[threadIdx.x >> 6] = least; sh.scan.v[threadIdx.x >> 6] = most; }
+        __syncthreads();
+        for (int i = 0; i < SP_WAVES; ++i) { least = sp_min(least, sh.scan.w[i]); most = sp_max(most, sh.scan.v[i]); }
+        int shift = 0;
+        while ((most - least) >> shift >= SP_BINS) ++shift;
+        sp_clear(sh.sub.n, sh.sub.w);
+        sp_over_list(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+#pragma unroll 1
+            for (int i = 0; i < 8; ++i) {
+                const uint64_t place = sp_place(v[i], id + i);
+                if (sp_bin(v[i], top, c32) != bin || place < least || place > most) continue;
+                const int part = (int)((place - least) >> shift);
+                atomicAdd(&sh.sub.n[part], 1u);
+                atomicAdd((unsigned long long *)&sh.sub.w[part], (unsigned long long)sp_weight(v[i], top, c, a.bits));
+            }
+        });
         uint64_t w_all;
         uint32_t n_all;
-        for (;;) {
-            int mine = 0;
-            bool in[SP_PER];
+        sp_find(sh.scan, sh.sub.n, sh.sub.w, by_n, target, w_all, n_all);
+        const int part = sh.scan.found; // there is one: the target lies within the bin
+        lo = least + ((uint64_t)part << shift);
+        hi = sp_min(most, lo + (((uint64_t)1 << shift) - 1));
+        n = sh.sub.n[part];
+        target -= by_n ? sh.scan.found_n : sh.scan.found_w;
+        before += sh.scan.found_w;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) { sh.fill = 0; sh.place = 0; sh.scan.found_w = 0; }
+    int size = 64;
+    while (size < (int)n) size <<= 1;
+    for (int i = n + threadIdx.x; i < size; i += SP_NT) sh.cand[i] = ~(uint64_t)0;
+    __syncthreads();
+    sp_over_list(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < SP_PER; ++i) {
-                in[i] = sp_bin(my_max[i], top, c32) <= b0;
-                mine += in[i];
-            }
-            uint32_t at, n_list;
-            sp_scan(sh, 0, (uint32_t)mine, w0, at, w_all, n_list);
-#pragma unroll
-            for (int i = 0; i < SP_PER; ++i)
-                if (in[i]) sh.list[at++] = threadIdx.x * per + i;
-            if (threadIdx.x == 0) sh.n_list = (int)n_list;
-            sp_clear(sh.n, sh.w);
-            if (!rule.use_k && !rule.use_p) break; // min-p alone
-            sp_over_list(a, z, vec, sh, [&](float v, uint32_t) __attribute__((always_inline)) {
-                const int b = sp_bin(v, top, c32);
-                if (b > b0) return;
-                atomicAdd(&sh.n[b], 1u);
-                atomicAdd((unsigned long long *)&sh.w[b], (unsigned long long)sp_weight(v, top, c, a.bits));
-            });
-            if (rule.use_k) break;
-            sp_find(sh, sh.n, sh.w, false, target_p, w_all, n_all);
-            if (sh.found >= 0 || b0 >= bin_m) break;
-            b0 = (int)n_list * 2 > a.nseg ? bin_m : sp_min(b0 + 2 * SP_PER_BINADE, bin_m);
+        for (int i = 0; i < 8; ++i) {
+            const uint64_t place = sp_place(v[i], id + i);
+            if (sp_bin(v[i], top, c32) != bin || place < lo || place > hi) continue;
+            const uint32_t at = atomicAdd(&sh.fill, 1u);
+            if (at < n) sh.cand[at] = place;
         }
-        // 3  the last class that top-k, then top-p keeps
+    });
+    __syncthreads();
+    sp_sort(sh.cand, size);
+    constexpr int EACH = SP_MANY_CAND / SP_NT;
+    uint64_t w[EACH], mine = 0, w0, w_all;
+    uint32_t unused, unused_all;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int at = threadIdx.x * EACH + i;
+        w[i] = at < (int)n ? sp_weight(sp_place_z(sh.cand[at]), top, c, a.bits) : 0;
+        mine += w[i];
+    }
+    sp_scan(sh.scan, mine, 0, w0, unused, w_all, unused_all);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int at = threadIdx.x * EACH + i;
+        if (at < (int)n && (by_n ? at + 1 == (int)target : w0 < target && target <= w0 + w[i])) {
+            sh.place = sh.cand[at];
+            sh.scan.found_w = w0 + w[i];
+        }
+        w0 += w[i];
+    }
+    __syncthreads();
+    weight = before + sh.scan.found_w;
+    return sh.place;
+}
+
+// A workgroup per row: numbers and weights of the bins, the bin in which top-k or top-p ends in order, what is kept of every granule, the class.
+template <typename T>
+__global__ void __launch_bounds__(SP_NT)
+sp_many_kernel(SpArgs a) {
+    __shared__ SpMany sh;
+    const int row = a.row0 + blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (!a.many[row]) return;
+    const SpRule rule(a, row);
+    bool vec;
+    const T *const z = sp_row<T>(a, row, vec);
+    const SpMine mine(a, row, sh.scan);
+    const float top = mine.row_top;
+    const double c = rule.c;
+    const float c32 = sp_c32(rule);
+    const int limit = sp_limit(a);
+    int b0 = sp_bin_m(a, rule);
+    uint64_t w0, w_all, target_p = 0;
+    uint32_t n0, n_all;
+    if (rule.use_k) {
+        sp_clear(sh.n, sh.w);
+#pragma unroll
+        for (int i = 0; i < SP_PER; ++i) {
+            const int b = sp_bin(mine.top[i], top, c32);
+            if (b < limit) atomicAdd(&sh.n[b], 1u);
+        }
+        sp_find(sh.scan, sh.n, sh.w, true, (uint64_t)rule.k, w_all, n_all);
+        const int found = sh.scan.found < 0 ? limit - 1 : sh.scan.found;
+        b0 = rule.use_p ? found : sp_min(found, b0);
+    } else if (rule.use_p) {
+        uint64_t sum = 0;
+#pragma unroll
+        for (int i = 0; i < SP_PER; ++i) sum += mine.weight(a, row, rule, i);
+        sp_scan(sh.scan, sum, 0, w0, n0, w_all, n_all);
+        target_p = sp_share(rule.p, w_all);
+    }
+    const int n_list = sp_list(mine, sh.scan, c32, b0, sh.list);
+    if (threadIdx.x == 0) sh.n_list = n_list;
+    sp_clear(sh.n, sh.w);
+    uint64_t cut = ~(uint64_t)0;
+    if (rule.use_k || rule.use_p) {
+        sp_over_list(a, z, vec, sh.list, n_list, [&](const float (&v)[8], uint32_t) __attribute__((always_inline)) {
+#pragma unroll 2
+            for (int i = 0; i < 8; ++i) {
+                const int b = sp_bin(v[i], top, c32);
+                if (b > b0) continue;
+                atomicAdd(&sh.n[b], 1u);
+                atomicAdd((unsigned long long *)&sh.w[b], (unsigned long long)sp_weight(v[i], top, c, a.bits));
+            }
+        });
         if (rule.use_k) {
-            sp_find(sh, sh.n, sh.w, true, (uint64_t)rule.k, w_all, n_all);
-            if (sh.found >= 0) {
-                const uint64_t before = sh.found_w;
+            sp_find(sh.scan, sh.n, sh.w, true, (uint64_t)rule.k, w_all, n_all);
+            if (sh.scan.found >= 0) {
+                const uint64_t before = sh.scan.found_w;
                 uint64_t w;
-                cut = sp_refine(a, z, vec, sh, top, c, c32, sh.found, true, (uint64_t)rule.k - sh.found_n, w);
+                cut = sp_refine(a, z, vec, sh, top, c, c32, sh.scan.found, true, (uint64_t)rule.k - sh.scan.found_n, w);
                 w_all = before + w;
             }
-            target_p = sp_max((uint64_t)ceil(rule.p * (double)w_all), (uint64_t)1);
+            target_p = sp_share(rule.p, w_all);
         }
         if (rule.use_p) {
             uint64_t all;
-            sp_find(sh, sh.n, sh.w, false, target_p, all, n_all);
-            if (sh.found >= 0) {
+            sp_find(sh.scan, sh.n, sh.w, false, target_p, all, n_all);
+            if (sh.scan.found >= 0) {
                 uint64_t w;
-                cut = sp_min(cut, sp_refine(a, z, vec, sh, top, c, c32, sh.found, false, target_p - sh.found_w, w));
+                cut = sp_min(cut, sp_refine(a, z, vec, sh, top, c, c32, sh.scan.found, false, target_p - sh.scan.found_w, w));
             }
         }
-        if (rule.use_m) floor_w = sp_max((uint64_t)ceil((double)rule.m * (double)(1ull << a.bits)), (uint64_t)1);
-        // 4  what is kept of each listed segment
-        __syncthreads();
-        for (int i = wave; i < sh.n_list; i += SP_WAVES) {
-            const int64_t first = sh.list[i] * a.seg, last = sp_min(first + a.seg, a.C);
-            uint64_t sum = 0;
-            for (int64_t e = first; e < last; e += SP_CHUNK) {
-                float v[8];
-                sp_load(z, vec, e + lane * 8, a.C, v);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    if (sp_bin(v[j], top, c32) > b0 || sp_place(v[j], (uint32_t)(e + lane * 8 + j)) > cut) continue;
-                    const uint64_t w = sp_weight(v[j], top, c, a.bits);
-                    if (w >= floor_w) sum += w;
-                }
-            }
-            sum = sp_wave_scan(sum);
-            if (lane == 63) sh.seg_w[i] = sum;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < SP_PER; ++i)
-            if (threadIdx.x * SP_PER + i < sh.n_list) my_w[i] = sh.seg_w[threadIdx.x * SP_PER + i];
     }
-    // the segment, then the class, at which the running weight exceeds u times all of it
-    uint64_t mine = 0;
-#pragma unroll
-    for (int i = 0; i < SP_PER; ++i) mine += my_w[i];
-    sp_scan(sh, mine, 0, w0, unused_n, all_w, unused_all);
-    const double share = fmax((double)a.u[row], 0.0) * (double)all_w;
-    const uint64_t target = share >= (double)all_w ? all_w - 1 : sp_min((uint64_t)share, all_w - 1);
+    const uint64_t floor_w = sp_floor(a, rule);
+    for (int i = threadIdx.x; i < n_list; i += SP_NT) sh.g_w[i] = 0;
+    __syncthreads();
+    const int at_once = SP_NT >> a.lg;
+    int turn = 0; // which of its granules a thread is at
+    sp_over_list(a, z, vec, sh.list, n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+        uint64_t sum = 0;
+#pragma unroll 2
+        for (int i = 0; i < 8; ++i) {
+            if (sp_bin(v[i], top, c32) > b0 || sp_place(v[i], id + i) > cut) continue;
+            const uint64_t w = sp_weight(v[i], top, c, a.bits);
+            if (w >= floor_w) sum += w;
+        }
+        int at;
+        if (a.gran <= SP_CHUNK) {
+            at = turn * at_once + (threadIdx.x >> a.lg);
+            ++turn;
+        } else {
+            at = wave + turn * SP_WAVES;
+            if ((int64_t)(id - lane * 8) + SP_CHUNK >= sp_min((sh.list[at] + (int64_t)1) * a.gran, a.C)) ++turn;
+        }
+        if (sum) atomicAdd((unsigned long long *)&sh.g_w[at], (unsigned long long)sum);
+    });
+    __syncthreads();
+    uint64_t w[SP_PER], sum = 0;
 #pragma unroll
     for (int i = 0; i < SP_PER; ++i) {
-        if (w0 <= target && target < w0 + my_w[i]) {
-            sh.found = plain ? threadIdx.x * per + i : sh.list[threadIdx.x * SP_PER + i];
-            sh.found_w = target - w0;
-        }
-        w0 += my_w[i];
+        w[i] = threadIdx.x * SP_PER + i < n_list ? sh.g_w[threadIdx.x * SP_PER + i] : 0;
+        sum += w[i];
+    }
+    sp_scan(sh.scan, sum, 0, w0, n0, w_all, n_all);
+    const uint64_t target = sp_target(a, row, w_all);
+#pragma unroll
+    for (int i = 0; i < SP_PER; ++i) {
+        if (w0 <= target && target < w0 + w[i]) { sh.scan.found = sh.list[threadIdx.x * SP_PER + i]; sh.scan.found_w = target - w0; }
+        w0 += w[i];
     }
     __syncthreads();
     if (wave == 0) {
         int id;
         float logit;
-        sp_pick(a, z, vec, sh.found, sh.found_w, top, c, cut, floor_w, id, logit);
-        if (lane == 0) {
-            a.ids[row] = id;
-            if (a.logprob) // log of 2^(c (z - top)) / (all_w 2^-bits)
-                a.logprob[row] = (float)((sp_log2w(logit, top, c) - (log2((double)all_w) - a.bits)) * 0.6931471805599453);
-        }
+        const int64_t first = sh.scan.found * a.gran;
+        sp_pick(a, z, vec, first, sp_min(first + a.gran, a.C), sh.scan.found_w, top, c, cut, floor_w, id, logit);
+        if (lane == 0) sp_result(a, row, id, logit, top, c, w_all);
     }
 }
 
-static bool sp_sizes(int64_t C, int B, int64_t &seg, int &nseg, int &bits) {
+static bool sp_sizes(int64_t C, int B, SpArgs &a) {
     if (C < 1 || C >= (int64_t)1 << 31 || B < 1) return false;
-    seg = SP_CHUNK;
-    while (ks_ceil_div(C, seg) > SP_SEGS) seg *= 2;
-    nseg = (int)ks_ceil_div(C, seg);
+    a.gran = 8;
+    while (ks_ceil_div(C, a.gran) > SP_GRANULES) a.gran *= 2;
+    a.ngr = (int)ks_ceil_div(C, a.gran);
+    a.lg = 0;
+    while (a.lg < 6 && 8 << a.lg < a.gran) ++a.lg;
     int lg = 0;
     while (((int64_t)1 << lg) < C) ++lg;
-    bits = 62 - lg < 48 ? 62 - lg : 48;
+    a.bits = 62 - lg < 48 ? 62 - lg : 48;
     return true;
+}
+static void sp_places(KsArena &ws, int B, SpArgs &a) {
+    a.g_max = ws.take<float>((size_t)B * a.ngr);
+    a.g_sum = ws.take<double>((size_t)B * a.ngr);
+    a.many = ws.take<int32_t>((size_t)B);
 }
 
 extern "C" size_t class_sample_workspace(int64_t C, int B) {
-    int64_t seg;
-    int nseg, bits;
-    if (!sp_sizes(C, B, seg, nseg, bits)) return 0;
+    SpArgs a;
+    if (!sp_sizes(C, B, a)) return 0;
     KsArena ws(nullptr);
-    ws.take<float>((size_t)B * nseg);
-    ws.take<double>((size_t)B * nseg);
+    sp_places(ws, B, a);
     return ws.off;
+}
+
+template <typename T> static void sp_sample(SpArgs &a, int B, hipStream_t st) {
+    for (int64_t r = 0; r < B; r += 1 << 15) { // a launch's second dimension ends at 65,535
+        const unsigned rows = (unsigned)(B - r < 1 << 15 ? B - r : 1 << 15);
+        a.row0 = (int)r;
+        const int64_t waves = a.gran < SP_CHUNK ? ks_ceil_div(a.C, SP_CHUNK) : a.ngr;
+        const dim3 grid((unsigned)ks_ceil_div(waves, 4), rows);
+        const auto granules = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a); };
+        switch (a.lg) {
+        case 0: granules(sp_granules_kernel<0, T>); break;
+        case 1: granules(sp_granules_kernel<1, T>); break;
+        case 2: granules(sp_granules_kernel<2, T>); break;
+        case 3: granules(sp_granules_kernel<3, T>); break;
+        case 4: granules(sp_granules_kernel<4, T>); break;
+        case 5: granules(sp_granules_kernel<5, T>); break;
+        default: granules(sp_granules_kernel<6, T>);
+        }
+        hipLaunchKernelGGL(sp_draw_kernel<T>, dim3(rows), dim3(SP_NT), 0, st, a);
+        if (a.C > SP_CAND) hipLaunchKernelGGL(sp_many_kernel<T>, dim3(rows), dim3(SP_NT), 0, st, a); // else LDS holds all
+    }
 }
 
 extern "C" int class_sample(const void *logits, int64_t ldl, int dtype, int64_t C, int B, const float *u, const float *temperature,
                             const int32_t *top_k, const float *top_p, const float *min_p, int32_t *ids, float *logprob, void *ws,
                             size_t ws_bytes, void *stream) {
     SpArgs a;
-    if (!logits || !u || !ids || !ws || ldl < C || !sp_sizes(C, B, a.seg, a.nseg, a.bits)) return KS_INVALID_ARG;
+    if (!logits || !u || !ids || !ws || ldl < C || !sp_sizes(C, B, a)) return KS_INVALID_ARG;
     if (dtype != KS_DTYPE_BF16 && dtype != KS_DTYPE_FP32) return KS_INVALID_ARG;
     if ((uintptr_t)logits % (dtype == KS_DTYPE_FP32 ? 4 : 2) || (uintptr_t)ws % 256) return KS_INVALID_ARG;
     if (((uintptr_t)u | (uintptr_t)temperature | (uintptr_t)top_k | (uintptr_t)top_p | (uintptr_t)min_p | (uintptr_t)ids | (uintptr_t)logprob) % 4) return KS_INVALID_ARG;
     if (ws_bytes < class_sample_workspace(C, B)) return KS_WORKSPACE_TOO_SMALL;
     KsArena arena(ws);
-    a.seg_max = arena.take<float>((size_t)B * a.nseg);
-    a.seg_sum = arena.take<double>((size_t)B * a.nseg);
+    sp_places(arena, B, a);
     a.logits = logits; a.ldl = ldl; a.C = C;
     a.u = u; a.temperature = temperature; a.top_p = top_p; a.min_p = min_p; a.top_k = top_k;
     a.ids = ids; a.logprob = logprob;
-    for (int64_t r = 0; r < B; r += 1 << 15) { // a launch's second dimension ends at 65,535
-        const unsigned rows = (unsigned)(B - r < 1 << 15 ? B - r : 1 << 15);
-        a.row0 = (int)r;
-        const dim3 grid((unsigned)((a.nseg + 3) / 4), rows);
-        if (dtype == KS_DTYPE_FP32) {
-            hipLaunchKernelGGL(sp_segments_kernel<float>, grid, dim3(256), 0, (hipStream_t)stream, a);
-            hipLaunchKernelGGL(sp_draw_kernel<float>, dim3(rows), dim3(SP_NT), 0, (hipStream_t)stream, a);
-        } else {
-            hipLaunchKernelGGL(sp_segments_kernel<uint16_t>, grid, dim3(256), 0, (hipStream_t)stream, a);
-            hipLaunchKernelGGL(sp_draw_kernel<uint16_t>, dim3(rows), dim3(SP_NT), 0, (hipStream_t)stream, a);
-        }
-    }
+    if (dtype == KS_DTYPE_FP32) sp_sample<float>(a, B, (hipStream_t)stream);
+    else sp_sample<uint16_t>(a, B, (hipStream_t)stream);
     KS_LAUNCH_CHECK();
     return KS_OK;
 }

@@ -27,9 +27,9 @@ def test_header_symbols_are_exported(ks):
 
 def test_workspace(ks):
     assert [ks.class_sample_workspace(*a) for a in ((0, 1), (1, 0), (1 << 31, 1), ((1 << 32) + 8, 1), (8, (1 << 32) + 1), (-1, 1))] == [0] * 6
-    assert ks.class_sample_workspace(1, 1) == 512
-    assert ks.class_sample_workspace(390_625, 256) >= 763 * 256 * 12
-    assert 0 < ks.class_sample_workspace((1 << 31) - 1, 1) <= 4_096 * 12 + 512  # segments grow with the row
+    assert ks.class_sample_workspace(1, 1) == 768
+    assert ks.class_sample_workspace(390_625, 256) >= 256 * 12
+    assert 0 < ks.class_sample_workspace((1 << 31) - 1, 1) <= 4_096 * 12 + 768  # parts grow with the row
 
 
 def test_refusals(ks):
@@ -39,7 +39,7 @@ def test_refusals(ks):
                 dict(B=-1), dict(z=258), dict(z=257, dtype=0), dict(ws=260), dict(u=257), dict(t=257), dict(k=258), dict(p=257), dict(m=259), dict(ids=258),
                 dict(lp=257)):
         assert call(**bad) == ks.KS_INVALID_ARG, bad
-    assert call(size=511) == ks.KS_WORKSPACE_TOO_SMALL
+    assert call(size=767) == ks.KS_WORKSPACE_TOO_SMALL
 
 
 def test_binding_refuses_host_tensors(ks):
