@@ -9,14 +9,13 @@
 #include "../../include/class_sample.h"
 #include "ks_common.h"
 
-#define SP_NT 1024
-#define SP_WAVES (SP_NT / 64)
+#define SP_NT 256  /* threads of a row: its steps are short, and more wavefronts would only share their instructions' time */
+#define SP_NT2 1024 /* where much is kept */
 #define SP_CHUNK 512     /* classes that a wavefront takes at a time: eight consecutive ones a lane */
 #define SP_GRANULES 4096 /* most granules of a row */
-#define SP_PER (SP_GRANULES / SP_NT) /* most granules of a thread */
 #define SP_BINS 2048     /* of the weights: 32 to a factor of two */
 #define SP_PER_BINADE 32
-#define SP_CAND 8192     /* classes that are put in order in LDS */
+#define SP_CAND 4096     /* classes that are put in order in LDS */
 #define SP_NO_BIN (1 << 20)
 
 // of one type: min() and max() of the runtime's headers go through double for 64-bit numbers
@@ -32,6 +31,7 @@ struct SpArgs {
     float *g_max;  // [B, ngr]
     double *g_sum; // [B, ngr]: sum of exp((z - g_max) / T)
     int32_t *many; // [B]: the row is left to the third launch
+    int64_t most;  // classes that a row's workgroup looks at itself
     int32_t *ids;
     float *logprob;
 };
@@ -58,24 +58,29 @@ struct SpRule {
     }
 };
 
-// 2^t for t >= -200, by 2^rint(t) and the series of exp around 0: the first term left out is less than 1e-17
+// 2^t for -200 <= t < 900: the addition of 1.5 * 2^52 leaves the nearest whole number in the low bits; of the rest (at most a half) the series
+// of 2^f = exp(f ln 2), whose first term left out is less than 1e-17
+#define SP_LN2 0.69314718055994530942
+static constexpr double sp_term(int k) { return k == 0 ? 1.0 : sp_term(k - 1) * SP_LN2 / k; }
 __device__ __forceinline__ double sp_exp2(double t) {
-    const double n = rint(t), x = (t - n) * 0.6931471805599453;
-    double s = 1.0 / 6227020800.0;
-    s = __builtin_fma(s, x, 1.0 / 479001600.0);
-    s = __builtin_fma(s, x, 1.0 / 39916800.0);
-    s = __builtin_fma(s, x, 1.0 / 3628800.0);
-    s = __builtin_fma(s, x, 1.0 / 362880.0);
-    s = __builtin_fma(s, x, 1.0 / 40320.0);
-    s = __builtin_fma(s, x, 1.0 / 5040.0);
-    s = __builtin_fma(s, x, 1.0 / 720.0);
-    s = __builtin_fma(s, x, 1.0 / 120.0);
-    s = __builtin_fma(s, x, 1.0 / 24.0);
-    s = __builtin_fma(s, x, 1.0 / 6.0);
-    s = __builtin_fma(s, x, 0.5);
-    s = __builtin_fma(s, x, 1.0);
-    s = __builtin_fma(s, x, 1.0);
-    return __hiloint2double(__double2hiint(s) + ((int)n << 20), __double2loint(s));
+    const double whole = t + 6755399441055744.0, f = t - (whole - 6755399441055744.0);
+    constexpr double c1 = sp_term(1), c2 = sp_term(2), c3 = sp_term(3), c4 = sp_term(4), c5 = sp_term(5), c6 = sp_term(6), c7 = sp_term(7),
+                     c8 = sp_term(8), c9 = sp_term(9), c10 = sp_term(10), c11 = sp_term(11), c12 = sp_term(12), c13 = sp_term(13);
+    double s = c13;
+    s = __builtin_fma(s, f, c12);
+    s = __builtin_fma(s, f, c11);
+    s = __builtin_fma(s, f, c10);
+    s = __builtin_fma(s, f, c9);
+    s = __builtin_fma(s, f, c8);
+    s = __builtin_fma(s, f, c7);
+    s = __builtin_fma(s, f, c6);
+    s = __builtin_fma(s, f, c5);
+    s = __builtin_fma(s, f, c4);
+    s = __builtin_fma(s, f, c3);
+    s = __builtin_fma(s, f, c2);
+    s = __builtin_fma(s, f, c1);
+    s = __builtin_fma(s, f, 1.0);
+    return __hiloint2double(__double2hiint(s) + (__double2loint(whole) << 20), __double2loint(s));
 }
 // log2 of the weight of z relative to that of ref, -200 for less: infinities of either sign, and 0 times them, end there
 __device__ __forceinline__ double sp_log2w(float z, float ref, double c) {
@@ -183,27 +188,30 @@ sp_granules_kernel(SpArgs a) {
     if (writes) a.g_sum[(int64_t)row * a.ngr + g] = sum;
 }
 
-// inclusive sum over the wavefront
+// inclusive sum over the wavefront, as ks_wave_iscan
+template <int CTRL, int ROWS> __device__ __forceinline__ uint64_t sp_moved(uint64_t v) {
+    return (uint64_t)(uint32_t)KS_DPP(0, (int)(v >> 32), CTRL, ROWS) << 32 | (uint32_t)KS_DPP(0, (int)(uint32_t)v, CTRL, ROWS);
+}
 __device__ __forceinline__ uint64_t sp_wave_scan(uint64_t v) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t o = __shfl_up((unsigned long long)v, d);
-        if (lane >= d) v += o;
-    }
+    v += sp_moved<0x111, 0xf>(v);
+    v += sp_moved<0x112, 0xf>(v);
+    v += sp_moved<0x114, 0xf>(v);
+    v += sp_moved<0x118, 0xf>(v);
+    v += sp_moved<0x142, 0xa>(v);
+    v += sp_moved<0x143, 0xc>(v);
     return v;
 }
 
 struct SpScan {
-    uint64_t w[SP_WAVES], v[SP_WAVES];
-    uint32_t n[SP_WAVES];
+    uint64_t w[16], v[16]; // of wavefronts
+    uint32_t n[16];
     uint64_t found_w;
     uint32_t found_n;
     int found;
 };
 
 // exclusive sums over the workgroup of a weight and a number a thread, and their totals
-__device__ __forceinline__ void sp_scan(SpScan &sh, uint64_t w, uint32_t n, uint64_t &w0, uint32_t &n0, uint64_t &w_all, uint32_t &n_all) {
+template <int NT> __device__ __forceinline__ void sp_scan(SpScan &sh, uint64_t w, uint32_t n, uint64_t &w0, uint32_t &n0, uint64_t &w_all, uint32_t &n_all) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint64_t wi = sp_wave_scan(w);
     const uint32_t ni = (uint32_t)ks_wave_iscan((int)n);
@@ -212,70 +220,66 @@ __device__ __forceinline__ void sp_scan(SpScan &sh, uint64_t w, uint32_t n, uint
     __syncthreads();
     w0 = wi - w; n0 = ni - n; w_all = 0; n_all = 0;
 #pragma unroll
-    for (int i = 0; i < SP_WAVES; ++i) {
+    for (int i = 0; i < NT / 64; ++i) {
         if (i < wave) { w0 += sh.w[i]; n0 += sh.n[i]; }
         w_all += sh.w[i];
         n_all += sh.n[i];
     }
 }
-__device__ __forceinline__ float sp_block_max(SpScan &sh, float v) {
+template <int NT> __device__ __forceinline__ uint64_t sp_total(SpScan &sh, uint64_t w) {
+    uint64_t w0, w_all;
+    uint32_t n0, n_all;
+    sp_scan<NT>(sh, w, 0, w0, n0, w_all, n_all);
+    return w_all;
+}
+template <int NT> __device__ __forceinline__ float sp_block_max(SpScan &sh, float v) {
     v = ks_wave_max(v);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) sh.n[threadIdx.x >> 6] = __float_as_uint(v);
     __syncthreads();
     v = __uint_as_float(sh.n[0]);
 #pragma unroll
-    for (int i = 1; i < SP_WAVES; ++i) v = fmaxf(v, __uint_as_float(sh.n[i]));
+    for (int i = 1; i < NT / 64; ++i) v = fmaxf(v, __uint_as_float(sh.n[i]));
     return v;
 }
-__device__ __forceinline__ void sp_clear(uint32_t *n, uint64_t *w) {
+template <int NT> __device__ __forceinline__ void sp_clear(uint32_t *n, uint64_t *w) {
     __syncthreads();
-    for (int i = threadIdx.x; i < SP_BINS; i += SP_NT) { n[i] = 0; w[i] = 0; }
+#pragma unroll
+    for (int i = 0; i < SP_BINS / NT; ++i) { n[i * NT + threadIdx.x] = 0; w[i * NT + threadIdx.x] = 0; }
     __syncthreads();
 }
 // The first bin at which the running number (by_n) or weight reaches `target` >= 1: found (-1: none does), and what lies before it;
 // the totals.
+template <int NT>
 __device__ __forceinline__ void sp_find(SpScan &sh, const uint32_t *n, const uint64_t *w, bool by_n, uint64_t target, uint64_t &w_all, uint32_t &n_all) {
     __syncthreads();
     if (threadIdx.x == 0) sh.found = -1;
-    constexpr int EACH = SP_BINS / SP_NT;
+    constexpr int EACH = SP_BINS / NT;
     const int b = threadIdx.x * EACH;
     uint64_t w0, w_mine = 0;
     uint32_t n0, n_mine = 0;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) { w_mine += w[b + i]; n_mine += n[b + i]; }
-    sp_scan(sh, w_mine, n_mine, w0, n0, w_all, n_all);
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        const uint64_t before = by_n ? n0 : w0, size = by_n ? n[b + i] : w[b + i];
-        if (before < target && target <= before + size) { sh.found = b + i; sh.found_n = n0; sh.found_w = w0; }
-        n0 += n[b + i];
-        w0 += w[b + i];
-    }
+    sp_scan<NT>(sh, w_mine, n_mine, w0, n0, w_all, n_all);
+    const uint64_t before = by_n ? n0 : w0, mine = by_n ? n_mine : w_mine;
+    if (before < target && target <= before + mine) // one thread
+        for (int i = 0;; ++i) {
+            if (target <= (by_n ? n0 + n[b + i] : w0 + w[b + i])) {
+                sh.found = b + i;
+                sh.found_n = n0;
+                sh.found_w = w0;
+                break;
+            }
+            n0 += n[b + i];
+            w0 += w[b + i];
+        }
     __syncthreads();
 }
 
-// granules of a workgroup's threads, SP_PER consecutive ones each
-struct SpMine {
-    float top[SP_PER], row_top;
-    int first, n; // of the thread
-    __device__ __forceinline__ SpMine(const SpArgs &a, int row, SpScan &sh) {
-        const int per = (a.ngr + SP_NT - 1) / SP_NT;
-        first = threadIdx.x * per;
-        n = sp_max(0, sp_min(per, a.ngr - first));
-        row_top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < SP_PER; ++i) {
-            top[i] = i < n ? a.g_max[(int64_t)row * a.ngr + first + i] : -INFINITY;
-            row_top = fmaxf(row_top, top[i]);
-        }
-        row_top = sp_block_max(sh, row_top);
-    }
-    // weight of granule i
-    __device__ __forceinline__ uint64_t weight(const SpArgs &a, int row, const SpRule &rule, int i) const {
-        return top[i] > -INFINITY ? (uint64_t)(a.g_sum[(int64_t)row * a.ngr + first + i] * sp_exp2(sp_log2w(top[i], row_top, rule.c) + a.bits) + 0.5) : 0;
-    }
-};
+// weight of granule g of a row, whose largest logit is `z`
+__device__ __forceinline__ uint64_t sp_mass(const SpArgs &a, int row, int g, float z, float top, double c) {
+    return z > -INFINITY ? (uint64_t)(a.g_sum[(int64_t)row * a.ngr + g] * sp_exp2(sp_log2w(z, top, c) + a.bits) + 0.5) : 0;
+}
 __device__ __forceinline__ float sp_c32(const SpRule &rule) { return (float)(rule.c * SP_PER_BINADE); }
 __device__ __forceinline__ int sp_limit(const SpArgs &a) { return (a.bits + 1) * SP_PER_BINADE; } // from this bin on weights are 0
 __device__ __forceinline__ int sp_bin_m(const SpArgs &a, const SpRule &rule) { // last bin with weights of m or more
@@ -357,9 +361,9 @@ template <typename T> __device__ __forceinline__ int sp_first(const SpArgs &a, c
 }
 
 // f(z, id) for eight classes a thread of the n listed granules; all lanes of a wavefront call it together
-template <typename T, typename F> __device__ __forceinline__ void sp_over_list(const SpArgs &a, const T *z, bool vec, const int32_t *list, int n, F f) {
+template <int NT, typename T, typename F> __device__ __forceinline__ void sp_over_list(const SpArgs &a, const T *z, bool vec, const int32_t *list, int n, F f) {
     if (a.gran <= SP_CHUNK) {
-        const int lanes = 1 << a.lg, at_once = SP_NT >> a.lg, sub = threadIdx.x & (lanes - 1);
+        const int lanes = 1 << a.lg, at_once = NT >> a.lg, sub = threadIdx.x & (lanes - 1);
         for (int i0 = 0; i0 < n; i0 += at_once) {
             const int i = i0 + (threadIdx.x >> a.lg);
             float v[8];
@@ -369,7 +373,7 @@ template <typename T, typename F> __device__ __forceinline__ void sp_over_list(c
         }
     } else {
         const int lane = threadIdx.x & 63;
-        for (int i = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < n; i += SP_WAVES) {
+        for (int i = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < n; i += NT / 64) {
             const int64_t first = list[i] * a.gran, last = sp_min(first + a.gran, a.C);
             for (int64_t e = first + lane * 8; e - lane * 8 < last; e += SP_CHUNK) {
                 float v[8];
@@ -379,33 +383,14 @@ template <typename T, typename F> __device__ __forceinline__ void sp_over_list(c
         }
     }
 }
-// the granules whose largest logit lies in bin b0 or before, in order: list, and how many
-__device__ __forceinline__ int sp_list(const SpMine &mine, SpScan &sh, float c32, int b0, int32_t *list) {
-    bool in[SP_PER];
-    int n = 0;
-#pragma unroll
-    for (int i = 0; i < SP_PER; ++i) {
-        in[i] = sp_bin(mine.top[i], mine.row_top, c32) <= b0;
-        n += in[i];
-    }
-    uint64_t w0, w_all;
-    uint32_t at, all;
-    sp_scan(sh, 0, (uint32_t)n, w0, at, w_all, all);
-#pragma unroll
-    for (int i = 0; i < SP_PER; ++i)
-        if (in[i]) list[at++] = mine.first + i;
-    __syncthreads();
-    return (int)all;
-}
-
 // p[0 .. size) into ascending order (bitonic), size a power of two, at least 64.  A wavefront's 64 pairs lie within 128 numbers where they are at
 // most 64 apart: only wider steps, and the first one after them, wait for the other wavefronts.
-__device__ __forceinline__ void sp_sort(uint64_t *p, int size) {
+template <int NT> __device__ __forceinline__ void sp_sort(uint64_t *p, int size) {
     for (int k = 2; k <= size; k <<= 1)
         for (int j = k >> 1; j > 0; j >>= 1) {
             if (j >= 64) __syncthreads();
             else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            for (int i = threadIdx.x; i < size / 2; i += SP_NT) {
+            for (int i = threadIdx.x; i < size / 2; i += NT) {
                 const int x = ((i & ~(j - 1)) << 1) | (i & (j - 1)), y = x + j;
                 const uint64_t u = p[x], v = p[y];
                 if ((u > v) == ((x & k) == 0)) { p[x] = v; p[y] = u; }
@@ -416,10 +401,15 @@ __device__ __forceinline__ void sp_sort(uint64_t *p, int size) {
 
 struct SpShared {
     SpScan scan;
-    uint32_t n[SP_BINS];   // of the bins: granules, and their weight; then of ranges of ids
+    float top[SP_GRANULES]; // of the granules
+    uint32_t n[SP_BINS];    // of the bins: granules, and their weight; then of ranges of ids
     uint64_t w[SP_BINS];
     uint64_t cand[SP_CAND]; // places of classes that may be kept
-    int32_t list[SP_CAND > SP_GRANULES ? SP_CAND : SP_GRANULES]; // granules; then candidates of one range of ids
+    union {
+        int32_t list[SP_GRANULES]; // granules
+        uint64_t cand_w[SP_CAND];  // the candidates' weights, 0 for those that are not kept
+    };
+    int32_t member[SP_CAND]; // candidates of one range of ids
     uint32_t fill;
 };
 
@@ -428,12 +418,18 @@ template <typename T>
 __global__ void __launch_bounds__(SP_NT)
 sp_draw_kernel(SpArgs a) {
     __shared__ SpShared sh;
+    constexpr int NT = SP_NT;
     const int row = a.row0 + blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const SpRule rule(a, row);
     bool vec;
     const T *const z = sp_row<T>(a, row, vec);
-    const SpMine mine(a, row, sh.scan);
-    const float top = mine.row_top;
+    float top = -INFINITY;
+    for (int i = threadIdx.x; i < a.ngr; i += NT) {
+        const float t = a.g_max[(int64_t)row * a.ngr + i];
+        sh.top[i] = t;
+        top = fmaxf(top, t);
+    }
+    top = sp_block_max<NT>(sh.scan, top);
     if (threadIdx.x == 0) a.many[row] = 0;
     if (!(top > -INFINITY)) {
         if (threadIdx.x == 0) {
@@ -445,12 +441,14 @@ sp_draw_kernel(SpArgs a) {
     const double c = rule.c;
     uint64_t w0, w_all;
     uint32_t n0, n_all;
+    // consecutive granules of a thread
+    const int per = (a.ngr + NT - 1) / NT, g0 = sp_min((int)threadIdx.x * per, a.ngr), g1 = sp_min(g0 + per, a.ngr);
+    const auto mass = [&](int g) __attribute__((always_inline)) { return sp_mass(a, row, g, sh.top[g], top, c); };
     if (rule.greedy) { // the first class with the largest logit: the only one that is kept
         if (threadIdx.x == 0) sh.fill = 0x7FFFFFFF;
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < SP_PER; ++i)
-            if (mine.top[i] == top) atomicMin(&sh.fill, (uint32_t)(mine.first + i));
+        for (int g = g1 - 1; g >= g0; --g)
+            if (sh.top[g] == top) atomicMin(&sh.fill, (uint32_t)g);
         __syncthreads();
         if (wave == 0) {
             const int64_t first = sh.fill * a.gran;
@@ -463,19 +461,16 @@ sp_draw_kernel(SpArgs a) {
         return;
     }
     if (!rule.use_k && !rule.use_p && !rule.use_m) { // all classes: the granules' weights say where to look
-        uint64_t w[SP_PER], sum = 0;
-#pragma unroll
-        for (int i = 0; i < SP_PER; ++i) {
-            w[i] = mine.weight(a, row, rule, i);
-            sum += w[i];
-        }
-        sp_scan(sh.scan, sum, 0, w0, n0, w_all, n_all);
+        uint64_t sum = 0;
+        for (int g = g0; g < g1; ++g) sum += mass(g);
+        sp_scan<NT>(sh.scan, sum, 0, w0, n0, w_all, n_all);
         const uint64_t target = sp_target(a, row, w_all);
-#pragma unroll
-        for (int i = 0; i < SP_PER; ++i) {
-            if (w0 <= target && target < w0 + w[i]) { sh.scan.found = mine.first + i; sh.scan.found_w = target - w0; }
-            w0 += w[i];
-        }
+        if (w0 <= target && target < w0 + sum) // one thread
+            for (int g = g0; g < g1; ++g) {
+                const uint64_t w = mass(g);
+                if (target < w0 + w) { sh.scan.found = g; sh.scan.found_w = target - w0; break; }
+                w0 += w;
+            }
         __syncthreads();
         if (wave == 0) {
             int id;
@@ -492,49 +487,50 @@ sp_draw_kernel(SpArgs a) {
     int b0 = bin_m;
     uint64_t target_p = 0;
     if (rule.use_k || rule.use_p) {
-        sp_clear(sh.n, sh.w);
+        sp_clear<NT>(sh.n, sh.w);
         uint64_t sum = 0;
-#pragma unroll
-        for (int i = 0; i < SP_PER; ++i) {
-            const int b = sp_bin(mine.top[i], top, c32);
+        for (int g = g0; g < g1; ++g) {
+            const int b = sp_bin(sh.top[g], top, c32);
             if (b >= limit) continue;
             atomicAdd(&sh.n[b], 1u);
             if (!rule.use_k) {
-                const uint64_t w = mine.weight(a, row, rule, i);
+                const uint64_t w = mass(g);
                 sum += w;
                 atomicAdd((unsigned long long *)&sh.w[b], (unsigned long long)w);
             }
         }
-        if (!rule.use_k) {
-            sp_scan(sh.scan, sum, 0, w0, n0, w_all, n_all);
-            target_p = sp_share(rule.p, w_all);
-        }
-        sp_find(sh.scan, sh.n, sh.w, rule.use_k, rule.use_k ? (uint64_t)rule.k : target_p, w_all, n_all);
+        if (!rule.use_k) target_p = sp_share(rule.p, sp_total<NT>(sh.scan, sum));
+        sp_find<NT>(sh.scan, sh.n, sh.w, rule.use_k, rule.use_k ? (uint64_t)rule.k : target_p, w_all, n_all);
         const int found = sh.scan.found < 0 ? limit - 1 : sh.scan.found;
         b0 = rule.use_k ? (rule.use_p ? found : sp_min(found, bin_m)) : sp_min(found + SP_PER_BINADE / 2, bin_m);
     }
     // 2  the classes down to there in order, and their running weight; more of them while a share of the weight is not reached
-    constexpr int EACH = SP_CAND / SP_NT;
-    int n;
-    uint64_t w[EACH];
+    int n, c0, c1; // consecutive candidates of a thread
     for (;;) {
-        if (rule.use_k && rule.k > SP_CAND) { // b0 has more than k
-            n = SP_CAND + 1;
-        } else {
+        uint32_t listed = 0;
+        for (int g = g0; g < g1; ++g) listed += sp_bin(sh.top[g], top, c32) <= b0;
+        sp_scan<NT>(sh.scan, 0, listed, w0, n0, w_all, n_all);
+        if (n_all > SP_CAND || (rule.use_k && rule.k > SP_CAND) || n_all * a.gran > a.most) n = SP_CAND + 1; // a class of each granule is in
+        else {
             if (threadIdx.x == 0) sh.fill = 0;
-            const int n_list = sp_list(mine, sh.scan, c32, b0, sh.list);
-            sp_over_list(a, z, vec, sh.list, n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+            for (int g = g0; g < g1; ++g)
+                if (sp_bin(sh.top[g], top, c32) <= b0) sh.list[n0++] = g;
+            __syncthreads();
+            sp_over_list<NT>(a, z, vec, sh.list, (int)n_all, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+                uint32_t in = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const bool in = sp_bin(v[i], top, c32) <= b0;
-                    const uint64_t who = __ballot(in);
-                    if (who == 0) continue;
-                    uint32_t at = 0;
-                    const int leader = __ffsll((unsigned long long)who) - 1;
-                    if (lane == leader) at = atomicAdd(&sh.fill, (uint32_t)__popcll(who));
-                    at = __builtin_amdgcn_readlane(at, leader) + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
-                    if (in && at < SP_CAND) sh.cand[at] = sp_place(v[i], id + i);
-                }
+                for (int i = 0; i < 8; ++i) in |= (uint32_t)(sp_bin(v[i], top, c32) <= b0) << i;
+                if (__ballot(in) == 0) return;
+                const uint32_t mine = __popc(in), upto = (uint32_t)ks_wave_iscan((int)mine);
+                uint32_t at = 0;
+                if (lane == 63) at = atomicAdd(&sh.fill, upto);
+                at = __builtin_amdgcn_readlane(at, 63) + upto - mine;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (in >> i & 1) {
+                        if (at < SP_CAND) sh.cand[at] = sp_place(v[i], id + i);
+                        ++at;
+                    }
             });
             __syncthreads();
             n = (int)sh.fill;
@@ -543,95 +539,143 @@ sp_draw_kernel(SpArgs a) {
             if (threadIdx.x == 0) a.many[row] = 1;
             return;
         }
-        int size = 64;
-        while (size < n) size <<= 1;
-        for (int i = n + threadIdx.x; i < size; i += SP_NT) sh.cand[i] = ~(uint64_t)0;
-        __syncthreads();
-        sp_sort(sh.cand, size);
-        uint64_t sum = 0;
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int at = threadIdx.x * EACH + i;
-            w[i] = at < n ? sp_weight(sp_place_z(sh.cand[at]), top, c, a.bits) : 0;
-            sum += w[i];
+        if (n <= NT) { // a candidate's place in the order is the number of those before it; several threads count for one where there are few
+            const int lg = n <= 64 ? 6 : n <= 128 ? 7 : 8, each = threadIdx.x & ((1 << lg) - 1), parts = NT >> lg, part = threadIdx.x >> lg;
+            const uint64_t place = each < n ? sh.cand[each] : 0;
+            uint32_t before = 0;
+#pragma unroll 4
+            for (int j = part; j < n; j += parts) before += sh.cand[j] < place;
+            if (threadIdx.x < NT) sh.member[threadIdx.x] = 0;
+            __syncthreads();
+            if (each < n) atomicAdd(&sh.member[each], (int)before);
+            __syncthreads();
+            if (part == 0 && each < n) sh.cand[sh.member[each]] = place;
+        } else {
+            int size = 2 * NT;
+            while (size < n) size <<= 1;
+            for (int i = n + threadIdx.x; i < size; i += NT) sh.cand[i] = ~(uint64_t)0;
+            sp_sort<NT>(sh.cand, size);
         }
-        sp_scan(sh.scan, sum, 0, w0, n0, w_all, n_all);
+        __syncthreads();
+        const int each = (n + NT - 1) / NT;
+        c0 = sp_min((int)threadIdx.x * each, n);
+        c1 = sp_min(c0 + each, n);
+        uint64_t sum = 0;
+        for (int i = c0; i < c1; ++i) {
+            const uint64_t w = sp_weight(sp_place_z(sh.cand[i]), top, c, a.bits);
+            sh.cand_w[i] = w;
+            sum += w;
+        }
+        sp_scan<NT>(sh.scan, sum, 0, w0, n0, w_all, n_all);
         if (!rule.use_p || rule.use_k || w_all >= target_p || b0 >= bin_m) break;
         b0 = sp_min(b0 + 2 * SP_PER_BINADE, bin_m);
     }
     // 3  how many of them top-k, then top-p and min-p keep, and their weight
     int keep = rule.use_k && rule.k < n ? (int)rule.k : n;
     if (rule.use_p) {
-        if (rule.use_k) { // the share is one of the weight that top-k keeps
-            uint64_t run = w0;
-            __syncthreads();
-            if (threadIdx.x == 0) sh.scan.found_w = w_all;
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                run += w[i];
-                if (threadIdx.x * EACH + i == keep - 1) sh.scan.found_w = run;
+        if (rule.use_k && keep < n) { // the share is one of the weight that top-k keeps
+            if (c0 < keep && keep <= c1) {
+                uint64_t run = w0;
+                for (int i = c0; i < keep; ++i) run += sh.cand_w[i];
+                sh.scan.found_w = run;
             }
             __syncthreads();
-            target_p = sp_share(rule.p, sh.scan.found_w);
+            w_all = sh.scan.found_w;
         }
-        uint64_t run = w0;
-        __syncthreads();
+        if (rule.use_k) target_p = sp_share(rule.p, w_all);
         if (threadIdx.x == 0) sh.scan.found = n;
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            if (run < target_p && target_p <= run + w[i]) sh.scan.found = threadIdx.x * EACH + i + 1;
-            run += w[i];
+        uint64_t run = w0;
+        for (int i = c0; i < c1; ++i) {
+            const uint64_t w = sh.cand_w[i];
+            if (run < target_p && target_p <= run + w) sh.scan.found = i + 1;
+            run += w;
         }
         __syncthreads();
         keep = sp_min(keep, sh.scan.found);
     }
     const uint64_t floor_w = sp_floor(a, rule);
     uint64_t kept = 0;
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        if (threadIdx.x * EACH + i >= keep || w[i] < floor_w) w[i] = 0;
-        kept += w[i];
+    for (int i = c0; i < c1; ++i) {
+        const uint64_t w = sh.cand_w[i];
+        if (i >= keep || w < floor_w) sh.cand_w[i] = 0;
+        else kept += w;
     }
-    // 4  by id: the range of ids, then the class, at which the running weight exceeds the target
-    int shift = 0;
-    while ((a.C - 1) >> shift >= SP_BINS) ++shift;
-    sp_clear(sh.n, sh.w);
-#pragma unroll
-    for (int i = 0; i < EACH; ++i)
-        if (w[i]) atomicAdd((unsigned long long *)&sh.w[(uint32_t)sh.cand[threadIdx.x * EACH + i] >> shift], (unsigned long long)w[i]);
-    sp_scan(sh.scan, kept, 0, w0, n0, w_all, n_all);
-    const uint64_t target = sp_target(a, row, w_all);
-    uint64_t unused;
-    sp_find(sh.scan, sh.n, sh.w, false, target + 1, unused, n_all);
-    const uint64_t rest = target - sh.scan.found_w;
-    const uint32_t range = (uint32_t)sh.scan.found;
-    if (threadIdx.x == 0) sh.fill = 0;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < EACH; ++i)
-        if (w[i] && (uint32_t)sh.cand[threadIdx.x * EACH + i] >> shift == range) {
-            const uint32_t at = atomicAdd(&sh.fill, 1u);
-            sh.list[at] = threadIdx.x * EACH + i;
-        }
-    __syncthreads();
-    const int members = (int)sh.fill;
-    for (int i = threadIdx.x; i < members; i += SP_NT) {
-        const uint64_t place = sh.cand[sh.list[i]];
+    w_all = sp_total<NT>(sh.scan, kept);
+    uint64_t target = sp_target(a, row, w_all);
+    // 4  by id: the class at which the running weight exceeds the target, among few in number, or of a range of ids
+    int members = n;
+    if (n > NT) {
+        int shift = 0;
+        while ((a.C - 1) >> shift >= SP_BINS) ++shift;
+        sp_clear<NT>(sh.n, sh.w);
+        for (int i = c0; i < c1; ++i)
+            if (sh.cand_w[i]) atomicAdd((unsigned long long *)&sh.w[(uint32_t)sh.cand[i] >> shift], (unsigned long long)sh.cand_w[i]);
+        uint64_t unused;
+        sp_find<NT>(sh.scan, sh.n, sh.w, false, target + 1, unused, n_all);
+        target -= sh.scan.found_w;
+        const uint32_t range = (uint32_t)sh.scan.found;
+        if (threadIdx.x == 0) sh.fill = 0;
+        __syncthreads();
+        for (int i = c0; i < c1; ++i)
+            if (sh.cand_w[i] && (uint32_t)sh.cand[i] >> shift == range) sh.member[atomicAdd(&sh.fill, 1u)] = i;
+        __syncthreads();
+        members = (int)sh.fill;
+    }
+    for (int i = threadIdx.x; i < members; i += NT) {
+        const int at = n > NT ? sh.member[i] : i;
+        const uint64_t place = sh.cand[at], w = sh.cand_w[at];
         uint64_t before = 0;
-        for (int j = 0; j < members; ++j) {
-            const uint64_t other = sh.cand[sh.list[j]];
-            if ((uint32_t)other < (uint32_t)place) before += sp_weight(sp_place_z(other), top, c, a.bits);
-        }
-        const float logit = sp_place_z(place);
-        if (before <= rest && rest < before + sp_weight(logit, top, c, a.bits)) sp_result(a, row, (int)(uint32_t)place, logit, top, c, w_all);
+        if (n > NT)
+            for (int j = 0; j < members; ++j) before += (uint32_t)sh.cand[sh.member[j]] < (uint32_t)place ? sh.cand_w[sh.member[j]] : 0;
+        else
+#pragma unroll 4
+            for (int j = 0; j < keep; ++j) before += (uint32_t)sh.cand[j] < (uint32_t)place ? sh.cand_w[j] : 0;
+        if (before <= target && target < before + w) sp_result(a, row, (int)(uint32_t)place, sp_place_z(place), top, c, w_all);
     }
 }
 
 // ------------------------------------------------------------------------------------------------
 // rows of which more may be kept than LDS holds
 // ------------------------------------------------------------------------------------------------
+// granules of a workgroup's threads, SP_PER consecutive ones each
+#define SP_PER (SP_GRANULES / SP_NT2)
+struct SpMine {
+    float top[SP_PER], row_top;
+    int first, n; // of the thread
+    __device__ __forceinline__ SpMine(const SpArgs &a, int row, SpScan &sh) {
+        const int per = (a.ngr + SP_NT2 - 1) / SP_NT2;
+        first = threadIdx.x * per;
+        n = sp_max(0, sp_min(per, a.ngr - first));
+        row_top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < SP_PER; ++i) {
+            top[i] = i < n ? a.g_max[(int64_t)row * a.ngr + first + i] : -INFINITY;
+            row_top = fmaxf(row_top, top[i]);
+        }
+        row_top = sp_block_max<SP_NT2>(sh, row_top);
+    }
+    __device__ __forceinline__ uint64_t mass(const SpArgs &a, int row, const SpRule &rule, int i) const { return i < n ? sp_mass(a, row, first + i, top[i], row_top, rule.c) : 0; }
+};
+// the granules whose largest logit lies in bin b0 or before, in order: list, and how many
+__device__ __forceinline__ int sp_list(const SpMine &mine, SpScan &sh, float c32, int b0, int32_t *list) {
+    bool in[SP_PER];
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < SP_PER; ++i) {
+        in[i] = sp_bin(mine.top[i], mine.row_top, c32) <= b0;
+        n += in[i];
+    }
+    uint64_t w0, w_all;
+    uint32_t at, all;
+    sp_scan<SP_NT2>(sh, 0, (uint32_t)n, w0, at, w_all, all);
+#pragma unroll
+    for (int i = 0; i < SP_PER; ++i)
+        if (in[i]) list[at++] = mine.first + i;
+    __syncthreads();
+    return (int)all;
+}
+
 struct SpMany {
     SpScan scan;
     uint32_t n[SP_BINS];   // of the bins: classes (at first: granules), and their weight
@@ -660,7 +704,7 @@ __device__ __forceinline__ uint64_t sp_refine(const SpArgs &a, const T *z, bool 
     uint32_t n = sh.n[bin];
     while (n > SP_MANY_CAND) {
         uint64_t least = ~(uint64_t)0, most = 0;
-        sp_over_list(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+        sp_over_list<SP_NT2>(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint64_t place = sp_place(v[i], id + i);
@@ -677,11 +721,11 @@ __device__ __forceinline__ uint64_t sp_refine(const SpArgs &a, const T *z, bool 
         __syncthreads();
         if ((threadIdx.x & 63) == 0) { sh.scan.w[threadIdx.x >> 6] = least; sh.scan.v[threadIdx.x >> 6] = most; }
         __syncthreads();
-        for (int i = 0; i < SP_WAVES; ++i) { least = sp_min(least, sh.scan.w[i]); most = sp_max(most, sh.scan.v[i]); }
+        for (int i = 0; i < (SP_NT2 / 64); ++i) { least = sp_min(least, sh.scan.w[i]); most = sp_max(most, sh.scan.v[i]); }
         int shift = 0;
         while ((most - least) >> shift >= SP_BINS) ++shift;
-        sp_clear(sh.sub.n, sh.sub.w);
-        sp_over_list(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+        sp_clear<SP_NT2>(sh.sub.n, sh.sub.w);
+        sp_over_list<SP_NT2>(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
 #pragma unroll 1
             for (int i = 0; i < 8; ++i) {
                 const uint64_t place = sp_place(v[i], id + i);
@@ -693,7 +737,7 @@ __device__ __forceinline__ uint64_t sp_refine(const SpArgs &a, const T *z, bool 
         });
         uint64_t w_all;
         uint32_t n_all;
-        sp_find(sh.scan, sh.sub.n, sh.sub.w, by_n, target, w_all, n_all);
+        sp_find<SP_NT2>(sh.scan, sh.sub.n, sh.sub.w, by_n, target, w_all, n_all);
         const int part = sh.scan.found; // there is one: the target lies within the bin
         lo = least + ((uint64_t)part << shift);
         hi = sp_min(most, lo + (((uint64_t)1 << shift) - 1));
@@ -705,9 +749,9 @@ __device__ __forceinline__ uint64_t sp_refine(const SpArgs &a, const T *z, bool 
     if (threadIdx.x == 0) { sh.fill = 0; sh.place = 0; sh.scan.found_w = 0; }
     int size = 64;
     while (size < (int)n) size <<= 1;
-    for (int i = n + threadIdx.x; i < size; i += SP_NT) sh.cand[i] = ~(uint64_t)0;
+    for (int i = n + threadIdx.x; i < size; i += SP_NT2) sh.cand[i] = ~(uint64_t)0;
     __syncthreads();
-    sp_over_list(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+    sp_over_list<SP_NT2>(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint64_t place = sp_place(v[i], id + i);
@@ -717,8 +761,8 @@ __device__ __forceinline__ uint64_t sp_refine(const SpArgs &a, const T *z, bool 
         }
     });
     __syncthreads();
-    sp_sort(sh.cand, size);
-    constexpr int EACH = SP_MANY_CAND / SP_NT;
+    sp_sort<SP_NT2>(sh.cand, size);
+    constexpr int EACH = SP_MANY_CAND / SP_NT2;
     uint64_t w[EACH], mine = 0, w0, w_all;
     uint32_t unused, unused_all;
 #pragma unroll
@@ -727,7 +771,7 @@ __device__ __forceinline__ uint64_t sp_refine(const SpArgs &a, const T *z, bool 
         w[i] = at < (int)n ? sp_weight(sp_place_z(sh.cand[at]), top, c, a.bits) : 0;
         mine += w[i];
     }
-    sp_scan(sh.scan, mine, 0, w0, unused, w_all, unused_all);
+    sp_scan<SP_NT2>(sh.scan, mine, 0, w0, unused, w_all, unused_all);
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         const int at = threadIdx.x * EACH + i;
@@ -744,7 +788,7 @@ __device__ __forceinline__ uint64_t sp_refine(const SpArgs &a, const T *z, bool 
 
 // A workgroup per row: numbers and weights of the bins, the bin in which top-k or top-p ends in order, what is kept of every granule, the class.
 template <typename T>
-__global__ void __launch_bounds__(SP_NT)
+__global__ void __launch_bounds__(SP_NT2)
 sp_many_kernel(SpArgs a) {
     __shared__ SpMany sh;
     const int row = a.row0 + blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -761,28 +805,28 @@ sp_many_kernel(SpArgs a) {
     uint64_t w0, w_all, target_p = 0;
     uint32_t n0, n_all;
     if (rule.use_k) {
-        sp_clear(sh.n, sh.w);
+        sp_clear<SP_NT2>(sh.n, sh.w);
 #pragma unroll
         for (int i = 0; i < SP_PER; ++i) {
             const int b = sp_bin(mine.top[i], top, c32);
             if (b < limit) atomicAdd(&sh.n[b], 1u);
         }
-        sp_find(sh.scan, sh.n, sh.w, true, (uint64_t)rule.k, w_all, n_all);
+        sp_find<SP_NT2>(sh.scan, sh.n, sh.w, true, (uint64_t)rule.k, w_all, n_all);
         const int found = sh.scan.found < 0 ? limit - 1 : sh.scan.found;
         b0 = rule.use_p ? found : sp_min(found, b0);
     } else if (rule.use_p) {
         uint64_t sum = 0;
 #pragma unroll
-        for (int i = 0; i < SP_PER; ++i) sum += mine.weight(a, row, rule, i);
-        sp_scan(sh.scan, sum, 0, w0, n0, w_all, n_all);
+        for (int i = 0; i < SP_PER; ++i) sum += mine.mass(a, row, rule, i);
+        sp_scan<SP_NT2>(sh.scan, sum, 0, w0, n0, w_all, n_all);
         target_p = sp_share(rule.p, w_all);
     }
     const int n_list = sp_list(mine, sh.scan, c32, b0, sh.list);
     if (threadIdx.x == 0) sh.n_list = n_list;
-    sp_clear(sh.n, sh.w);
+    sp_clear<SP_NT2>(sh.n, sh.w);
     uint64_t cut = ~(uint64_t)0;
     if (rule.use_k || rule.use_p) {
-        sp_over_list(a, z, vec, sh.list, n_list, [&](const float (&v)[8], uint32_t) __attribute__((always_inline)) {
+        sp_over_list<SP_NT2>(a, z, vec, sh.list, n_list, [&](const float (&v)[8], uint32_t) __attribute__((always_inline)) {
 #pragma unroll 2
             for (int i = 0; i < 8; ++i) {
                 const int b = sp_bin(v[i], top, c32);
@@ -792,7 +836,7 @@ sp_many_kernel(SpArgs a) {
             }
         });
         if (rule.use_k) {
-            sp_find(sh.scan, sh.n, sh.w, true, (uint64_t)rule.k, w_all, n_all);
+            sp_find<SP_NT2>(sh.scan, sh.n, sh.w, true, (uint64_t)rule.k, w_all, n_all);
             if (sh.scan.found >= 0) {
                 const uint64_t before = sh.scan.found_w;
                 uint64_t w;
@@ -803,7 +847,7 @@ sp_many_kernel(SpArgs a) {
         }
         if (rule.use_p) {
             uint64_t all;
-            sp_find(sh.scan, sh.n, sh.w, false, target_p, all, n_all);
+            sp_find<SP_NT2>(sh.scan, sh.n, sh.w, false, target_p, all, n_all);
             if (sh.scan.found >= 0) {
                 uint64_t w;
                 cut = sp_min(cut, sp_refine(a, z, vec, sh, top, c, c32, sh.scan.found, false, target_p - sh.scan.found_w, w));
@@ -811,11 +855,11 @@ sp_many_kernel(SpArgs a) {
         }
     }
     const uint64_t floor_w = sp_floor(a, rule);
-    for (int i = threadIdx.x; i < n_list; i += SP_NT) sh.g_w[i] = 0;
+    for (int i = threadIdx.x; i < n_list; i += SP_NT2) sh.g_w[i] = 0;
     __syncthreads();
-    const int at_once = SP_NT >> a.lg;
+    const int at_once = SP_NT2 >> a.lg;
     int turn = 0; // which of its granules a thread is at
-    sp_over_list(a, z, vec, sh.list, n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+    sp_over_list<SP_NT2>(a, z, vec, sh.list, n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
         uint64_t sum = 0;
 #pragma unroll 2
         for (int i = 0; i < 8; ++i) {
@@ -828,7 +872,7 @@ sp_many_kernel(SpArgs a) {
             at = turn * at_once + (threadIdx.x >> a.lg);
             ++turn;
         } else {
-            at = wave + turn * SP_WAVES;
+            at = wave + turn * (SP_NT2 / 64);
             if ((int64_t)(id - lane * 8) + SP_CHUNK >= sp_min((sh.list[at] + (int64_t)1) * a.gran, a.C)) ++turn;
         }
         if (sum) atomicAdd((unsigned long long *)&sh.g_w[at], (unsigned long long)sum);
@@ -840,7 +884,7 @@ sp_many_kernel(SpArgs a) {
         w[i] = threadIdx.x * SP_PER + i < n_list ? sh.g_w[threadIdx.x * SP_PER + i] : 0;
         sum += w[i];
     }
-    sp_scan(sh.scan, sum, 0, w0, n0, w_all, n_all);
+    sp_scan<SP_NT2>(sh.scan, sum, 0, w0, n0, w_all, n_all);
     const uint64_t target = sp_target(a, row, w_all);
 #pragma unroll
     for (int i = 0; i < SP_PER; ++i) {
@@ -900,7 +944,7 @@ template <typename T> static void sp_sample(SpArgs &a, int B, hipStream_t st) {
         default: granules(sp_granules_kernel<6, T>);
         }
         hipLaunchKernelGGL(sp_draw_kernel<T>, dim3(rows), dim3(SP_NT), 0, st, a);
-        if (a.C > SP_CAND) hipLaunchKernelGGL(sp_many_kernel<T>, dim3(rows), dim3(SP_NT), 0, st, a); // else LDS holds all
+        if (a.C > SP_CAND) hipLaunchKernelGGL(sp_many_kernel<T>, dim3(rows), dim3(SP_NT2), 0, st, a); // else LDS holds all
     }
 }
 
@@ -918,6 +962,7 @@ extern "C" int class_sample(const void *logits, int64_t ldl, int dtype, int64_t 
     a.logits = logits; a.ldl = ldl; a.C = C;
     a.u = u; a.temperature = temperature; a.top_p = top_p; a.min_p = min_p; a.top_k = top_k;
     a.ids = ids; a.logprob = logprob;
+    a.most = (int64_t)1 << 40;
     if (dtype == KS_DTYPE_FP32) sp_sample<float>(a, B, (hipStream_t)stream);
     else sp_sample<uint16_t>(a, B, (hipStream_t)stream);
     KS_LAUNCH_CHECK();
