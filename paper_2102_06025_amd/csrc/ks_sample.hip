@@ -22,20 +22,35 @@
 template <typename T> static __device__ __forceinline__ T sp_min(T a, T b) { return b < a ? b : a; }
 template <typename T> static __device__ __forceinline__ T sp_max(T a, T b) { return a < b ? b : a; }
 
+struct SpRow;
 struct SpArgs {
     const void *logits;
     int64_t ldl, C, gran; // classes of a granule: 8 << lg, beyond 512 a multiple of that
-    int lg, ngr, bits, row0;
+    int lg, gshift, ngr, bits, row0; // gran = 1 << gshift
     const float *u, *temperature, *top_p, *min_p;
     const int32_t *top_k;
     float *g_max;  // [B, ngr]
     double *g_sum; // [B, ngr]: sum of exp((z - g_max) / T)
     int32_t *many; // [B]: the row is left to the third launch
     int64_t most;  // classes that a row's workgroup looks at itself
+    int64_t span;  // classes of a workgroup that counts
+    // where all compute units share such a row:
+    SpRow *rows;        // [B], NULL: they do not
+    float *row_top;     // [B]
+    uint32_t *bins_n;   // [B, SP_BINS]: classes, and their weight
+    uint64_t *bins_w;
+    uint64_t *pool, *pool_used, pool_size; // places of classes of the bins in which top-k and top-p end, of all rows
     int32_t *ids;
     float *logprob;
 };
 
+// a row that all compute units share
+struct SpRow {
+    int b0, bin_k, p_first, p_last, sure; // bins: the last to look at; of top-k (-1: none); of top-p; those before `sure` are kept (but for min-p)
+    uint32_t k_rest, n_cand, fill, done;
+    uint64_t target_p, w_all, before_k, before_p; // weight of all (or up to bin_k: before_k), before p_first
+    uint64_t cand0;                               // of its candidates in the pool
+};
 // what a row asks for
 struct SpRule {
     double c;            // weight of z: 2^(c (z - z_max))
@@ -160,6 +175,7 @@ template <int LG, typename T>
 __global__ void __launch_bounds__(256)
 sp_granules_kernel(SpArgs a) {
     const int lane = threadIdx.x & 63, wave = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = a.row0 + blockIdx.y;
+    if (a.rows && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.pool_used = 0;
     const int64_t span = LG < 6 ? SP_CHUNK : a.gran, first = wave * span, last = sp_min(first + span, a.C);
     if (first >= a.C) return;
     const SpRule rule(a, row);
@@ -361,15 +377,20 @@ template <typename T> __device__ __forceinline__ int sp_first(const SpArgs &a, c
 }
 
 // f(z, id) for eight classes a thread of the n listed granules; all lanes of a wavefront call it together
-template <int NT, typename T, typename F> __device__ __forceinline__ void sp_over_list(const SpArgs &a, const T *z, bool vec, const int32_t *list, int n, F f) {
+template <int NT, int SP_AHEAD, typename T, typename F> __device__ __forceinline__ void sp_over_list(const SpArgs &a, const T *z, bool vec, const int32_t *list, int n, F f) {
     if (a.gran <= SP_CHUNK) {
         const int lanes = 1 << a.lg, at_once = NT >> a.lg, sub = threadIdx.x & (lanes - 1);
-        for (int i0 = 0; i0 < n; i0 += at_once) {
-            const int i = i0 + (threadIdx.x >> a.lg);
-            float v[8];
-            const int64_t e = i < n ? list[i] * a.gran + sub * 8 : a.C;
-            sp_load(z, vec, e, a.C, v);
-            f(v, (uint32_t)e);
+        for (int i0 = 0; i0 < n; i0 += at_once * SP_AHEAD) { // several loads at a time
+            float v[SP_AHEAD][8];
+            int64_t e[SP_AHEAD];
+#pragma unroll
+            for (int u = 0; u < SP_AHEAD; ++u) {
+                const int i = i0 + u * at_once + (threadIdx.x >> a.lg);
+                e[u] = i < n ? list[i] * a.gran + sub * 8 : a.C;
+                sp_load(z, vec, e[u], a.C, v[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < SP_AHEAD; ++u) f(v[u], (uint32_t)e[u]);
         }
     } else {
         const int lane = threadIdx.x & 63;
@@ -399,6 +420,7 @@ template <int NT> __device__ __forceinline__ void sp_sort(uint64_t *p, int size)
     __syncthreads();
 }
 
+__device__ __forceinline__ void sp_share_row(const SpArgs &a, int row, float top, int b0, uint64_t target_p);
 struct SpShared {
     SpScan scan;
     float top[SP_GRANULES]; // of the granules
@@ -510,13 +532,13 @@ sp_draw_kernel(SpArgs a) {
         uint32_t listed = 0;
         for (int g = g0; g < g1; ++g) listed += sp_bin(sh.top[g], top, c32) <= b0;
         sp_scan<NT>(sh.scan, 0, listed, w0, n0, w_all, n_all);
-        if (n_all > SP_CAND || (rule.use_k && rule.k > SP_CAND) || n_all * a.gran > a.most) n = SP_CAND + 1; // a class of each granule is in
+        if (n_all > SP_CAND || (rule.use_k && rule.k > SP_CAND) || n_all * a.gran > (rule.use_k ? 4 * a.most : a.most)) n = SP_CAND + 1; // a class of each granule is in
         else {
             if (threadIdx.x == 0) sh.fill = 0;
             for (int g = g0; g < g1; ++g)
                 if (sp_bin(sh.top[g], top, c32) <= b0) sh.list[n0++] = g;
             __syncthreads();
-            sp_over_list<NT>(a, z, vec, sh.list, (int)n_all, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+            sp_over_list<NT, 4>(a, z, vec, sh.list, (int)n_all, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
                 uint32_t in = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) in |= (uint32_t)(sp_bin(v[i], top, c32) <= b0) << i;
@@ -537,6 +559,7 @@ sp_draw_kernel(SpArgs a) {
         }
         if (n > SP_CAND) { // more than LDS holds
             if (threadIdx.x == 0) a.many[row] = 1;
+            if (a.rows) sp_share_row(a, row, top, rule.use_k ? b0 : bin_m, target_p);
             return;
         }
         if (n <= NT) { // a candidate's place in the order is the number of those before it; several threads count for one where there are few
@@ -704,7 +727,7 @@ __device__ __forceinline__ uint64_t sp_refine(const SpArgs &a, const T *z, bool 
     uint32_t n = sh.n[bin];
     while (n > SP_MANY_CAND) {
         uint64_t least = ~(uint64_t)0, most = 0;
-        sp_over_list<SP_NT2>(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+        sp_over_list<SP_NT2, 1>(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint64_t place = sp_place(v[i], id + i);
@@ -725,8 +748,8 @@ __device__ __forceinline__ uint64_t sp_refine(const SpArgs &a, const T *z, bool 
         int shift = 0;
         while ((most - least) >> shift >= SP_BINS) ++shift;
         sp_clear<SP_NT2>(sh.sub.n, sh.sub.w);
-        sp_over_list<SP_NT2>(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
-#pragma unroll 1
+        sp_over_list<SP_NT2, 1>(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+#pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint64_t place = sp_place(v[i], id + i);
                 if (sp_bin(v[i], top, c32) != bin || place < least || place > most) continue;
@@ -751,7 +774,7 @@ __device__ __forceinline__ uint64_t sp_refine(const SpArgs &a, const T *z, bool 
     while (size < (int)n) size <<= 1;
     for (int i = n + threadIdx.x; i < size; i += SP_NT2) sh.cand[i] = ~(uint64_t)0;
     __syncthreads();
-    sp_over_list<SP_NT2>(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+    sp_over_list<SP_NT2, 1>(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint64_t place = sp_place(v[i], id + i);
@@ -786,13 +809,115 @@ __device__ __forceinline__ uint64_t sp_refine(const SpArgs &a, const T *z, bool 
     return sh.place;
 }
 
+// The class of a row that all compute units shared: the classes of the bins in which top-k and top-p end in order, what they add to their granules.
+struct SpFinal {
+    SpScan scan;
+    uint64_t cand[SP_CAND], cand_w[SP_CAND], g_w[SP_GRANULES];
+};
+template <typename T> __device__ __forceinline__ void sp_final(const SpArgs &a, int row, SpFinal &sh) {
+    constexpr int NT = SP_NT2;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const SpRule rule(a, row);
+    const SpRow &st = a.rows[row];
+    bool vec;
+    const T *const z = sp_row<T>(a, row, vec);
+    const float top = a.row_top[row], c32 = sp_c32(rule);
+    const double c = rule.c;
+    const int bin_k = st.bin_k, p_first = st.p_first, p_last = st.p_last;
+    const uint64_t floor_w = sp_floor(a, rule), *const g_w = (const uint64_t *)a.g_sum + (int64_t)row * a.ngr;
+    const uint32_t n = st.n_cand;
+    for (int g = threadIdx.x; g < a.ngr; g += NT) sh.g_w[g] = g_w[g];
+    for (int i = threadIdx.x; i < (int)n; i += NT) sh.cand[i] = a.pool[st.cand0 + i];
+    int size = 64;
+    while (size < (int)n) size <<= 1;
+    for (int i = n + threadIdx.x; i < size; i += NT) sh.cand[i] = ~(uint64_t)0;
+    __syncthreads();
+    if (n) sp_sort<NT>(sh.cand, size);
+    const int each = (n + NT - 1) / NT, c0 = sp_min((int)threadIdx.x * each, (int)n), c1 = sp_min(c0 + each, (int)n);
+    // the last class that top-k, then top-p keeps
+    uint64_t cut = ~(uint64_t)0, w0, all, target = st.target_p, sum = 0;
+    uint32_t n0, n_all, in_k = 0;
+    for (int i = c0; i < c1; ++i) {
+        const float v = sp_place_z(sh.cand[i]);
+        sh.cand_w[i] = sp_weight(v, top, c, a.bits);
+        in_k += sp_bin(v, top, c32) == bin_k;
+    }
+    if (bin_k >= 0) {
+        for (int i = c0; i < c1; ++i)
+            if (sp_bin(sp_place_z(sh.cand[i]), top, c32) == bin_k) sum += sh.cand_w[i];
+        sp_scan<NT>(sh.scan, sum, in_k, w0, n0, all, n_all);
+        if (n0 < st.k_rest && st.k_rest <= n0 + in_k) // one thread
+            for (int i = c0; i < c1; ++i)
+                if (sp_bin(sp_place_z(sh.cand[i]), top, c32) == bin_k) {
+                    ++n0;
+                    w0 += sh.cand_w[i];
+                    if (n0 == st.k_rest) {
+                        sh.scan.found_w = w0;
+                        sh.scan.found = i;
+                    }
+                }
+        __syncthreads();
+        cut = sh.cand[sh.scan.found];
+        target = sp_share(rule.p, st.before_k + sh.scan.found_w);
+    } else if (rule.use_k) target = sp_share(rule.p, st.w_all);
+    if (p_first < SP_NO_BIN) {
+        sum = 0;
+        for (int i = c0; i < c1; ++i) {
+            const int b = sp_bin(sp_place_z(sh.cand[i]), top, c32);
+            if (b >= p_first && b <= p_last) sum += sh.cand_w[i];
+        }
+        sp_scan<NT>(sh.scan, sum, 0, w0, n0, all, n_all);
+        w0 += st.before_p;
+        if (threadIdx.x == 0) sh.scan.found = -1;
+        __syncthreads();
+        for (int i = c0; i < c1; ++i) {
+            const int b = sp_bin(sp_place_z(sh.cand[i]), top, c32);
+            if (b < p_first || b > p_last) continue;
+            if (w0 < target && target <= w0 + sh.cand_w[i]) sh.scan.found = i;
+            w0 += sh.cand_w[i];
+        }
+        __syncthreads();
+        if (sh.scan.found >= 0) cut = sp_min(cut, sh.cand[sh.scan.found]);
+    }
+    __syncthreads();
+    for (int i = c0; i < c1; ++i) {
+        const uint64_t place = sh.cand[i], w = sh.cand_w[i];
+        if (place <= cut && w >= floor_w) atomicAdd((unsigned long long *)&sh.g_w[(uint32_t)place >> a.gshift], (unsigned long long)w);
+    }
+    __syncthreads();
+    const int per = (a.ngr + NT - 1) / NT, g0 = sp_min((int)threadIdx.x * per, a.ngr), g1 = sp_min(g0 + per, a.ngr);
+    sum = 0;
+    for (int g = g0; g < g1; ++g) sum += sh.g_w[g];
+    sp_scan<NT>(sh.scan, sum, 0, w0, n0, all, n_all);
+    target = sp_target(a, row, all);
+    if (w0 <= target && target < w0 + sum) // one thread
+        for (int g = g0; g < g1; ++g) {
+            if (target < w0 + sh.g_w[g]) { sh.scan.found = g; sh.scan.found_w = target - w0; break; }
+            w0 += sh.g_w[g];
+        }
+    __syncthreads();
+    if (wave == 0) {
+        int id;
+        float logit;
+        const int64_t from = sh.scan.found * a.gran;
+        sp_pick(a, z, vec, from, sp_min(from + a.gran, a.C), sh.scan.found_w, top, c, cut, floor_w, id, logit);
+        if (lane == 0) sp_result(a, row, id, logit, top, c, all);
+    }
+}
+
 // A workgroup per row: numbers and weights of the bins, the bin in which top-k or top-p ends in order, what is kept of every granule, the class.
 template <typename T>
 __global__ void __launch_bounds__(SP_NT2)
 sp_many_kernel(SpArgs a) {
-    __shared__ SpMany sh;
-    const int row = a.row0 + blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (!a.many[row]) return;
+    __shared__ union U {
+        SpMany many;
+        SpFinal final;
+        __device__ U() {}
+    } u;
+    const int row = a.row0 + blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), state = a.many[row];
+    if (state == 3) sp_final<T>(a, row, u.final);
+    if (state != (a.rows ? 2 : 1)) return;
+    SpMany &sh = u.many;
     const SpRule rule(a, row);
     bool vec;
     const T *const z = sp_row<T>(a, row, vec);
@@ -814,7 +939,8 @@ sp_many_kernel(SpArgs a) {
         sp_find<SP_NT2>(sh.scan, sh.n, sh.w, true, (uint64_t)rule.k, w_all, n_all);
         const int found = sh.scan.found < 0 ? limit - 1 : sh.scan.found;
         b0 = rule.use_p ? found : sp_min(found, b0);
-    } else if (rule.use_p) {
+    } else if (rule.use_p && a.rows) target_p = a.rows[row].target_p;
+    else if (rule.use_p) {
         uint64_t sum = 0;
 #pragma unroll
         for (int i = 0; i < SP_PER; ++i) sum += mine.mass(a, row, rule, i);
@@ -826,8 +952,8 @@ sp_many_kernel(SpArgs a) {
     sp_clear<SP_NT2>(sh.n, sh.w);
     uint64_t cut = ~(uint64_t)0;
     if (rule.use_k || rule.use_p) {
-        sp_over_list<SP_NT2>(a, z, vec, sh.list, n_list, [&](const float (&v)[8], uint32_t) __attribute__((always_inline)) {
-#pragma unroll 2
+        sp_over_list<SP_NT2, 1>(a, z, vec, sh.list, n_list, [&](const float (&v)[8], uint32_t) __attribute__((always_inline)) {
+#pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int b = sp_bin(v[i], top, c32);
                 if (b > b0) continue;
@@ -859,9 +985,9 @@ sp_many_kernel(SpArgs a) {
     __syncthreads();
     const int at_once = SP_NT2 >> a.lg;
     int turn = 0; // which of its granules a thread is at
-    sp_over_list<SP_NT2>(a, z, vec, sh.list, n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+    sp_over_list<SP_NT2, 1>(a, z, vec, sh.list, n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
         uint64_t sum = 0;
-#pragma unroll 2
+#pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (sp_bin(v[i], top, c32) > b0 || sp_place(v[i], id + i) > cut) continue;
             const uint64_t w = sp_weight(v[i], top, c, a.bits);
@@ -901,11 +1027,219 @@ sp_many_kernel(SpArgs a) {
     }
 }
 
+// ------------------------------------------------------------------------------------------------
+// such rows of many classes: all compute units share them
+// ------------------------------------------------------------------------------------------------
+// Two launches before the one above.  In the first the workgroups of a row count its bins; the one that is done last knows in which bin top-k ends,
+// and between which bins top-p does (the weight that top-k keeps is known but for a part of its own bin).  In the second they write what
+// lies before those bins, which is kept, granule by granule, and the places of the classes inside them, which the last launch puts in order.
+#define SP_SPAN 32768
+// what the two launches start from; all threads of the row's workgroup
+__device__ __forceinline__ void sp_share_row(const SpArgs &a, int row, float top, int b0, uint64_t target_p) {
+    for (int i = threadIdx.x; i < SP_BINS; i += blockDim.x) {
+        a.bins_n[(int64_t)row * SP_BINS + i] = 0;
+        a.bins_w[(int64_t)row * SP_BINS + i] = 0;
+    }
+    if (a.gran > SP_CHUNK) // granules' kept weights are added up there (the granules' own are no longer needed)
+        for (int i = threadIdx.x; i < a.ngr; i += blockDim.x) ((uint64_t *)a.g_sum)[(int64_t)row * a.ngr + i] = 0;
+    if (threadIdx.x == 0) {
+        SpRow &st = a.rows[row];
+        st.b0 = b0;
+        st.target_p = target_p;
+        st.fill = st.done = 0;
+        a.row_top[row] = top;
+    }
+}
+
+template <typename V> __device__ __forceinline__ V sp_read(const V *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// The workgroup that calls this last of `all` ones finds what the others have added and stored: all of it by atomic operations at the device's
+// scope, which have been done (a wavefront's own are waited for here) before `done` is counted up.  A fence would also write back the
+// whole L2, for each workgroup: 256 x 390,625 bf16 took 550 us in either launch.
+__device__ __forceinline__ bool sp_last(uint32_t *done, int all, uint32_t &sh) {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (threadIdx.x == 0) sh = __hip_atomic_fetch_add(done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    return sh == (uint32_t)all - 1;
+}
+
+struct SpCount {
+    SpScan scan;
+    uint32_t n[SP_BINS];
+    uint64_t w[SP_BINS];
+    uint32_t done;
+};
+template <typename T>
+__global__ void __launch_bounds__(SP_NT2)
+sp_count_kernel(SpArgs a) {
+    constexpr int NT = SP_NT2;
+    __shared__ SpCount sh;
+    const int row = a.row0 + blockIdx.y;
+    if (a.many[row] != 1) return;
+    const SpRule rule(a, row);
+    SpRow &st = a.rows[row];
+    uint32_t *const g_n = a.bins_n + (int64_t)row * SP_BINS;
+    uint64_t *const g_w = a.bins_w + (int64_t)row * SP_BINS;
+    bool vec;
+    const T *const z = sp_row<T>(a, row, vec);
+    const float top = a.row_top[row], c32 = sp_c32(rule);
+    const double c = rule.c;
+    const int b0 = st.b0;
+    sp_clear<NT>(sh.n, sh.w);
+    const int64_t first = blockIdx.x * a.span, last = sp_min(first + a.span, a.C);
+    for (int64_t e = first + threadIdx.x * 8; e < last; e += NT * 8) {
+        if (!(sp_bin(a.g_max[(int64_t)row * a.ngr + (e >> a.gshift)], top, c32) <= b0)) continue;
+        float v[8];
+        sp_load(z, vec, e, last, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int b = sp_bin(v[i], top, c32);
+            if (b > b0) continue;
+            atomicAdd(&sh.n[b], 1u);
+            atomicAdd((unsigned long long *)&sh.w[b], (unsigned long long)sp_weight(v[i], top, c, a.bits));
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < SP_BINS / NT; ++i) {
+        const int b = i * NT + threadIdx.x;
+        if (sh.n[b]) {
+            atomicAdd(&g_n[b], sh.n[b]);
+            atomicAdd((unsigned long long *)&g_w[b], (unsigned long long)sh.w[b]);
+        }
+    }
+    if (!sp_last(&st.done, gridDim.x, sh.done)) return;
+#pragma unroll
+    for (int i = 0; i < SP_BINS / NT; ++i) {
+        const int b = i * NT + threadIdx.x;
+        sh.n[b] = sp_read(&g_n[b]);
+        sh.w[b] = sp_read(&g_w[b]);
+    }
+    uint64_t w_all, target = st.target_p, before_k = 0, before_p = 0, unused;
+    uint32_t n_all, k_rest = 0;
+    int bin_k = -1, p_first = SP_NO_BIN + 1, p_last = -1;
+    uint64_t most;
+    if (rule.use_k) {
+        sp_find<NT>(sh.scan, sh.n, sh.w, true, (uint64_t)rule.k, w_all, n_all);
+        bin_k = sh.scan.found;
+        most = w_all;
+        if (bin_k >= 0) {
+            before_k = sh.scan.found_w;
+            k_rest = (uint32_t)(rule.k - sh.scan.found_n);
+            w_all = before_k;
+            most = before_k + sh.w[bin_k];
+        }
+    } else most = w_all = 0;
+    if (rule.use_p) {
+        sp_find<NT>(sh.scan, sh.n, sh.w, false, rule.use_k ? sp_share(rule.p, w_all) : target, unused, n_all);
+        if (sh.scan.found >= 0) { // else top-p ends behind what min-p keeps
+            p_first = p_last = sh.scan.found;
+            before_p = sh.scan.found_w;
+            if (bin_k >= 0) {
+                sp_find<NT>(sh.scan, sh.n, sh.w, false, sp_share(rule.p, most), unused, n_all);
+                p_last = sh.scan.found;
+            }
+        }
+    }
+    __syncthreads();
+    uint32_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < SP_BINS / NT; ++i) {
+        const int b = i * NT + threadIdx.x;
+        if (b == bin_k || (b >= p_first && b <= p_last)) mine += sh.n[b];
+    }
+    uint64_t w0;
+    uint32_t n0, n_cand;
+    sp_scan<NT>(sh.scan, 0, mine, w0, n0, unused, n_cand);
+    if (threadIdx.x == 0) {
+        st.bin_k = bin_k;
+        st.p_first = p_first;
+        st.p_last = p_last;
+        st.sure = sp_min(p_first, bin_k >= 0 ? bin_k : b0 + 1);
+        st.k_rest = k_rest;
+        st.n_cand = n_cand;
+        st.w_all = w_all;
+        st.before_k = before_k;
+        st.before_p = before_p;
+        uint64_t at = 0;
+        if (n_cand <= SP_CAND) at = atomicAdd((unsigned long long *)a.pool_used, (unsigned long long)n_cand);
+        st.cand0 = at;
+        a.many[row] = n_cand <= SP_CAND && at + n_cand <= a.pool_size ? 3 : 2; // 2: a bin of equal logits, one workgroup's work
+    }
+}
+
+#define SP_NT3 512
+#define SP_SPAN3 8192 /* classes of a workgroup */
+struct SpKeep {
+    uint64_t cand[SP_CAND];
+    uint32_t fill, at;
+};
+template <typename T>
+__global__ void __launch_bounds__(SP_NT3)
+sp_keep_kernel(SpArgs a) {
+    constexpr int NT = SP_NT3;
+    __shared__ SpKeep sh;
+    const int row = a.row0 + blockIdx.y, lane = threadIdx.x & 63;
+    if (a.many[row] != 3) return;
+    const SpRule rule(a, row);
+    SpRow &st = a.rows[row];
+    bool vec;
+    const T *const z = sp_row<T>(a, row, vec);
+    const float top = a.row_top[row], c32 = sp_c32(rule);
+    const double c = rule.c;
+    const int b0 = st.b0, bin_k = st.bin_k, p_first = st.p_first, p_last = st.p_last, sure = st.sure;
+    const uint64_t floor_w = sp_floor(a, rule), cand0 = st.cand0;
+    const uint32_t n = st.n_cand;
+    uint64_t *const g_w = (uint64_t *)a.g_sum + (int64_t)row * a.ngr;
+    const int64_t first = (int64_t)blockIdx.x * SP_SPAN3, last = sp_min(first + SP_SPAN3, a.C);
+    if (threadIdx.x == 0) sh.fill = 0;
+    __syncthreads();
+    for (int64_t e0 = first; e0 < last; e0 += NT * 8) {
+        const int64_t e = e0 + threadIdx.x * 8;
+        uint64_t sum = 0;
+        if (e < last && sp_bin(a.g_max[(int64_t)row * a.ngr + (e >> a.gshift)], top, c32) <= b0) {
+            float v[8];
+            sp_load(z, vec, e, last, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int b = sp_bin(v[i], top, c32);
+                if (b < sure && b <= b0) {
+                    const uint64_t w = sp_weight(v[i], top, c, a.bits);
+                    if (w >= floor_w) sum += w;
+                } else if (b == bin_k || (b >= p_first && b <= p_last)) {
+                    const uint32_t at = atomicAdd(&sh.fill, 1u);
+                    if (at < SP_CAND) sh.cand[at] = sp_place(v[i], (uint32_t)(e + i)); // the row has no more than that
+                }
+            }
+        }
+        if (a.gran <= SP_CHUNK) {
+            for (int d = 1; d < 1 << a.lg; d <<= 1) sum += __shfl_xor((unsigned long long)sum, d);
+            if ((lane & ((1 << a.lg) - 1)) == 0 && e < last) g_w[e >> a.gshift] = sum;
+        } else {
+            sum = sp_wave_scan(sum);
+            if (lane == 63 && e - lane * 8 < last) { // several wavefronts, in any order
+                const int64_t g = (e - lane * 8) >> a.gshift;
+                atomicAdd((unsigned long long *)&g_w[g], (unsigned long long)sum);
+            }
+        }
+    }
+    __syncthreads();
+    const uint32_t here = sp_min(sh.fill, (uint32_t)SP_CAND);
+    if (threadIdx.x == 0 && here) sh.at = atomicAdd(&st.fill, here);
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < here; i += NT)
+        if (sh.at + i < n) a.pool[cand0 + sh.at + i] = sh.cand[i];
+}
+
 static bool sp_sizes(int64_t C, int B, SpArgs &a) {
     if (C < 1 || C >= (int64_t)1 << 31 || B < 1) return false;
+    a.C = C;
     a.gran = 8;
     while (ks_ceil_div(C, a.gran) > SP_GRANULES) a.gran *= 2;
     a.ngr = (int)ks_ceil_div(C, a.gran);
+    a.gshift = 3;
+    while ((int64_t)1 << a.gshift < a.gran) ++a.gshift;
     a.lg = 0;
     while (a.lg < 6 && 8 << a.lg < a.gran) ++a.lg;
     int lg = 0;
@@ -913,10 +1247,24 @@ static bool sp_sizes(int64_t C, int B, SpArgs &a) {
     a.bits = 62 - lg < 48 ? 62 - lg : 48;
     return true;
 }
+// From this many classes on, rows that keep much are shared by all compute units
+#define SP_SHARED_C 49152
 static void sp_places(KsArena &ws, int B, SpArgs &a) {
     a.g_max = ws.take<float>((size_t)B * a.ngr);
     a.g_sum = ws.take<double>((size_t)B * a.ngr);
     a.many = ws.take<int32_t>((size_t)B);
+    a.rows = nullptr;
+    a.most = (int64_t)1 << 40;
+    if (a.C < SP_SHARED_C) return;
+    a.most = SP_SPAN;
+    a.span = B * ks_ceil_div(a.C, SP_SPAN) < 512 ? SP_SPAN / 4 : SP_SPAN; // few rows: more workgroups; many: fewer bins to add up
+    a.rows = ws.take<SpRow>((size_t)B);
+    a.row_top = ws.take<float>((size_t)B);
+    a.bins_n = ws.take<uint32_t>((size_t)B * SP_BINS);
+    a.bins_w = ws.take<uint64_t>((size_t)B * SP_BINS);
+    a.pool_size = (uint64_t)(B < 256 ? B : 256) * SP_CAND;
+    a.pool = ws.take<uint64_t>((size_t)a.pool_size);
+    a.pool_used = ws.take<uint64_t>(1);
 }
 
 extern "C" size_t class_sample_workspace(int64_t C, int B) {
@@ -944,6 +1292,10 @@ template <typename T> static void sp_sample(SpArgs &a, int B, hipStream_t st) {
         default: granules(sp_granules_kernel<6, T>);
         }
         hipLaunchKernelGGL(sp_draw_kernel<T>, dim3(rows), dim3(SP_NT), 0, st, a);
+        if (a.rows) {
+            hipLaunchKernelGGL(sp_count_kernel<T>, dim3((unsigned)ks_ceil_div(a.C, a.span), rows), dim3(SP_NT2), 0, st, a);
+            hipLaunchKernelGGL(sp_keep_kernel<T>, dim3((unsigned)ks_ceil_div(a.C, SP_SPAN3), rows), dim3(SP_NT3), 0, st, a);
+        }
         if (a.C > SP_CAND) hipLaunchKernelGGL(sp_many_kernel<T>, dim3(rows), dim3(SP_NT2), 0, st, a); // else LDS holds all
     }
 }
@@ -959,10 +1311,9 @@ extern "C" int class_sample(const void *logits, int64_t ldl, int dtype, int64_t 
     if (ws_bytes < class_sample_workspace(C, B)) return KS_WORKSPACE_TOO_SMALL;
     KsArena arena(ws);
     sp_places(arena, B, a);
-    a.logits = logits; a.ldl = ldl; a.C = C;
+    a.logits = logits; a.ldl = ldl;
     a.u = u; a.temperature = temperature; a.top_p = top_p; a.min_p = min_p; a.top_k = top_k;
     a.ids = ids; a.logprob = logprob;
-    a.most = (int64_t)1 << 40;
     if (dtype == KS_DTYPE_FP32) sp_sample<float>(a, B, (hipStream_t)stream);
     else sp_sample<uint16_t>(a, B, (hipStream_t)stream);
     KS_LAUNCH_CHECK();
