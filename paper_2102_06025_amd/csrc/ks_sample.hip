@@ -9,7 +9,7 @@
 #include "../../include/class_sample.h"
 #include "ks_common.h"
 
-#define SP_NT 256  /* threads of a row: its steps are short, and more wavefronts would only share their instructions' time */
+#define SP_NT 512  /* threads of a row: with 256 1 x 10,000 fp32, k = 50 takes 2 us less, 256 x 390,625 bf16, k = 500 20 more */
 #define SP_NT2 1024 /* where much is kept */
 #define SP_CHUNK 512     /* classes that a wavefront takes at a time: eight consecutive ones a lane */
 #define SP_GRANULES 4096 /* most granules of a row */
@@ -377,20 +377,16 @@ template <typename T> __device__ __forceinline__ int sp_first(const SpArgs &a, c
 }
 
 // f(z, id) for eight classes a thread of the n listed granules; all lanes of a wavefront call it together
-template <int NT, int SP_AHEAD, typename T, typename F> __device__ __forceinline__ void sp_over_list(const SpArgs &a, const T *z, bool vec, const int32_t *list, int n, F f) {
+template <int NT, typename T, typename F>
+__device__ __forceinline__ void sp_over_list(const SpArgs &a, const T *z, bool vec, const int32_t *list, int n, F f) {
     if (a.gran <= SP_CHUNK) {
-        const int lanes = 1 << a.lg, at_once = NT >> a.lg, sub = threadIdx.x & (lanes - 1);
-        for (int i0 = 0; i0 < n; i0 += at_once * SP_AHEAD) { // several loads at a time
-            float v[SP_AHEAD][8];
-            int64_t e[SP_AHEAD];
-#pragma unroll
-            for (int u = 0; u < SP_AHEAD; ++u) {
-                const int i = i0 + u * at_once + (threadIdx.x >> a.lg);
-                e[u] = i < n ? list[i] * a.gran + sub * 8 : a.C;
-                sp_load(z, vec, e[u], a.C, v[u]);
-            }
-#pragma unroll
-            for (int u = 0; u < SP_AHEAD; ++u) f(v[u], (uint32_t)e[u]);
+        const int lanes = 1 << a.lg, at_once = NT >> a.lg, sub = threadIdx.x & (lanes - 1), own = threadIdx.x >> a.lg;
+        const auto at = [&](int i) __attribute__((always_inline)) { return i < n ? list[i] * a.gran + sub * 8 : a.C; };
+        for (int i0 = 0; i0 < n; i0 += at_once) {
+            const int64_t e = at(i0 + own);
+            float v[8];
+            sp_load(z, vec, e, a.C, v);
+            f(v, (uint32_t)e);
         }
     } else {
         const int lane = threadIdx.x & 63;
@@ -404,6 +400,7 @@ template <int NT, int SP_AHEAD, typename T, typename F> __device__ __forceinline
         }
     }
 }
+
 // p[0 .. size) into ascending order (bitonic), size a power of two, at least 64.  A wavefront's 64 pairs lie within 128 numbers where they are at
 // most 64 apart: only wider steps, and the first one after them, wait for the other wavefronts.
 template <int NT> __device__ __forceinline__ void sp_sort(uint64_t *p, int size) {
@@ -420,6 +417,72 @@ template <int NT> __device__ __forceinline__ void sp_sort(uint64_t *p, int size)
     __syncthreads();
 }
 
+struct SpOrder {
+    uint32_t n[SP_BINS];   // of buckets
+    int32_t slot[SP_CAND]; // of a place in its bucket
+    unsigned long long lo, hi;
+    uint32_t most;
+};
+// p[0 .. n) into ascending order: into buckets of equal ranges, then by counting inside them; with many in one bucket (equal logits) as above.
+// tmp: as long as p, p up to the next power of two.
+template <int NT> __device__ __forceinline__ void sp_order(uint64_t *p, uint64_t *tmp, int n, SpOrder &o, SpScan &sh) {
+    constexpr int EACH = SP_BINS / NT;
+    __syncthreads();
+    if (threadIdx.x == 0) { o.lo = ~0ull; o.hi = 0; o.most = 0; }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) o.n[i * NT + threadIdx.x] = 0;
+    uint64_t lo = ~(uint64_t)0, hi = 0;
+    for (int i = threadIdx.x; i < n; i += NT) {
+        lo = sp_min(lo, p[i]);
+        hi = sp_max(hi, p[i]);
+    }
+    __syncthreads();
+    if (lo <= hi) {
+        atomicMin(&o.lo, (unsigned long long)lo);
+        atomicMax(&o.hi, (unsigned long long)hi);
+    }
+    __syncthreads();
+    lo = o.lo;
+    const uint64_t span = o.hi - lo;
+    const int top = 63 - __clzll((long long)(span | 1)), shift = top < 11 ? 0 : top - 10; // span >> shift < 2^11
+    for (int i = threadIdx.x; i < n; i += NT) o.slot[i] = (int)atomicAdd(&o.n[(p[i] - lo) >> shift], 1u);
+    __syncthreads();
+    uint32_t mine = 0, most = 0, before, all;
+    uint64_t w0, w_all;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        mine += o.n[threadIdx.x * EACH + i];
+        most = sp_max(most, o.n[threadIdx.x * EACH + i]);
+    }
+    if (most > 64) atomicMax(&o.most, most);
+    sp_scan<NT>(sh, 0, mine, w0, before, w_all, all);
+    if (o.most > 512) {
+        int size = 64;
+        while (size < n) size <<= 1;
+        for (int i = n + threadIdx.x; i < size; i += NT) p[i] = ~(uint64_t)0;
+        __syncthreads();
+        sp_sort<NT>(p, size);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const uint32_t k = o.n[threadIdx.x * EACH + i];
+        o.n[threadIdx.x * EACH + i] = before;
+        before += k;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += NT) tmp[o.n[(p[i] - lo) >> shift] + o.slot[i]] = p[i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += NT) {
+        const uint64_t place = tmp[i];
+        const int b = (int)((place - lo) >> shift), first = (int)o.n[b], last = b + 1 < SP_BINS ? (int)o.n[b + 1] : n;
+        int at = first;
+        for (int j = first; j < last; ++j) at += tmp[j] < place;
+        p[at] = place;
+    }
+    __syncthreads();
+}
+
 __device__ __forceinline__ void sp_share_row(const SpArgs &a, int row, float top, int b0, uint64_t target_p);
 struct SpShared {
     SpScan scan;
@@ -431,7 +494,10 @@ struct SpShared {
         int32_t list[SP_GRANULES]; // granules
         uint64_t cand_w[SP_CAND];  // the candidates' weights, 0 for those that are not kept
     };
-    int32_t member[SP_CAND]; // candidates of one range of ids
+    union {
+        int32_t member[SP_CAND]; // candidates of one range of ids
+        SpOrder order;
+    };
     uint32_t fill;
 };
 
@@ -538,15 +604,15 @@ sp_draw_kernel(SpArgs a) {
             for (int g = g0; g < g1; ++g)
                 if (sp_bin(sh.top[g], top, c32) <= b0) sh.list[n0++] = g;
             __syncthreads();
-            sp_over_list<NT, 4>(a, z, vec, sh.list, (int)n_all, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+            sp_over_list<NT>(a, z, vec, sh.list, (int)n_all, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+                float best = v[0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) best = fmaxf(best, v[i]);
+                if (sp_bin(best, top, c32) > b0) return;
                 uint32_t in = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) in |= (uint32_t)(sp_bin(v[i], top, c32) <= b0) << i;
-                if (__ballot(in) == 0) return;
-                const uint32_t mine = __popc(in), upto = (uint32_t)ks_wave_iscan((int)mine);
-                uint32_t at = 0;
-                if (lane == 63) at = atomicAdd(&sh.fill, upto);
-                at = __builtin_amdgcn_readlane(at, 63) + upto - mine;
+                uint32_t at = atomicAdd(&sh.fill, (uint32_t)__popc(in));
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     if (in >> i & 1) {
@@ -563,22 +629,17 @@ sp_draw_kernel(SpArgs a) {
             return;
         }
         if (n <= NT) { // a candidate's place in the order is the number of those before it; several threads count for one where there are few
-            const int lg = n <= 64 ? 6 : n <= 128 ? 7 : 8, each = threadIdx.x & ((1 << lg) - 1), parts = NT >> lg, part = threadIdx.x >> lg;
+            const int lg = n <= 64 ? 6 : n <= 128 ? 7 : n <= 256 ? 8 : 9, each = threadIdx.x & ((1 << lg) - 1), parts = NT >> lg, part = threadIdx.x >> lg;
             const uint64_t place = each < n ? sh.cand[each] : 0;
             uint32_t before = 0;
 #pragma unroll 4
             for (int j = part; j < n; j += parts) before += sh.cand[j] < place;
-            if (threadIdx.x < NT) sh.member[threadIdx.x] = 0;
+            sh.member[threadIdx.x] = 0;
             __syncthreads();
             if (each < n) atomicAdd(&sh.member[each], (int)before);
             __syncthreads();
             if (part == 0 && each < n) sh.cand[sh.member[each]] = place;
-        } else {
-            int size = 2 * NT;
-            while (size < n) size <<= 1;
-            for (int i = n + threadIdx.x; i < size; i += NT) sh.cand[i] = ~(uint64_t)0;
-            sp_sort<NT>(sh.cand, size);
-        }
+        } else sp_order<NT>(sh.cand, sh.cand_w, n, sh.order, sh.scan);
         __syncthreads();
         const int each = (n + NT - 1) / NT;
         c0 = sp_min((int)threadIdx.x * each, n);
@@ -727,7 +788,7 @@ __device__ __forceinline__ uint64_t sp_refine(const SpArgs &a, const T *z, bool 
     uint32_t n = sh.n[bin];
     while (n > SP_MANY_CAND) {
         uint64_t least = ~(uint64_t)0, most = 0;
-        sp_over_list<SP_NT2, 1>(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+        sp_over_list<SP_NT2>(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint64_t place = sp_place(v[i], id + i);
@@ -748,7 +809,7 @@ __device__ __forceinline__ uint64_t sp_refine(const SpArgs &a, const T *z, bool 
         int shift = 0;
         while ((most - least) >> shift >= SP_BINS) ++shift;
         sp_clear<SP_NT2>(sh.sub.n, sh.sub.w);
-        sp_over_list<SP_NT2, 1>(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+        sp_over_list<SP_NT2>(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint64_t place = sp_place(v[i], id + i);
@@ -774,7 +835,7 @@ __device__ __forceinline__ uint64_t sp_refine(const SpArgs &a, const T *z, bool 
     while (size < (int)n) size <<= 1;
     for (int i = n + threadIdx.x; i < size; i += SP_NT2) sh.cand[i] = ~(uint64_t)0;
     __syncthreads();
-    sp_over_list<SP_NT2, 1>(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+    sp_over_list<SP_NT2>(a, z, vec, sh.list, sh.n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint64_t place = sp_place(v[i], id + i);
@@ -813,6 +874,7 @@ __device__ __forceinline__ uint64_t sp_refine(const SpArgs &a, const T *z, bool 
 struct SpFinal {
     SpScan scan;
     uint64_t cand[SP_CAND], cand_w[SP_CAND], g_w[SP_GRANULES];
+    SpOrder order;
 };
 template <typename T> __device__ __forceinline__ void sp_final(const SpArgs &a, int row, SpFinal &sh) {
     constexpr int NT = SP_NT2;
@@ -828,11 +890,7 @@ template <typename T> __device__ __forceinline__ void sp_final(const SpArgs &a, 
     const uint32_t n = st.n_cand;
     for (int g = threadIdx.x; g < a.ngr; g += NT) sh.g_w[g] = g_w[g];
     for (int i = threadIdx.x; i < (int)n; i += NT) sh.cand[i] = a.pool[st.cand0 + i];
-    int size = 64;
-    while (size < (int)n) size <<= 1;
-    for (int i = n + threadIdx.x; i < size; i += NT) sh.cand[i] = ~(uint64_t)0;
-    __syncthreads();
-    if (n) sp_sort<NT>(sh.cand, size);
+    if (n) sp_order<NT>(sh.cand, sh.cand_w, n, sh.order, sh.scan);
     const int each = (n + NT - 1) / NT, c0 = sp_min((int)threadIdx.x * each, (int)n), c1 = sp_min(c0 + each, (int)n);
     // the last class that top-k, then top-p keeps
     uint64_t cut = ~(uint64_t)0, w0, all, target = st.target_p, sum = 0;
@@ -952,7 +1010,7 @@ sp_many_kernel(SpArgs a) {
     sp_clear<SP_NT2>(sh.n, sh.w);
     uint64_t cut = ~(uint64_t)0;
     if (rule.use_k || rule.use_p) {
-        sp_over_list<SP_NT2, 1>(a, z, vec, sh.list, n_list, [&](const float (&v)[8], uint32_t) __attribute__((always_inline)) {
+        sp_over_list<SP_NT2>(a, z, vec, sh.list, n_list, [&](const float (&v)[8], uint32_t) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int b = sp_bin(v[i], top, c32);
@@ -985,7 +1043,7 @@ sp_many_kernel(SpArgs a) {
     __syncthreads();
     const int at_once = SP_NT2 >> a.lg;
     int turn = 0; // which of its granules a thread is at
-    sp_over_list<SP_NT2, 1>(a, z, vec, sh.list, n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
+    sp_over_list<SP_NT2>(a, z, vec, sh.list, n_list, [&](const float (&v)[8], uint32_t id) __attribute__((always_inline)) {
         uint64_t sum = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
