@@ -239,18 +239,24 @@ __device__ __forceinline__ void m4_finish(const f32x16_t (&acc)[2], float scale,
         for (int r = 0; r < 16; ++r) {
             m4_store2(to, off, fmaf(acc[0][r], scale, b[0]), fmaf(acc[1][r], scale, b[1]), (const OUT *)nullptr);
             off += r % 4 < 3 ? row_bytes : 5 * row_bytes; // the other half of the wavefront holds the four rows between
+            asm volatile("" : "+v"(off));                 // one register, not sixteen that are kept from call to call
         }
     }
-    if (!vec || c0 + M4_GROUP > C) // element by element; of pairs only the last class that has none
+    if (!vec || c0 + M4_GROUP > C) { // element by element; of pairs only the last class that has none
+        int rows = B - m0 - half4;
+        asm volatile("" : "+v"(rows), "+s"(ldl));
+        OUT *p = out + (int64_t)(m0 + half4) * ldl + c;
+        const bool one = c < C && (!vec || c + 1 == C), two = c + 1 < C && !vec;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            const int m = m0 + half4 + r / 4 * 8 + r % 4;
-            OUT *const p = out + (int64_t)m * ldl + c;
-            if (m < B) {
-                if (c < C && (!vec || c + 1 == C)) m4_store(p, fmaf(acc[0][r], scale, b[0]));
-                if (c + 1 < C && !vec) m4_store(p + 1, fmaf(acc[1][r], scale, b[1]));
+            if (r / 4 * 8 + r % 4 < rows) {
+                if (one) m4_store(p, fmaf(acc[0][r], scale, b[0]));
+                if (two) m4_store(p + 1, fmaf(acc[1][r], scale, b[1]));
             }
+            p += r % 4 < 3 ? ldl : 5 * ldl;
+            asm volatile("" : "+v"(p));
         }
+    }
 }
 __device__ __forceinline__ void m4_bias_of(const float *__restrict__ bias, int64_t c0, int64_t C, float (&b)[2]) {
     const int64_t c = c0 + 2 * (threadIdx.x & 31);
@@ -342,6 +348,350 @@ m4_direct_kernel(const uint8_t *__restrict__ xq, const uint8_t *__restrict__ wq,
     for (int s = 0; s < S; ++s) m4_finish(acc[s], scale, b, grp * M4_GROUP, C, (sb + s) * 32, B, out, ldl, vec);
 }
 
+// The work of a workgroup that keeps samples: stretches of an XCD's class groups for one sample tile each.  Workgroup i runs on XCD i % 8, and
+// the groups are dealt to the XCDs in eight ranges; the tiles of a round, at most eight, are taken by as many workgroups side by side, which
+// are at the same groups at the same time and share their codes in the L2.
+struct M4Share {
+    int g_lo, g_n, n_sb, sb0; // the XCD's groups; tiles, those of the rounds before
+    __device__ __forceinline__ M4Share(int groups, int n_sb_) {
+        const int xcd = blockIdx.x & 7;
+        g_lo = (int)((int64_t)groups * xcd / 8);
+        g_n = (int)((int64_t)groups * (xcd + 1) / 8) - g_lo;
+        n_sb = n_sb_;
+        sb0 = 0;
+    }
+    // the next stretch: groups [first, last) of g_lo on, for tile sb (none: first >= last)
+    __device__ __forceinline__ bool next(int &sb, int &first, int &last) {
+        if (sb0 >= n_sb) return false;
+        const int rounds = (n_sb - sb0 + 7) / 8, tiles = (n_sb - sb0 + rounds - 1) / rounds;
+        const int sets = (int)(gridDim.x >> 3) / tiles, j = blockIdx.x >> 3, set = j / tiles;
+        sb = sb0 + j % tiles;
+        first = set < sets ? (int)((int64_t)g_n * set / sets) : 0;
+        last = set < sets ? (int)((int64_t)g_n * (set + 1) / sets) : 0;
+        sb0 += tiles;
+        return true;
+    }
+};
+
+// The last of an odd number of classes, which has no pair to be stored with: the wavefronts of all workgroups take 32 samples each.
+template <typename OUT>
+__device__ __forceinline__ void m4_last_class(const uint8_t *xq, const uint8_t *wq, const float *bias, int64_t C, int kb, int B, float scale, OUT *out, int64_t ldl) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, bytes = m4_row_bytes(kb);
+    const uint8_t *const w = wq + (C - 1) / M4_GROUP * 2 * bytes; // C is odd: slot (C - 1) % 64 / 2 of the group's first codes
+    for (int sb = blockIdx.x * waves + wave; sb * 32 < B; sb += gridDim.x * waves) {
+        const uint8_t *const x = xq + (int64_t)sb * bytes;
+        f32x16_t acc;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+        for (int k = 0; k < kb; ++k) {
+            const int ex = *(const int *)(x + kb * M4_PIECE + k / 4 * M4_EXPS + lane * 4) >> k % 4 * 8, ew = *(const int *)(w + kb * M4_PIECE + k / 4 * M4_EXPS + lane * 4) >> k % 4 * 8;
+            acc = m4_mfma<0>(*(const m4_i32x4 *)(x + k * M4_PIECE + lane * 16), *(const m4_i32x4 *)(w + k * M4_PIECE + lane * 16), acc, ex, ew);
+        }
+        const float b = bias ? bias[C - 1] : 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int m = sb * 32 + 4 * (lane >> 5) + r / 4 * 8 + r % 4;
+            if (m < B && (lane & 31) == (int)((C - 1) % M4_GROUP / 2)) m4_store(out + (int64_t)m * ldl + C - 1, fmaf(acc[r], scale, b));
+        }
+    }
+}
+
+#define M4X_NT 512
+// Rows of up to 512 elements: a wavefront keeps the codes of 64 classes in registers, a workgroup those of up to 4,096 / KB samples in LDS, and
+// the samples go past 32 at a time: 2 KB matrix instructions a block, with the stores of the block before in between.  During a group's
+// last block each piece of codes is replaced, when it has been used, by the next group's.
+template <int KB, typename OUT>
+__global__ void __launch_bounds__(M4X_NT, 2)
+m4_steady_kernel(const uint8_t *__restrict__ xq, const uint8_t *__restrict__ wq, const float *__restrict__ bias, int64_t C, int kb, int B, float scale,
+                 OUT *__restrict__ out, int64_t ldl, int tile) { // tile: blocks of 32 samples at a time, even, at most 128 / KB
+    constexpr int NW = M4X_NT / 64, KQ = KB / 4;
+    __shared__ __attribute__((aligned(16))) char s_x[128 * M4_PIECE];
+    __shared__ int s_e[128 / 4 * 64];
+    __shared__ int s_next; // group that the next wavefront to ask gets: of two on a SIMD the older one runs ahead
+    const uint32_t row_bytes = (uint32_t)(ldl * sizeof(OUT)); // 32 rows: less than 2^31 bytes
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half4 = 4 * (lane >> 5);
+    const int xblocks = (B + 31) / 32, n_sb = (xblocks + tile - 1) / tile, bytes = m4_row_bytes(kb);
+    const int groups = (int)((C + M4_GROUP - 1) / M4_GROUP);
+    M4Share share(groups, n_sb);
+    const int g_lo = share.g_lo;
+    int sb, first, last;
+    while (share.next(sb, first, last)) {
+        if (first >= last) continue;
+        __syncthreads();
+        for (int p = wave; p < tile * KB; p += NW) { // k-step k of block i at (KB i + k), 0 beyond the depth
+            const int blk = sb * tile + p / KB < xblocks ? sb * tile + p / KB : xblocks - 1, k = p % KB;
+            m4_i32x4 v = {0, 0, 0, 0};
+            if (k < kb) v = *(const m4_i32x4 *)(xq + (int64_t)blk * bytes + k * M4_PIECE + lane * 16);
+            *(m4_i32x4 *)(s_x + p * M4_PIECE + lane * 16) = v;
+        }
+        for (int p = wave; p < tile * KQ; p += NW) {
+            const int blk = sb * tile + p / KQ < xblocks ? sb * tile + p / KQ : xblocks - 1, q = p % KQ;
+            s_e[p * 64 + lane] = q * 4 < kb ? *(const int *)(xq + (int64_t)blk * bytes + kb * M4_PIECE + q * M4_EXPS + lane * 4) : 0;
+        }
+        if (threadIdx.x == 0) s_next = first + NW;
+        __syncthreads();
+
+        int grp = first + wave;
+        if (grp >= last) continue;
+        const auto group_codes = [&](int g, int q) __attribute__((always_inline)) { // of a half of a group: 0 beyond the depth
+            return __builtin_amdgcn_make_buffer_rsrc((void *)(wq + ((int64_t)(g_lo + g) * 2 + q) * bytes), 0, kb * M4_PIECE, 0x00020000);
+        };
+        const auto group_exps = [&](int g, int q) __attribute__((always_inline)) {
+            return __builtin_amdgcn_make_buffer_rsrc((void *)(wq + ((int64_t)(g_lo + g) * 2 + q) * bytes + kb * M4_PIECE), 0, (kb + 3) / 4 * M4_EXPS, 0x00020000);
+        };
+        const auto codes = [&](__amdgpu_buffer_rsrc_t p, int k) __attribute__((always_inline)) {
+            return __builtin_bit_cast(m4_i32x4, __builtin_amdgcn_raw_buffer_load_b128(p, lane * 16, k * M4_PIECE, 0));
+        };
+        m4_i32x4 w[KB][2], x[4];
+        int ew[KQ][2], ex[2][KQ];
+        f32x16_t acc[2][2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const __amdgpu_buffer_rsrc_t p = group_codes(grp, q), e = group_exps(grp, q);
+#pragma unroll
+            for (int k = 0; k < KB; ++k) w[k][q] = codes(p, k);
+#pragma unroll
+            for (int k = 0; k < KQ; ++k) ew[k][q] = __builtin_amdgcn_raw_buffer_load_b32(e, lane * 4, k * M4_EXPS, 0);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = *(const m4_i32x4 *)(s_x + k * M4_PIECE + lane * 16);
+#pragma unroll
+        for (int k = 0; k < KQ; ++k) ex[0][k] = s_e[k * 64 + lane];
+        // the block that is finished while the next one is multiplied; none yet: a buffer of no bytes
+        __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc(out, 0, 0, 0x00020000);
+        uint32_t off = 0;
+        float b[2] = {0.f, 0.f};
+        const auto finish = [&](const f32x16_t (&a)[2], int r) __attribute__((always_inline)) { // one row of each half
+            m4_store2(to, off, fmaf(a[0][r], scale, b[0]), fmaf(a[1][r], scale, b[1]), (const OUT *)nullptr);
+            off += r % 4 < 3 ? row_bytes : 5 * row_bytes;
+            asm volatile("" : "+v"(off)); // one register, not sixteen that are kept for every block
+        };
+        while (grp < last) {
+            int got = 0;
+            if (lane == 0) got = atomicAdd(&s_next, 1);
+            const int next = __builtin_amdgcn_readfirstlane(got);
+            const int g_next = next < last ? next : grp;
+            const __amdgpu_buffer_rsrc_t p_next[2] = {group_codes(g_next, 0), group_codes(g_next, 1)}, e_next[2] = {group_exps(g_next, 0), group_exps(g_next, 1)};
+            const int64_t c0 = (int64_t)(g_lo + grp) * M4_GROUP, c = c0 + 2 * (lane & 31);
+            float nb[2];
+            m4_bias_of(bias, c0, C, nb);
+            const uint32_t off0 = c + 1 < C ? half4 * row_bytes + 2 * (lane & 31) * (uint32_t)sizeof(OUT) : M4_NO_CLASS;
+            const auto block = [&](int blk, f32x16_t (&a)[2], const f32x16_t (&before)[2], const int (&e)[KQ], int (&e_after)[KQ], auto reload) __attribute__((always_inline)) {
+                const int after = reload ? 0 : blk + 1;
+                const char *xp = s_x + blk * (KB * M4_PIECE) + lane * 16, *xn = s_x + after * (KB * M4_PIECE) + lane * 16;
+#pragma unroll
+                for (int k = 0; k < KQ; ++k) e_after[k] = s_e[(after * KQ + k) * 64 + lane];
+                const auto step = [&](int k4, auto j) __attribute__((always_inline)) {
+                    const int k = k4 * 4 + j.value;
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        if (k == 0) a[q] = m4_mfma<0>(x[0], w[0][q], f32x16_t{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0}, e[0], ew[0][q]);
+                        else a[q] = m4_mfma<j.value>(x[k & 3], w[k][q], a[q], e[k4], ew[k4][q]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    x[k & 3] = *(const m4_i32x4 *)(k + 4 < KB ? xp + (k + 4) * M4_PIECE : xn + (k + 4 - KB) * M4_PIECE);
+                    if (reload)
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            w[k][q] = codes(p_next[q], k);
+                            if (j.value == 3) ew[k4][q] = __builtin_amdgcn_raw_buffer_load_b32(e_next[q], lane * 4, k4 * M4_EXPS, 0);
+                        }
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (r * KB / 16 == k) finish(before, r);
+                };
+#pragma unroll
+                for (int k4 = 0; k4 < KQ; ++k4) {
+                    step(k4, std::integral_constant<int, 0>());
+                    step(k4, std::integral_constant<int, 1>());
+                    step(k4, std::integral_constant<int, 2>());
+                    step(k4, std::integral_constant<int, 3>());
+                }
+                to = m4_rows_of(out, ldl, (sb * tile + blk) * 32, c0, C, B);
+                off = off0;
+                b[0] = nb[0];
+                b[1] = nb[1];
+            };
+            for (int i = 0; i + 2 < tile; i += 2) {
+                block(i, acc[0], acc[1], ex[0], ex[1], std::false_type());
+                block(i + 1, acc[1], acc[0], ex[1], ex[0], std::false_type());
+            }
+            block(tile - 2, acc[0], acc[1], ex[0], ex[1], std::false_type());
+            block(tile - 1, acc[1], acc[0], ex[1], ex[0], std::true_type());
+            grp = next;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) finish(acc[1], r);
+    }
+    if (C & 1) m4_last_class(xq, wq, bias, C, kb, B, scale, out, ldl);
+}
+
+// workgroup barrier that waits for this wavefront's LDS accesses but, unlike __syncthreads(), not for loads in flight
+__device__ __forceinline__ void m4_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F); // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Deeper rows: the samples pass through LDS in chunks of eight k-steps, which eight wavefronts with 64 classes each read at the same time: three
+// buffers, a barrier a chunk.  While chunk t is multiplied, a fragment is read for the next k-step when it has been used (the last ones
+// from chunk t + 1, which is there since the barrier), and chunk t + 2 is written to LDS from registers.  Weights come straight from memory,
+// four k-steps ahead.  The chunks run on from one tile of 512 classes by 128 samples to the next; what lies beyond the depth is loaded as 0.
+template <typename OUT>
+__global__ void __launch_bounds__(M4X_NT, 2)
+m4_staged_kernel(const uint8_t *__restrict__ xq, const uint8_t *__restrict__ wq, const float *__restrict__ bias, int64_t C, int kb, int B, float scale,
+                 OUT *__restrict__ out, int64_t ldl, int vec) {
+    constexpr int NW = M4X_NT / 64, R = 8, CHUNK = R * 4 * M4_PIECE, EXPS = R / 4 * 4 * 64 /* words of a chunk's exponents */;
+    __shared__ __attribute__((aligned(16))) char s_x[3 * CHUNK];
+    __shared__ int s_e[3 * EXPS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int xblocks = (B + 31) / 32, n_sb = (B + 127) / 128, chunks = (kb + R - 1) / R, bytes = m4_row_bytes(kb);
+    const int groups = (int)((C + M4_GROUP - 1) / M4_GROUP), n_ct = (groups + NW - 1) / NW;
+    // workgroup i runs on XCD i % 8; an XCD has a range of the class tiles, and its workgroups take them for all samples before the
+    // next ones: what 32 of them read at a time are a few class tiles and the samples
+    const int xcd = blockIdx.x & 7, per_xcd = gridDim.x >> 3, j0 = blockIdx.x >> 3;
+    const int c_lo = (int)((int64_t)n_ct * xcd / 8), c_n = (int)((int64_t)n_ct * (xcd + 1) / 8) - c_lo;
+    int64_t left = (int64_t)c_n * n_sb - j0; // tiles from this one on, of this and the XCD's other workgroups
+    const int step_c = per_xcd / n_sb, step_s = per_xcd % n_sb; // from one of this workgroup's tiles to its next
+    int ct = c_lo + j0 / n_sb, sb = j0 % n_sb;
+
+    // samples: this wavefront moves k-step `wave` of a chunk, for four blocks of samples, and one word of exponents
+    int64_t r_left = left;
+    int r_sb = sb, r_c = 0; // chunk that is requested next
+    m4_i32x4 held[2];
+    int held_e;
+    const auto request = [&](auto h) __attribute__((always_inline)) { // a half of it
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int s = r_sb * 4 + h.value * 2 + i, blk = s < xblocks ? s : xblocks - 1;
+            const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void *)(xq + (int64_t)blk * bytes), 0, kb * M4_PIECE, 0x00020000);
+            held[i] = __builtin_bit_cast(m4_i32x4, __builtin_amdgcn_raw_buffer_load_b128(from, lane * 16, (r_c * R + wave) * M4_PIECE, 0));
+        }
+        if (h.value == 0) {
+            const int s = r_sb * 4 + (wave & 3), blk = s < xblocks ? s : xblocks - 1;
+            const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void *)(xq + (int64_t)blk * bytes + kb * M4_PIECE), 0, (kb + 3) / 4 * M4_EXPS, 0x00020000);
+            held_e = __builtin_amdgcn_raw_buffer_load_b32(from, lane * 4, (r_c * 2 + (wave >> 2)) * M4_EXPS, 0);
+        } else { // behind the last tile: the same again, read by nobody
+            const bool end = ++r_c == chunks, more = end && r_left > per_xcd;
+            r_c = end ? 0 : r_c;
+            r_left = more ? r_left - per_xcd : r_left;
+            r_sb = more ? r_sb + step_s : r_sb;
+            r_sb = r_sb >= n_sb ? r_sb - n_sb : r_sb;
+        }
+    };
+    const auto place = [&](auto h, char *to, int *to_e) __attribute__((always_inline)) { // k-step k of block s at (4 k + s)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) *(m4_i32x4 *)(to + (wave * 4 + h.value * 2 + i) * M4_PIECE + lane * 16) = held[i];
+        if (h.value == 0) to_e[wave * 64 + lane] = held_e;
+    };
+    const std::integral_constant<int, 0> H0;
+    const std::integral_constant<int, 1> H1;
+    const auto rsrc = [&](int tile, int q, bool exps) __attribute__((always_inline)) { // of this wavefront's classes in a tile; beyond the last group: that one
+        const int g = tile * NW + wave;
+        const uint8_t *const p = wq + ((int64_t)(g < groups ? g : groups - 1) * 2 + q) * bytes;
+        return __builtin_amdgcn_make_buffer_rsrc((void *)(exps ? p + kb * M4_PIECE : p), 0, exps ? (kb + 3) / 4 * M4_EXPS : kb * M4_PIECE, 0x00020000);
+    };
+    char *b0 = s_x, *b1 = s_x + CHUNK, *b2 = s_x + 2 * CHUNK; // chunks t, t + 1, t + 2
+    int *e0 = s_e, *e1 = s_e + EXPS, *e2 = s_e + 2 * EXPS;
+    request(H0);
+    place(H0, b0, e0);
+    request(H1);
+    place(H1, b0, e0);
+    request(H0);
+    place(H0, b1, e1);
+    request(H1);
+    place(H1, b1, e1);
+    request(H0);
+    m4_i32x4 w[4][2], x[4];
+    int ew[2][2], ex[4]; // ew: of this and of the next four k-steps
+    __amdgpu_buffer_rsrc_t wr[2] = {rsrc(ct, 0, false), rsrc(ct, 1, false)}, er[2] = {rsrc(ct, 0, true), rsrc(ct, 1, true)};
+#pragma unroll
+    for (int q = 0; q < 2; ++q) ew[0][q] = __builtin_amdgcn_raw_buffer_load_b32(er[q], lane * 4, 0, 0);
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) w[kk][q] = __builtin_bit_cast(m4_i32x4, __builtin_amdgcn_raw_buffer_load_b128(wr[q], lane * 16, kk * M4_PIECE, 0));
+    m4_barrier();
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        x[s] = *(const m4_i32x4 *)(b0 + s * M4_PIECE + lane * 16);
+        ex[s] = e0[s * 64 + lane];
+    }
+    for (; left > 0; left -= per_xcd) {
+        int next_ct = ct + step_c, next_sb = sb + step_s;
+        if (next_sb >= n_sb) { next_sb -= n_sb; ++next_ct; }
+        if (left <= per_xcd) next_ct = ct;
+        f32x16_t acc[4][2];
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[s][q][r] = 0.f;
+        for (int c = 0; c < chunks; ++c) {
+            // four k-steps on: the second half of this chunk, then the first of the next one (of the next tile)
+            const int at_mid = (c * R + 4) * M4_PIECE, at_next = c + 1 < chunks ? (c + 1) * R * M4_PIECE : 0;
+            // no branch for that: behind one the compiler would gather all matrix instructions before it
+            const int after = c + 1 < chunks ? ct : next_ct;
+            const __amdgpu_buffer_rsrc_t wn[2] = {rsrc(after, 0, false), rsrc(after, 1, false)}, en[2] = {rsrc(after, 0, true), rsrc(after, 1, true)};
+            m4_barrier(); // chunk t + 1 is whole, and nobody reads chunk t - 1 any more
+            const auto step = [&](auto K) __attribute__((always_inline)) {
+                constexpr int kk = K.value, half = kk / 4, j = kk % 4;
+                if (j == 0) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) ew[1 - half][q] = __builtin_amdgcn_raw_buffer_load_b32(half == 0 ? er[q] : en[q], lane * 4, (half == 0 ? at_mid : at_next) / (4 * M4_PIECE) * M4_EXPS, 0);
+                }
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) acc[s][q] = m4_mfma<j>(x[s], w[j][q], acc[s][q], ex[s], ew[half][q]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    x[s] = *(const m4_i32x4 *)((kk < R - 1 ? b0 + (kk + 1) * 4 * M4_PIECE : b1) + s * M4_PIECE + lane * 16);
+                    if (j == 3) ex[s] = (half == 0 ? e0 + 4 * 64 : e1)[s * 64 + lane];
+                    if (s == 3)
+#pragma unroll
+                        for (int q = 0; q < 2; ++q)
+                            w[j][q] = __builtin_bit_cast(m4_i32x4, __builtin_amdgcn_raw_buffer_load_b128(half == 0 ? wr[q] : wn[q], lane * 16, (half == 0 ? at_mid : at_next) + j * M4_PIECE, 0));
+                }
+                if (kk == 2) {
+                    place(H0, b2, e2);
+                    request(H1);
+                }
+                if (kk == 6) {
+                    place(H1, b2, e2);
+                    request(H0);
+                }
+            };
+            step(std::integral_constant<int, 0>());
+            step(std::integral_constant<int, 1>());
+            step(std::integral_constant<int, 2>());
+            step(std::integral_constant<int, 3>());
+            step(std::integral_constant<int, 4>());
+            step(std::integral_constant<int, 5>());
+            step(std::integral_constant<int, 6>());
+            step(std::integral_constant<int, 7>());
+#pragma unroll
+            for (int q = 0; q < 2; ++q) { wr[q] = wn[q]; er[q] = en[q]; }
+            char *const b = b0;
+            b0 = b1; b1 = b2; b2 = b;
+            int *const e = e0;
+            e0 = e1; e1 = e2; e2 = e;
+        }
+        const int g = ct * NW + wave;
+        if (g < groups) {
+            float b[2];
+            m4_bias_of(bias, (int64_t)g * M4_GROUP, C, b);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) m4_finish(acc[s], scale, b, (int64_t)g * M4_GROUP, C, sb * 128 + s * 32, B, out, ldl, vec);
+        }
+        ct = next_ct;
+        sb = next_sb;
+    }
+}
+
 template <typename OUT>
 static void m4_logits(const uint8_t *xq, const uint8_t *wq, const float *bias, int64_t C, int D, int B, float scale, OUT *out, int64_t ldl, hipStream_t st) {
     // vec: pairs of classes in one store; 64 MB from row to row and more, whose offsets are no 32 bits, go element by element
@@ -353,7 +703,15 @@ static void m4_logits(const uint8_t *xq, const uint8_t *wq, const float *bias, i
     };
     const int64_t waves = groups * ks_ceil_div(B, 64);
     if (B <= 32) return waves <= 1024 && kb >= 16 ? direct(m4_direct_kernel<1, 4, OUT>, 32, 1) : direct(m4_direct_kernel<1, 1, OUT>, 32, 4);
-    return waves <= 320 && kb >= 16 ? direct(m4_direct_kernel<2, 4, OUT>, 64, 1) : direct(m4_direct_kernel<2, 1, OUT>, 64, 4);
+    if (B <= 64 || waves <= 1280 || (kb <= 8 && !vec))
+        return waves <= 320 && kb >= 16 ? direct(m4_direct_kernel<2, 4, OUT>, 64, 1) : direct(m4_direct_kernel<2, 1, OUT>, 64, 4);
+    if (kb > 8) {
+        hipLaunchKernelGGL(m4_staged_kernel<OUT>, dim3(256), dim3(M4X_NT), 0, st, xq, wq, bias, C, kb, B, scale, out, ldl, vec);
+        return;
+    }
+    const int KB = kb <= 4 ? 4 : 8, xblocks = (B + 31) / 32, most = 128 / KB, tiles = (xblocks + most - 1) / most, tile = ((xblocks + tiles - 1) / tiles + 1) / 2 * 2;
+    hipLaunchKernelGGL((KB == 4 ? m4_steady_kernel<4, OUT> : m4_steady_kernel<8, OUT>), dim3(256), dim3(M4X_NT), 0, st, xq,
+                       wq, bias, C, kb, B, scale, out, ldl, tile);
 }
 
 extern "C" int class_logits_mxfp4(const uint8_t *x_codes, const uint8_t *w_codes, const float *bias, int64_t C, int D, int B, float scale,
