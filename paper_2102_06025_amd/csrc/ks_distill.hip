@@ -9,6 +9,8 @@
 #include "ks_common.h"
 
 #define DS_NT 256
+#define DS_PARTS (DS_NT * DS_HELD)
+#define DS_HELD 8 /* vectors of 16 bytes that a thread holds: a slice is DS_NT * DS_HELD of them */
 
 struct DsArgs {
     const void *logits, *t_logits;
@@ -20,6 +22,7 @@ struct DsArgs {
     float *loss, *loss_mean;
     float2 *part;  // [B, parts]: largest logit, sum of the powers relative to it
     double *a;     // [B]: A
+    float2 *t;     // [B]: the teacher's largest logit, sum of the powers relative to it
     int32_t *dev_status;
 };
 
@@ -28,18 +31,18 @@ template <> struct DsVec<float> {
     static constexpr int N = 4;
     static __device__ __forceinline__ float one(const float *p) { return *p; }
     static __device__ __forceinline__ void put(float *p, float v) { *p = v; }
-    static __device__ __forceinline__ void load(const float *p, float (&v)[4]) {
-        const float4 a = *(const float4 *)p;
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    static __device__ __forceinline__ void values(uint4 a, float (&v)[4]) {
+        v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
     }
-    static __device__ __forceinline__ void store(float *p, const float (&v)[4]) { *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]); }
+    static __device__ __forceinline__ uint4 packed(const float (&v)[4]) {
+        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    }
 };
 template <> struct DsVec<uint16_t> {
     static constexpr int N = 8;
     static __device__ __forceinline__ float one(const uint16_t *p) { return ks_bf2f(*p); }
     static __device__ __forceinline__ void put(uint16_t *p, float v) { *p = (uint16_t)ks_f2bf(v); }
-    static __device__ __forceinline__ void load(const uint16_t *p, float (&v)[8]) {
-        const uint4 a = *(const uint4 *)p;
+    static __device__ __forceinline__ void values(uint4 a, float (&v)[8]) {
         const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -47,8 +50,8 @@ template <> struct DsVec<uint16_t> {
             v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
         }
     }
-    static __device__ __forceinline__ void store(uint16_t *p, const float (&v)[8]) {
-        *(uint4 *)p = make_uint4(ks_pack_bf2(v[0], v[1]), ks_pack_bf2(v[2], v[3]), ks_pack_bf2(v[4], v[5]), ks_pack_bf2(v[6], v[7]));
+    static __device__ __forceinline__ uint4 packed(const float (&v)[8]) {
+        return make_uint4(ks_pack_bf2(v[0], v[1]), ks_pack_bf2(v[2], v[3]), ks_pack_bf2(v[4], v[5]), ks_pack_bf2(v[6], v[7]));
     }
 };
 
@@ -76,6 +79,21 @@ template <typename T, bool VEC> struct DsSlice {
         if (VEC && i == a.slices - 1 && t < (int)(a.C - rest)) f(rest + t);
     }
 };
+
+// A thread's vectors of a slice, all requested at once; behind its end the last one again (one: there is at least that)
+__device__ __forceinline__ void ds_hold(const void *row, int64_t v0, int64_t v1, uint4 (&held)[DS_HELD]) {
+#pragma unroll
+    for (int i = 0; i < DS_HELD; ++i) {
+        const int64_t at = v0 + i * DS_NT + threadIdx.x;
+        held[i] = ((const uint4 *)row)[at < v1 ? at : v1 - 1];
+    }
+}
+
+// past the caches: nobody here reads a gradient, and the logits of the rows that come next stay in them
+__device__ __forceinline__ void ds_stream(void *p, uint4 v) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, (u32x4 *)p);
+}
 
 // (largest, sum of 2^(l (z - largest))): NaN and +infinity stay visible, -infinity adds nothing
 __device__ __forceinline__ void ds_join(float &m, float &s, float m2, float s2, float l) {
@@ -105,12 +123,12 @@ __device__ __forceinline__ float ds_block_max(float v, float *sh) {
     return fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
 }
 // the row's entries into LDS (ids, -1: empty, and weights), and their sum
-__device__ __forceinline__ DsTeacher ds_teacher(const DsArgs &a, int row, int32_t *s_id, float *s_q, float *sh, bool report) {
+__device__ __forceinline__ DsTeacher ds_teacher(const DsArgs &a, int row, int32_t *s_id, float *s_q, float *sh) {
     float top = -INFINITY;
     for (int k = threadIdx.x; k < a.K; k += DS_NT) {
         int id = a.t_ids[(int64_t)row * a.K + k];
         if (id >= a.C) {
-            if (report) ks_flag(a.dev_status, KS_DEV_BAD_LABEL);
+            ks_flag(a.dev_status, KS_DEV_BAD_LABEL);
             id = -1;
         }
         const float t = id >= 0 ? ds_t_logit(a, (int64_t)row * a.K + k) : -INFINITY;
@@ -142,19 +160,26 @@ ds_stats_kernel(DsArgs a) {
     typedef DsVec<T> V;
     constexpr int N = V::N;
     float m = -INFINITY, s = 0.f;
-    for (int64_t i = sl.v0 + threadIdx.x; i < sl.v1; i += DS_NT) {
-        float v[N];
-        V::load(z + sl.head + i * N, v);
-        float top = v[0];
+    if (sl.v0 < sl.v1) {
+        uint4 held[DS_HELD];
+        ds_hold(z + sl.head, sl.v0, sl.v1, held);
 #pragma unroll
-        for (int j = 1; j < N; ++j) top = fmaxf(top, v[j]);
-        if (top > m) { // seldom after the first ones
-            s *= __builtin_amdgcn_exp2f(a.l * (m - top));
-            m = top;
+        for (int i = 0; i < DS_HELD; ++i) { // a vector that is there twice changes no maximum
+            float v[N];
+            V::values(held[i], v);
+#pragma unroll
+            for (int j = 0; j < N; ++j) m = fmaxf(m, v[j]);
         }
         const float base = m > -INFINITY ? m : 0.f;
 #pragma unroll
-        for (int j = 0; j < N; ++j) s += __builtin_amdgcn_exp2f(a.l * (v[j] - base));
+        for (int i = 0; i < DS_HELD; ++i) {
+            if (sl.v0 + i * DS_NT + threadIdx.x >= sl.v1) break;
+            float v[N];
+            V::values(held[i], v);
+#pragma unroll
+            for (int j = 0; j < N; ++j) s += __builtin_amdgcn_exp2f(a.l * (v[j] - base));
+        }
+        if (s == 0.f) m = -INFINITY; // none of them was its own
     }
     sl.singles(a, blockIdx.x, [&](int64_t c) __attribute__((always_inline)) {
         ds_join(m, s, V::one(z + c), 1.f, a.l);
@@ -163,7 +188,8 @@ ds_stats_kernel(DsArgs a) {
     s = ds_block_sum(s * (m == base ? 1.f : __builtin_amdgcn_exp2f(a.l * (m - base))), sh);
     if (threadIdx.x == 0) a.part[(int64_t)row * a.parts + blockIdx.x] = make_float2(top, s);
     if (blockIdx.x) return;
-    const DsTeacher t = ds_teacher(a, row, s_id, s_q, sh, true);
+    const DsTeacher t = ds_teacher(a, row, s_id, s_q, sh);
+    if (threadIdx.x == 0) a.t[row] = make_float2(t.top, t.sum);
     double sum = 0.0;
     const double inv_T = 1.0 / (double)a.T, log_sum = log((double)t.sum);
     for (int k = threadIdx.x; k < a.K; k += DS_NT) {
@@ -180,69 +206,104 @@ ds_stats_kernel(DsArgs a) {
     if (threadIdx.x == 0) a.a[row] = shd[0] + shd[1] + shd[2] + shd[3];
 }
 
-// Second pass: the gradient of every slice, the first one also the row's loss.
+__device__ __forceinline__ uint32_t ds_pad(int K) { return (uint32_t)(K + 3) & ~3u; }
+// Second pass: the gradient of every slice, the first one also the row's loss.  What it has to look up is requested together with the slice's
+// logits, which stay in registers: every vector (of single elements: as many as make 2,048 parts) has a chain of the classes that the teacher
+// names in it, mostly none.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(DS_NT)
 ds_grad_kernel(DsArgs a) {
-    extern __shared__ int32_t s_id[];
-    float *const s_q = (float *)(s_id + a.K), *const s_grad = s_q + a.K;
-    uint8_t *const s_again = (uint8_t *)(s_grad + a.K);
-    __shared__ float sh[4];
-    const int row = a.row0 + blockIdx.y;
+    extern __shared__ __attribute__((aligned(16))) int32_t s_id[]; // [K, up to a multiple of 4], -1: empty
+    float *const s_q = (float *)(s_id + ds_pad(a.K)), *const s_sum = s_q + a.K;
+    uint16_t *const s_next = (uint16_t *)(s_sum + a.K); // chains of entries + 1; only a class's first entry is in one, s_sum: what all of them come to
+    __shared__ uint32_t s_chain[DS_PARTS + 1];          // the last: of the row's first and last elements, which are in no vector
+    typedef DsVec<T> V;
+    constexpr int N = DsSlice<T, VEC>::N, PART = V::N; // of single elements in a chain
+    const int row = a.row0 + blockIdx.y, lane = threadIdx.x & 63;
     const T *const z = (const T *)a.logits + (int64_t)row * a.ldl;
     T *const out = (T *)a.out + (int64_t)row * a.ldd;
     const DsSlice<T, VEC> sl(a, z, blockIdx.x);
-    typedef DsVec<T> V;
-    constexpr int N = DsSlice<T, VEC>::N;
-    // the row's largest logit and sum, in every workgroup in the same order
+    uint4 held[DS_HELD];
+    if (VEC && sl.v0 < sl.v1) ds_hold(z + sl.head, sl.v0, sl.v1, held);
+    const float2 t = a.t[row];
+    const bool some = t.y != 0.f;
+    for (int i = threadIdx.x; i <= DS_PARTS; i += DS_NT) s_chain[i] = 0;
+    for (int k = threadIdx.x; k < (int)ds_pad(a.K); k += DS_NT) {
+        const int id = k < a.K ? a.t_ids[(int64_t)row * a.K + k] : -1;
+        const float l = k < a.K ? ds_t_logit(a, (int64_t)row * a.K + k) : -INFINITY;
+        const bool there = id >= 0 && id < a.C;
+        s_id[k] = there ? id : -1;
+        if (k < a.K) s_q[k] = !there || l == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(a.l * (l - t.x));
+    }
+    // the row's largest logit and sum, in every wavefront in the same order
     float m = -INFINITY, s = 0.f;
-    for (int i = threadIdx.x; i < a.parts; i += DS_NT) {
+    for (int i = lane; i < a.parts; i += 64) {
         const float2 p = a.part[(int64_t)row * a.parts + i];
         ds_join(m, s, p.x, p.y, a.l);
     }
-    const float top = ds_block_max(m, sh), base = top > -INFINITY ? top : 0.f;
-    s = ds_block_sum(s * (m == base ? 1.f : __builtin_amdgcn_exp2f(a.l * (m - base))), sh);
-    const DsTeacher t = ds_teacher(a, row, s_id, s_q, sh, false);
-    const bool some = t.sum != 0.f;
+    const float top = ks_wave_max(m), base = top > -INFINITY ? top : 0.f;
+    s = ks_wave_sum(s * (m == base ? 1.f : __builtin_amdgcn_exp2f(a.l * (m - base))));
     // p = 2^(l (z - base)) * f; a row without a class has p = 0, one with a NaN or +infinity NaN
-    const float f = !some || s == 0.f ? 0.f : top < INFINITY ? a.g / s : __int_as_float(0x7FC00000);
-    if (blockIdx.x == 0 && threadIdx.x == 0)
-        a.loss[row] = some ? (float)((double)a.T * (double)a.T * (a.a[row] + (s == 0.f ? 0.0 : (double)base / (double)a.T + log((double)s)))) : 0.f;
+    const float f = !some || s == 0.f ? 0.f : top < INFINITY ? a.g / s : __int_as_float(0x7FC00000), to_q = some ? a.g / t.y : 0.f;
     const auto grad = [&](float v) __attribute__((always_inline)) { return f == 0.f ? 0.f : __builtin_amdgcn_exp2f(a.l * (v - base)) * f; };
-    // the gradient at the named classes of this slice, before their logits may be overwritten: at a class's first entry, the others empty
-    const float to_q = some ? a.g / t.sum : 0.f;
     __syncthreads();
+    const int64_t from = sl.head + sl.v0 * N; // of the first vector
     for (int k = threadIdx.x; k < a.K; k += DS_NT) {
         const int id = s_id[k];
         if (id < sl.first || id >= sl.last) continue;
         float q = 0.f;
-        bool again = false;
-        for (int j = 0; j < a.K; ++j)
-            if (s_id[j] == id) {
-                again |= j < k;
-                q += s_q[j];
-            }
-        s_again[k] = again;
-        s_grad[k] = grad(V::one(z + id)) - to_q * q;
+        int before = k;
+#pragma unroll 4
+        for (int j = 0; j < a.K; j += 4) {
+            const int4 other = *(const int4 *)(s_id + j);
+            if (other.x == id) { q += s_q[j]; before = j < before ? j : before; }
+            if (other.y == id) { q += s_q[j + 1]; before = j + 1 < before ? j + 1 : before; }
+            if (other.z == id) { q += s_q[j + 2]; before = j + 2 < before ? j + 2 : before; }
+            if (other.w == id) { q += s_q[j + 3]; before = j + 3 < before ? j + 3 : before; }
+        }
+        if (before < k) continue;
+        s_sum[k] = q * to_q;
+        const int64_t at = (id - from) / N;
+        const int part = id >= from && at < sl.v1 - sl.v0 ? (int)(VEC ? at : at / PART) : DS_PARTS;
+        s_next[k] = (uint16_t)atomicExch(&s_chain[part], k + 1);
     }
     __syncthreads();
-    for (int64_t i = sl.v0 + threadIdx.x; i < sl.v1; i += DS_NT) {
-        float v[N];
-        if constexpr (VEC) V::load(z + sl.head + i * N, v);
-        else v[0] = V::one(z + i);
+    // what the teacher takes off at N classes from c on
+    const auto named = [&](uint32_t chain, int64_t c, auto &v) __attribute__((always_inline)) {
+        constexpr int M = sizeof(v) / sizeof(v[0]);
+        while (chain) {
+            const int64_t at = s_id[chain - 1] - c;
+            const float q = s_sum[chain - 1];
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = grad(v[j]);
-        if constexpr (VEC) V::store(out + sl.head + i * N, v);
-        else V::put(out + i, v[0]);
-    }
-    sl.singles(a, blockIdx.x, [&](int64_t c) __attribute__((always_inline)) { V::put(out + c, grad(V::one(z + c))); });
-    // the others' stores have to be there before the named classes are stored over them
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    for (int k = threadIdx.x; k < a.K; k += DS_NT) {
-        const int id = s_id[k];
-        if (id >= sl.first && id < sl.last && !s_again[k]) V::put(out + id, s_grad[k]);
-    }
+            for (int j = 0; j < M; ++j) v[j] -= at == j ? q : 0.f;
+            chain = s_next[chain - 1];
+        }
+    };
+    if constexpr (VEC) {
+#pragma unroll
+        for (int i = 0; i < DS_HELD; ++i) {
+            const int at = i * DS_NT + threadIdx.x;
+            if (sl.v0 + at >= sl.v1) break;
+            float v[N];
+            V::values(held[i], v);
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = grad(v[j]);
+            named(s_chain[at], from + (int64_t)at * N, v);
+            ds_stream(out + from + (int64_t)at * N, V::packed(v));
+        }
+    } else
+        for (int at = threadIdx.x; sl.v0 + at < sl.v1; at += DS_NT) {
+            float v[1] = {grad(V::one(z + sl.v0 + at))};
+            named(s_chain[at / PART], sl.v0 + at, v);
+            V::put(out + sl.v0 + at, v[0]);
+        }
+    sl.singles(a, blockIdx.x, [&](int64_t c) __attribute__((always_inline)) {
+        float v[1] = {grad(V::one(z + c))};
+        named(s_chain[DS_PARTS], c, v);
+        V::put(out + c, v[0]);
+    });
+    if (blockIdx.x == 0 && threadIdx.x == 0)
+        a.loss[row] = some ? (float)((double)a.T * (double)a.T * (a.a[row] + (s == 0.f ? 0.0 : (double)base / (double)a.T + log((double)s)))) : 0.f;
 }
 
 __global__ void __launch_bounds__(DS_NT) ds_mean_kernel(const float *__restrict__ loss, int B, float *__restrict__ mean) {
@@ -256,7 +317,8 @@ __global__ void __launch_bounds__(DS_NT) ds_mean_kernel(const float *__restrict_
     if (threadIdx.x == 0) *mean = (float)((sh[0] + sh[1] + sh[2] + sh[3]) / B);
 }
 
-#define DS_SLICE_BYTES (32 << 10)
+#define DS_SLICE_BYTES (DS_NT * DS_HELD * 16)
+#define DS_CACHED (96 << 20) /* bytes of logits between the passes over them: the last cache before the memory holds 256 MB */
 static int ds_slices(int64_t C) { return (int)ks_ceil_div(C, DS_SLICE_BYTES / 4); } // for the smaller slices of fp32
 
 extern "C" size_t class_distill_workspace(int64_t C, int B, int K) {
@@ -264,6 +326,7 @@ extern "C" size_t class_distill_workspace(int64_t C, int B, int K) {
     KsArena ws(nullptr);
     ws.take<float2>((size_t)B * ds_slices(C));
     ws.take<double>((size_t)B);
+    ws.take<float2>((size_t)B);
     return ws.off;
 }
 
@@ -283,6 +346,7 @@ extern "C" int class_distill_fwd_bwd(const void *logits, int64_t ldl, int dtype,
     KsArena arena(ws);
     a.part = arena.take<float2>((size_t)B * ds_slices(C));
     a.a = arena.take<double>((size_t)B);
+    a.t = arena.take<float2>((size_t)B);
     a.logits = logits; a.t_logits = t_logits; a.out = dlogits;
     a.ldl = ldl; a.ldd = ldd; a.C = C; a.t_ids = t_ids; a.B = B; a.K = K; a.t_bf16 = t_dtype == KS_DTYPE_BF16;
     a.T = temperature; a.l = (float)(1.4426950408889634 / (double)temperature); a.g = (float)((double)grad_scale * (double)temperature / B);
@@ -293,8 +357,12 @@ extern "C" int class_distill_fwd_bwd(const void *logits, int64_t ldl, int dtype,
     const int64_t slice = DS_SLICE_BYTES / size; // elements
     hipStream_t st = (hipStream_t)stream;
     a.parts = (int)ks_ceil_div(ks_ceil_div(C, n), slice / n);
-    for (int64_t r = 0; r < B; r += 1 << 15) { // a launch's second dimension ends at 65,535
-        const unsigned rows = (unsigned)(B - r < 1 << 15 ? B - r : 1 << 15);
+    // rows of one pass, then of the other; a launch's second dimension ends at 65,535
+    int64_t group = DS_CACHED / (C * size);
+    group = group < 1 ? 1 : group > 1 << 15 ? 1 << 15 : group;
+    group = ks_ceil_div(B, ks_ceil_div(B, group));
+    for (int64_t r = 0; r < B; r += group) {
+        const unsigned rows = (unsigned)(B - r < group ? B - r : group);
         a.row0 = (int)r;
         const auto go = [&](auto stats, auto grad) {
             a.slice = slice / n;
@@ -304,7 +372,7 @@ extern "C" int class_distill_fwd_bwd(const void *logits, int64_t ldl, int dtype,
                 a.slice = slice;
                 a.slices = (int)ks_ceil_div(C, slice);
             }
-            hipLaunchKernelGGL(grad, dim3((unsigned)a.slices, rows), dim3(DS_NT), (size_t)K * 13, st, a);
+            hipLaunchKernelGGL(grad, dim3((unsigned)a.slices, rows), dim3(DS_NT), (size_t)K * 14 + 16, st, a);
         };
         if (dtype == KS_DTYPE_FP32) go(ds_stats_kernel<float>, vec ? ds_grad_kernel<float, true> : ds_grad_kernel<float, false>);
         else go(ds_stats_kernel<uint16_t>, vec ? ds_grad_kernel<uint16_t, true> : ds_grad_kernel<uint16_t, false>);
