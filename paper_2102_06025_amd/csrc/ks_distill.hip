@@ -89,7 +89,7 @@ __device__ __forceinline__ void ds_hold(const void *row, int64_t v0, int64_t v1,
     }
 }
 
-// past the caches: nobody here reads a gradient, and the logits of the rows that come next stay in them
+// past the caches: nobody here reads a gradient
 __device__ __forceinline__ void ds_stream(void *p, uint4 v) {
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
     __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, (u32x4 *)p);
@@ -175,6 +175,7 @@ ds_stats_kernel(DsArgs a) {
         for (int i = 0; i < DS_HELD; ++i) {
             if (sl.v0 + i * DS_NT + threadIdx.x >= sl.v1) break;
             float v[N];
+            asm volatile("" : "+v"(held[i].x), "+v"(held[i].y), "+v"(held[i].z), "+v"(held[i].w)); // unpacked anew: half the registers
             V::values(held[i], v);
 #pragma unroll
             for (int j = 0; j < N; ++j) s += __builtin_amdgcn_exp2f(a.l * (v[j] - base));
@@ -318,7 +319,6 @@ __global__ void __launch_bounds__(DS_NT) ds_mean_kernel(const float *__restrict_
 }
 
 #define DS_SLICE_BYTES (DS_NT * DS_HELD * 16)
-#define DS_CACHED (96 << 20) /* bytes of logits between the passes over them: the last cache before the memory holds 256 MB */
 static int ds_slices(int64_t C) { return (int)ks_ceil_div(C, DS_SLICE_BYTES / 4); } // for the smaller slices of fp32
 
 extern "C" size_t class_distill_workspace(int64_t C, int B, int K) {
@@ -357,12 +357,8 @@ extern "C" int class_distill_fwd_bwd(const void *logits, int64_t ldl, int dtype,
     const int64_t slice = DS_SLICE_BYTES / size; // elements
     hipStream_t st = (hipStream_t)stream;
     a.parts = (int)ks_ceil_div(ks_ceil_div(C, n), slice / n);
-    // rows of one pass, then of the other; a launch's second dimension ends at 65,535
-    int64_t group = DS_CACHED / (C * size);
-    group = group < 1 ? 1 : group > 1 << 15 ? 1 << 15 : group;
-    group = ks_ceil_div(B, ks_ceil_div(B, group));
-    for (int64_t r = 0; r < B; r += group) {
-        const unsigned rows = (unsigned)(B - r < group ? B - r : group);
+    for (int64_t r = 0; r < B; r += 1 << 15) { // a launch's second dimension ends at 65,535
+        const unsigned rows = (unsigned)(B - r < 1 << 15 ? B - r : 1 << 15);
         a.row0 = (int)r;
         const auto go = [&](auto stats, auto grad) {
             a.slice = slice / n;
