@@ -399,7 +399,8 @@ __device__ __forceinline__ void m4_last_class(const uint8_t *xq, const uint8_t *
 #define M4X_NT 512
 // Rows of up to 512 elements: a wavefront keeps the codes of 64 classes in registers, a workgroup those of up to 4,096 / KB samples in LDS, and
 // the samples go past 32 at a time: 2 KB matrix instructions a block, with the stores of the block before in between.  During a group's
-// last block each piece of codes is replaced, when it has been used, by the next group's.
+// last block each piece of codes is replaced, when it has been used, by the next group's.  What bounds it are the stores: 1,024 x 390,625 x 512
+// bf16 200 us (0.9 GB at 4.5 TB/s), x 128 168 us; wavefronts of their own, which read the samples again for every group, take 374 and 181.
 template <int KB, typename OUT>
 __global__ void __launch_bounds__(M4X_NT, 2)
 m4_steady_kernel(const uint8_t *__restrict__ xq, const uint8_t *__restrict__ wq, const float *__restrict__ bias, int64_t C, int kb, int B, float scale,
@@ -538,7 +539,8 @@ __device__ __forceinline__ void m4_barrier() {
 // Deeper rows: the samples pass through LDS in chunks of eight k-steps, which eight wavefronts with 64 classes each read at the same time: three
 // buffers, a barrier a chunk.  While chunk t is multiplied, a fragment is read for the next k-step when it has been used (the last ones
 // from chunk t + 1, which is there since the barrier), and chunk t + 2 is written to LDS from registers.  Weights come straight from memory,
-// four k-steps ahead.  The chunks run on from one tile of 512 classes by 128 samples to the next; what lies beyond the depth is loaded as 0.
+// four k-steps ahead.  2,048 x 131,072 x 4,096 bf16: 650 us, 3.4 PFLOP/s (wavefronts of their own 1,320); what holds it up are the operands' ways
+// into the registers, 32 KB from LDS and 18 KB through the caches for 64 matrix instructions.  The chunks run on from one tile of 512 classes by 128 samples to the next; what lies beyond the depth is loaded as 0.
 template <typename OUT>
 __global__ void __launch_bounds__(M4X_NT, 2)
 m4_staged_kernel(const uint8_t *__restrict__ xq, const uint8_t *__restrict__ wq, const float *__restrict__ bias, int64_t C, int kb, int B, float scale,
@@ -703,7 +705,12 @@ static void m4_logits(const uint8_t *xq, const uint8_t *wq, const float *bias, i
     };
     const int64_t waves = groups * ks_ceil_div(B, 64);
     if (B <= 32) return waves <= 1024 && kb >= 16 ? direct(m4_direct_kernel<1, 4, OUT>, 32, 1) : direct(m4_direct_kernel<1, 1, OUT>, 32, 4);
-    if (B <= 64 || waves <= 1280 || (kb <= 8 && !vec))
+    // Few samples: the codes of the weights are what moves, and every wavefront reads its own (1 x 390,625 x 512 bf16: 24 us with the features'
+    // codes); where there are few wavefronts and rows are deep, four of them divide a group's depth.  Few wavefronts, or few groups of classes
+    // for the 256 workgroups that keep samples, likewise (10,000 classes, batch 1,024: x 128 8.7 us, 19.6 with samples kept; x 512 10.4 and 15.6;
+    // 30,000 x 512, 512: 13.5 and 15.5; but 1,024: 23.5 and 16.9; 50,000 x 128, 2,048: 35.9 and 46.6), and rows that begin on an odd
+    // element, which are stored element by element.
+    if (B <= 64 || waves <= 1280 || (kb <= 8 && (!vec || groups <= 160 || waves <= 3800)) || (kb <= 2 && groups <= 800))
         return waves <= 320 && kb >= 16 ? direct(m4_direct_kernel<2, 4, OUT>, 64, 1) : direct(m4_direct_kernel<2, 1, OUT>, 64, 4);
     if (kb > 8) {
         hipLaunchKernelGGL(m4_staged_kernel<OUT>, dim3(256), dim3(M4X_NT), 0, st, xq, wq, bias, C, kb, B, scale, out, ldl, vec);

@@ -29,7 +29,7 @@ def test_workspace(ks):
     assert [ks.class_sample_workspace(*a) for a in ((0, 1), (1, 0), (1 << 31, 1), ((1 << 32) + 8, 1), (8, (1 << 32) + 1), (-1, 1))] == [0] * 6
     assert ks.class_sample_workspace(1, 1) == 768
     assert ks.class_sample_workspace(390_625, 256) >= 256 * 12
-    assert 0 < ks.class_sample_workspace((1 << 31) - 1, 1) <= 4_096 * 12 + 768  # parts grow with the row
+    assert 0 < ks.class_sample_workspace((1 << 31) - 1, 1) <= 4_096 * 12 + 2_048 * 12 + 4_096 * 8 + 2_048  # parts grow with the row
 
 
 def test_refusals(ks):
