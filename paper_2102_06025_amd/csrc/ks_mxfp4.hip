@@ -440,8 +440,8 @@ m4_steady_kernel(const uint8_t *__restrict__ xq, const uint8_t *__restrict__ wq,
         const auto group_exps = [&](int g, int q) __attribute__((always_inline)) {
             return __builtin_amdgcn_make_buffer_rsrc((void *)(wq + ((int64_t)(g_lo + g) * 2 + q) * bytes + kb * M4_PIECE), 0, (kb + 3) / 4 * M4_EXPS, 0x00020000);
         };
-        const auto codes = [&](__amdgpu_buffer_rsrc_t p, int k) __attribute__((always_inline)) {
-            return __builtin_bit_cast(m4_i32x4, __builtin_amdgcn_raw_buffer_load_b128(p, lane * 16, k * M4_PIECE, 0));
+        const auto codes = [&](__amdgpu_buffer_rsrc_t p, int k) __attribute__((always_inline)) { // the whole offset in the register that is checked against the end
+            return __builtin_bit_cast(m4_i32x4, __builtin_amdgcn_raw_buffer_load_b128(p, lane * 16 + k * M4_PIECE, 0, 0));
         };
         m4_i32x4 w[KB][2], x[4];
         int ew[KQ][2], ex[2][KQ];
@@ -452,7 +452,7 @@ m4_steady_kernel(const uint8_t *__restrict__ xq, const uint8_t *__restrict__ wq,
 #pragma unroll
             for (int k = 0; k < KB; ++k) w[k][q] = codes(p, k);
 #pragma unroll
-            for (int k = 0; k < KQ; ++k) ew[k][q] = __builtin_amdgcn_raw_buffer_load_b32(e, lane * 4, k * M4_EXPS, 0);
+            for (int k = 0; k < KQ; ++k) ew[k][q] = __builtin_amdgcn_raw_buffer_load_b32(e, lane * 4 + k * M4_EXPS, 0, 0);
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) x[k] = *(const m4_i32x4 *)(s_x + k * M4_PIECE + lane * 16);
@@ -496,7 +496,7 @@ m4_steady_kernel(const uint8_t *__restrict__ xq, const uint8_t *__restrict__ wq,
 #pragma unroll
                         for (int q = 0; q < 2; ++q) {
                             w[k][q] = codes(p_next[q], k);
-                            if (j.value == 3) ew[k4][q] = __builtin_amdgcn_raw_buffer_load_b32(e_next[q], lane * 4, k4 * M4_EXPS, 0);
+                            if (j.value == 3) ew[k4][q] = __builtin_amdgcn_raw_buffer_load_b32(e_next[q], lane * 4 + k4 * M4_EXPS, 0, 0);
                         }
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
@@ -569,12 +569,12 @@ m4_staged_kernel(const uint8_t *__restrict__ xq, const uint8_t *__restrict__ wq,
         for (int i = 0; i < 2; ++i) {
             const int s = r_sb * 4 + h.value * 2 + i, blk = s < xblocks ? s : xblocks - 1;
             const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void *)(xq + (int64_t)blk * bytes), 0, kb * M4_PIECE, 0x00020000);
-            held[i] = __builtin_bit_cast(m4_i32x4, __builtin_amdgcn_raw_buffer_load_b128(from, lane * 16, (r_c * R + wave) * M4_PIECE, 0));
+            held[i] = __builtin_bit_cast(m4_i32x4, __builtin_amdgcn_raw_buffer_load_b128(from, lane * 16 + (r_c * R + wave) * M4_PIECE, 0, 0));
         }
         if (h.value == 0) {
             const int s = r_sb * 4 + (wave & 3), blk = s < xblocks ? s : xblocks - 1;
             const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void *)(xq + (int64_t)blk * bytes + kb * M4_PIECE), 0, (kb + 3) / 4 * M4_EXPS, 0x00020000);
-            held_e = __builtin_amdgcn_raw_buffer_load_b32(from, lane * 4, (r_c * 2 + (wave >> 2)) * M4_EXPS, 0);
+            held_e = __builtin_amdgcn_raw_buffer_load_b32(from, lane * 4 + (r_c * 2 + (wave >> 2)) * M4_EXPS, 0, 0);
         } else { // behind the last tile: the same again, read by nobody
             const bool end = ++r_c == chunks, more = end && r_left > per_xcd;
             r_c = end ? 0 : r_c;
@@ -614,7 +614,7 @@ m4_staged_kernel(const uint8_t *__restrict__ xq, const uint8_t *__restrict__ wq,
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-        for (int q = 0; q < 2; ++q) w[kk][q] = __builtin_bit_cast(m4_i32x4, __builtin_amdgcn_raw_buffer_load_b128(wr[q], lane * 16, kk * M4_PIECE, 0));
+        for (int q = 0; q < 2; ++q) w[kk][q] = __builtin_bit_cast(m4_i32x4, __builtin_amdgcn_raw_buffer_load_b128(wr[q], lane * 16 + kk * M4_PIECE, 0, 0));
     m4_barrier();
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
@@ -643,7 +643,7 @@ m4_staged_kernel(const uint8_t *__restrict__ xq, const uint8_t *__restrict__ wq,
                 constexpr int kk = K.value, half = kk / 4, j = kk % 4;
                 if (j == 0) {
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) ew[1 - half][q] = __builtin_amdgcn_raw_buffer_load_b32(half == 0 ? er[q] : en[q], lane * 4, (half == 0 ? at_mid : at_next) / (4 * M4_PIECE) * M4_EXPS, 0);
+                    for (int q = 0; q < 2; ++q) ew[1 - half][q] = __builtin_amdgcn_raw_buffer_load_b32(half == 0 ? er[q] : en[q], lane * 4 + (half == 0 ? at_mid : at_next) / (4 * M4_PIECE) * M4_EXPS, 0, 0);
                 }
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
@@ -656,7 +656,7 @@ m4_staged_kernel(const uint8_t *__restrict__ xq, const uint8_t *__restrict__ wq,
                     if (s == 3)
 #pragma unroll
                         for (int q = 0; q < 2; ++q)
-                            w[j][q] = __builtin_bit_cast(m4_i32x4, __builtin_amdgcn_raw_buffer_load_b128(half == 0 ? wr[q] : wn[q], lane * 16, (half == 0 ? at_mid : at_next) + j * M4_PIECE, 0));
+                            w[j][q] = __builtin_bit_cast(m4_i32x4, __builtin_amdgcn_raw_buffer_load_b128(half == 0 ? wr[q] : wn[q], lane * 16 + (half == 0 ? at_mid : at_next) + j * M4_PIECE, 0, 0));
                 }
                 if (kk == 2) {
                     place(H0, b2, e2);
