@@ -38,7 +38,7 @@ extern "C" {
  * A sample without entries (or whose entries are all -infinity) has loss and gradient 0: padding.  A class with logit -infinity has p = 0; where
  * its q > 0 the loss is +infinity and the gradient as above.  A row of logits that are all -infinity has p = 0.  A NaN or +infinity among
  * the logits makes the row's loss and gradient NaN, one among the teacher's logits the loss and the gradient at the named classes.
- * Requires B >= 1, 1 <= C < 2^31, 1 <= K <= KS_MAX_DISTILL_K (KS_UNSUPPORTED beyond), temperature > 0 and finite.
+ * Requires B >= 1, 1 <= C < 2^31, 1 <= K <= KS_MAX_DISTILL_K (KS_UNSUPPORTED beyond), 1e-30 <= temperature <= 1e30.
  * Workspace: class_distill_workspace, 0 for sizes that are refused.
  * ---------------------------------------------------------------------------------------------------- */
 size_t class_distill_workspace(int64_t C, int B, int K);

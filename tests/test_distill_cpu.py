@@ -38,7 +38,7 @@ def test_refusals(ks):
         return ks.lib().class_distill_fwd_bwd(z, ldl, dtype, C, B, ids, t, tt, K, T, 1.0, lo, lm, dz, ldd, ws, size, st, None)
     for bad in (dict(z=None), dict(ids=None), dict(t=None), dict(lo=None), dict(lm=None), dict(dz=None), dict(ws=None), dict(ldl=99), dict(ldd=99), dict(dtype=2),
                 dict(tt=2), dict(C=0), dict(C=1 << 31, ldl=1 << 31, ldd=1 << 31), dict(B=0), dict(B=-1), dict(K=0), dict(T=0.0), dict(T=-1.0),
-                dict(T=float("nan")), dict(T=float("inf")), dict(z=258), dict(dz=258), dict(z=257, dtype=0), dict(t=258), dict(t=257, tt=0), dict(ids=258),
+                dict(T=float("nan")), dict(T=float("inf")), dict(T=1e-31), dict(T=1e-45), dict(T=1e31), dict(z=258), dict(dz=258), dict(z=257, dtype=0), dict(t=258), dict(t=257, tt=0), dict(ids=258),
                 dict(lo=257), dict(lm=257), dict(ws=260), dict(st=258), dict(z=512, ldl=101)):
         assert call(**bad) == ks.KS_INVALID_ARG, bad
     assert call(K=4_097) == ks.KS_UNSUPPORTED
