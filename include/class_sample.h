@@ -35,7 +35,7 @@ extern "C" {
  *   temperature, top_p, min_p [B] fp32, top_k [B] int32      each may be NULL: 1, 1, 0, 0 for all rows
  *   ids [B]         out: the drawn class, -1 where a row has no class to draw (all of it -infinity or NaN)
  *   logprob [B]     out, fp32, may be NULL: the logarithm of its weight's share of what is kept; -infinity where ids is -1
- * Requires B >= 1, 1 <= C < 2^31.  Workspace: class_sample_workspace, 12 bytes for each of up to 4,096 parts of a row, and 25 to 57 KB a row of 49,152 classes or more; 0 for sizes that
+ * Requires B >= 1, 1 <= C < 2^31.  Workspace: class_sample_workspace, 12 bytes for each of up to 4,096 parts of a row, and 25 to 57 KB a row of 32,768 classes or more; 0 for sizes that
  * are refused.
  * ---------------------------------------------------------------------------------------------------- */
 size_t class_sample_workspace(int64_t C, int B);

@@ -1308,8 +1308,8 @@ static bool sp_sizes(int64_t C, int B, SpArgs &a) {
     return true;
 }
 // From this many classes on, rows that keep much are shared by all compute units (16 x 100,000 fp32, p = 0.98: 87 us, 234 with a workgroup a row;
-// 256 x 390,625 bf16, a rule for each: 246 and 817); two launches more, of 3 us each where no row needs them
-#define SP_SHARED_C 49152
+// 300 x 40,000: 150 and 238, x 20,000: 145 and 153); two launches more, together 3.5 us where no row needs them
+#define SP_SHARED_C 32768
 static void sp_places(KsArena &ws, int B, SpArgs &a) {
     a.g_max = ws.take<float>((size_t)B * a.ngr);
     a.g_sum = ws.take<double>((size_t)B * a.ngr);

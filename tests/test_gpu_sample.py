@@ -98,7 +98,7 @@ RULES = [dict(), dict(T=0.7), dict(k=1), dict(k=40), dict(p=0.9), dict(m=0.05), 
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("C", [1, 2, 7, 511, 512, 513, 2_000, 10_000, 100_003])
+@pytest.mark.parametrize("C", [1, 2, 7, 511, 512, 513, 2_000, 10_000, 32_768, 100_003])
 @pytest.mark.parametrize("masked", [0.0, 0.6])
 def test_rules(ks, C, dtype, masked):
     gen = torch.Generator("cuda").manual_seed(C)
