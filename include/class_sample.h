@@ -26,8 +26,9 @@ extern "C" {
  *        into [0, 1), of a u beyond the last kept class is drawn
  * T <= 0 or NaN: the first class of the order, whatever u is (k = 1).
  *
- * Weights are whole numbers of 2^-s, s = min(48, 62 - ceil(log2 C)): exp() in fp64 rounded to the nearest, their sums exact, so that the
- * result depends on neither the order of summation nor the batch; a class whose weight is less than half of 2^-s is not drawn.
+ * Weights are whole numbers of 2^-s, s = min(48, 62 - ceil(log2 C)): exp() in fp64 rounded to the nearest, their sums exact; a class whose
+ * weight is less than half of 2^-s is not drawn.  The weight of all classes, which rows without top-k need, is summed in fp64 over parts
+ * of the row whose sizes C alone decides, in a fixed order, before it is rounded.  The result depends on the row and its settings alone.
  *
  *   logits [B, C]   in, dtype KS_DTYPE_FP32 or KS_DTYPE_BF16; row i begins at element i * ldl (ldl >= C; aligned to its elements is
  *                   enough, rows that begin on 16 bytes are read faster)
@@ -35,8 +36,8 @@ extern "C" {
  *   temperature, top_p, min_p [B] fp32, top_k [B] int32      each may be NULL: 1, 1, 0, 0 for all rows
  *   ids [B]         out: the drawn class, -1 where a row has no class to draw (all of it -infinity or NaN)
  *   logprob [B]     out, fp32, may be NULL: the logarithm of its weight's share of what is kept; -infinity where ids is -1
- * Requires B >= 1, 1 <= C < 2^31.  Workspace: class_sample_workspace, 12 bytes for each of up to 4,096 parts of a row, and 25 to 57 KB a row of 32,768 classes or more; 0 for sizes that
- * are refused.
+ * Requires B >= 1, 1 <= C < 2^31.  Workspace: class_sample_workspace, 12 bytes for each of up to 4,096 parts of a row, and 25 to 57 KB a row of
+ * 32,768 classes or more; 0 for sizes that are refused.
  * ---------------------------------------------------------------------------------------------------- */
 size_t class_sample_workspace(int64_t C, int B);
 int class_sample(const void *logits, int64_t ldl, int dtype, int64_t C, int B, const float *u, const float *temperature,
