@@ -28,7 +28,9 @@ extern "C" {
  *
  * Weights are whole numbers of 2^-s, s = min(48, 62 - ceil(log2 C)): exp() in fp64 rounded to the nearest, their sums exact; a class whose
  * weight is less than half of 2^-s is not drawn.  The weight of all classes, which rows without top-k need, is summed in fp64 over parts
- * of the row whose sizes C alone decides, in a fixed order, before it is rounded.  The result depends on the row and its settings alone.
+ * of the row whose sizes C alone decides, in a fixed order, before it is rounded (a part of which no class has a weight counts nothing), and
+ * without top-k, top-p and min-p the running weight at the beginning of the part that is drawn from is made of these sums.  The result
+ * depends on the row and its settings alone.
  *
  *   logits [B, C]   in, dtype KS_DTYPE_FP32 or KS_DTYPE_BF16; row i begins at element i * ldl (ldl >= C; aligned to its elements is
  *                   enough, rows that begin on 16 bytes are read faster)

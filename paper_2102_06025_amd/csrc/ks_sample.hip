@@ -293,17 +293,20 @@ __device__ __forceinline__ void sp_find(SpScan &sh, const uint32_t *n, const uin
     __syncthreads();
 }
 
-// weight of granule g of a row, whose largest logit is `z`
+// Weight of granule g of a row, whose largest logit is `z`: the rounded sum, and none where no class of it has a weight (many that are less than
+// half of 2^-bits each would add up to one that belongs to nobody)
 __device__ __forceinline__ uint64_t sp_mass(const SpArgs &a, int row, int g, float z, float top, double c) {
-    return z > -INFINITY ? (uint64_t)(a.g_sum[(int64_t)row * a.ngr + g] * sp_exp2(sp_log2w(z, top, c) + a.bits) + 0.5) : 0;
+    if (!(z > -INFINITY)) return 0;
+    const uint64_t most = sp_weight(z, top, c, a.bits);
+    return most ? sp_max((uint64_t)(a.g_sum[(int64_t)row * a.ngr + g] * sp_exp2(sp_log2w(z, top, c) + a.bits) + 0.5), most) : 0;
 }
 __device__ __forceinline__ float sp_c32(const SpRule &rule) { return (float)(rule.c * SP_PER_BINADE); }
 __device__ __forceinline__ int sp_limit(const SpArgs &a) { return (a.bits + 1) * SP_PER_BINADE; } // from this bin on weights are 0
 __device__ __forceinline__ int sp_bin_m(const SpArgs &a, const SpRule &rule) { // last bin with weights of m or more
     return rule.use_m ? (int)fminf(-log2f(rule.m) * SP_PER_BINADE + 2.f, (float)(sp_limit(a) - 1)) : sp_limit(a) - 1;
 }
-__device__ __forceinline__ uint64_t sp_floor(const SpArgs &a, const SpRule &rule) {
-    return rule.use_m ? sp_max((uint64_t)ceil((double)rule.m * (double)((uint64_t)1 << a.bits)), (uint64_t)1) : 0;
+__device__ __forceinline__ uint64_t sp_floor(const SpArgs &a, const SpRule &rule) { // least weight that is kept
+    return rule.use_m ? sp_max((uint64_t)ceil((double)rule.m * (double)((uint64_t)1 << a.bits)), (uint64_t)1) : 1;
 }
 __device__ __forceinline__ uint64_t sp_share(double p, uint64_t w) { return sp_max((uint64_t)ceil(p * (double)w), (uint64_t)1); } // the weight that is p of w
 __device__ __forceinline__ uint64_t sp_target(const SpArgs &a, int row, uint64_t w) { // the running weight that the drawn class exceeds: u of w
@@ -315,8 +318,8 @@ __device__ __forceinline__ void sp_result(const SpArgs &a, int row, int id, floa
     if (a.logprob) a.logprob[row] = (float)((sp_log2w(z, top, c) - (log2((double)w) - a.bits)) * 0.6931471805599453); // log of 2^(c (z - top)) / (w 2^-bits)
 }
 
-// One wavefront: of the classes [first, last) that are kept, the one at which the running weight exceeds `target`; if rounding left less
-// weight than that the last that is kept.  -> its id and logit
+// One wavefront: of the classes [first, last) that are kept (weights of floor_w >= 1 or more), the one at which the running weight exceeds `target`;
+// if there is less weight than that the last that is kept.  -> its id and logit
 template <typename T>
 __device__ __forceinline__ void sp_pick(const SpArgs &a, const T *z, bool vec, int64_t first, int64_t last, uint64_t target, float top, double c, uint64_t cut,
                                         uint64_t floor_w, int &id, float &logit) {
@@ -565,8 +568,8 @@ sp_draw_kernel(SpArgs a) {
         if (wave == 0) {
             int id;
             float logit;
-            const int64_t first = sh.scan.found * a.gran;
-            sp_pick(a, z, vec, first, sp_min(first + a.gran, a.C), sh.scan.found_w, top, c, ~(uint64_t)0, 0, id, logit);
+            // from the granule on: its classes' own weights may come to less than its rounded sum, what is left of the target goes on to the next ones
+            sp_pick(a, z, vec, sh.scan.found * a.gran, a.C, sh.scan.found_w, top, c, ~(uint64_t)0, sp_floor(a, rule), id, logit);
             if (lane == 0) sp_result(a, row, id, logit, top, c, w_all);
         }
         return;

@@ -284,3 +284,41 @@ def test_refusals_of_tensors(ks):
     with pytest.raises(ks.KsError) as e:
         ks.class_sample(z, u, ws=torch.empty(256, dtype=torch.uint8, device="cuda"))
     assert e.value.code == ks.KS_WORKSPACE_TOO_SMALL
+
+
+# ---------------------------------------------------------------------------------------------------- weights at the end of what is counted
+def weightless(s, part, C, rest=-5.0):
+    """A row whose first `part` classes weigh two fifths of 2^-s each, which is no whole 2^-s, one of the largest logit behind them."""
+    z = torch.full((C,), rest, dtype=torch.float64)
+    z[:part] = math.log(0.4) - s * math.log(2.0)
+    z[part] = 0.0
+    return z
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("C,part", [(16, 8), (1_000, 16), (30_000, 800), (100_003, 32), (100_003, 32 * 7), (400_000, 1_024), (2_500_000, 3 * 1_024)])
+def test_classes_without_a_weight_are_not_drawn(ks, C, part, dtype):
+    """Parts of a row whose classes weigh nothing each, but together more than 2^-s: u = 0 and the like draw the first class with a weight."""
+    s = min(48, 62 - math.ceil(math.log2(C)))
+    z = torch.stack([weightless(s, part, C), weightless(s, part, C), weightless(s, part, C), weightless(s, part - 3, C)]).to(dtype).cuda()
+    z[1, 2] = -INF
+    z[2, part + 1:] = -200.0  # nothing with a weight behind the largest
+    ids, _ = check(ks, z, 0.0)
+    assert ids.tolist() == [part, part, part, part - 3]
+    check(ks, z, LAST)
+    check(ks, z, [1e-30, 2.0 ** -60, 0.5, 0.25])
+    check(ks, z[2:3], LAST)  # the running weight ends at the largest
+
+
+def test_a_part_that_weighs_less_than_the_sum_of_its_classes(ks):
+    """One class of a part has the weight 1, seven none: a target between 1 and the part's rounded sum is met behind it."""
+    C, s = 64, 48
+    z = torch.full((3, C), -INF, dtype=torch.float64)
+    z[:, :8] = math.log(0.4) - s * math.log(2.0)
+    z[:, 3] = math.log(0.6) - s * math.log(2.0)
+    z[:2, 40] = 0.0
+    z[2, 20] = 0.0
+    z[1, 30] = -0.5
+    ids, _ = check(ks, z.float().cuda(), [2.0 ** -48, 2.0 ** -47, 2.0 ** -48])
+    assert ids.tolist() == [40, 30, 20]
+    assert check(ks, z.float().cuda(), 0.0)[0].tolist() == [3, 3, 3]
