@@ -301,7 +301,8 @@ __device__ __forceinline__ uint64_t sp_mass(const SpArgs &a, int row, int g, flo
     return most ? sp_max((uint64_t)(a.g_sum[(int64_t)row * a.ngr + g] * sp_exp2(sp_log2w(z, top, c) + a.bits) + 0.5), most) : 0;
 }
 __device__ __forceinline__ float sp_c32(const SpRule &rule) { return (float)(rule.c * SP_PER_BINADE); }
-__device__ __forceinline__ int sp_limit(const SpArgs &a) { return (a.bits + 1) * SP_PER_BINADE; } // from this bin on weights are 0
+// from this bin on weights are 0: half of 2^-bits lies at the end of bin (bits + 1) * SP_PER_BINADE - 1, and bins are found with roundings
+__device__ __forceinline__ int sp_limit(const SpArgs &a) { return (a.bits + 1) * SP_PER_BINADE + 1; }
 __device__ __forceinline__ int sp_bin_m(const SpArgs &a, const SpRule &rule) { // last bin with weights of m or more
     return rule.use_m ? (int)fminf(-log2f(rule.m) * SP_PER_BINADE + 2.f, (float)(sp_limit(a) - 1)) : sp_limit(a) - 1;
 }

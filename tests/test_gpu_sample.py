@@ -322,3 +322,15 @@ def test_a_part_that_weighs_less_than_the_sum_of_its_classes(ks):
     ids, _ = check(ks, z.float().cuda(), [2.0 ** -48, 2.0 ** -47, 2.0 ** -48])
     assert ids.tolist() == [40, 30, 20]
     assert check(ks, z.float().cuda(), 0.0)[0].tolist() == [3, 3, 3]
+
+
+def test_the_least_weight_counts_with_and_without_rules(ks):
+    """A logit whose weight is just above half of 2^-s, which is the weight 1: u = 0 draws it where it comes first."""
+    for T, v in ((0.8333905935287476, -28.30545425415039), (3.8100030422210693, -129.40374755859375), (1.4537763595581055, -49.376365661621094),
+                 (3.362499713897705, -114.20465087890625), (1.8140368461608887, -61.612327575683594), (1.421820878982544, -48.29102325439453)):
+        for C in (8, 5_000):
+            z = torch.full((1, C), -200.0, device="cuda")
+            z[0, 1], z[0, 5], z[0, C - 1] = v, 0.0, -1.0
+            for rule in (dict(), dict(k=3), dict(m=1e-30), dict(k=3, m=1e-30)):
+                ids, _ = check(ks, z, 0.0, T=T, **rule)
+                assert ids.item() == 1, (T, C, rule)
