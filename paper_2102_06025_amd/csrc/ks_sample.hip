@@ -106,11 +106,14 @@ __device__ __forceinline__ uint64_t sp_weight(float z, float top, double c, int 
     const double w = sp_exp2(sp_log2w(z, top, c) + bits) + 4503599627370496.0;
     return (uint64_t)__double_as_longlong(w) & 0xFFFFFFFFFFFFFull;
 }
-// number of a weight's bin, which grows as z falls: the fp32 operations keep the order of the z
+// Number of a weight's bin, which grows as z falls: the fp32 operations keep the order of the z.  A difference beyond fp32 (which weighs
+// something at a temperature of 1e37 or more) and a c32 beyond it end at its largest number: a bin that is too low has its class looked at,
+// and the class's weight decides.
+#define SP_MOST 3.402823466e38f
 __device__ __forceinline__ int sp_bin(float z, float top, float c32) {
     if (z == top) return 0;
     if (!(z > -INFINITY)) return SP_NO_BIN;
-    return (int)fminf((top - z) * c32, (float)SP_NO_BIN);
+    return (int)fminf(fminf(top - z, SP_MOST) * c32, (float)SP_NO_BIN);
 }
 // place in the order as one number, lower first: z falling, then id rising
 __device__ __forceinline__ uint64_t sp_place(float z, uint32_t id) {
@@ -300,7 +303,7 @@ __device__ __forceinline__ uint64_t sp_mass(const SpArgs &a, int row, int g, flo
     const uint64_t most = sp_weight(z, top, c, a.bits);
     return most ? sp_max((uint64_t)(a.g_sum[(int64_t)row * a.ngr + g] * sp_exp2(sp_log2w(z, top, c) + a.bits) + 0.5), most) : 0;
 }
-__device__ __forceinline__ float sp_c32(const SpRule &rule) { return (float)(rule.c * SP_PER_BINADE); }
+__device__ __forceinline__ float sp_c32(const SpRule &rule) { return fminf((float)(rule.c * SP_PER_BINADE), SP_MOST); }
 // from this bin on weights are 0: half of 2^-bits lies at the end of bin (bits + 1) * SP_PER_BINADE - 1, and bins are found with roundings
 __device__ __forceinline__ int sp_limit(const SpArgs &a) { return (a.bits + 1) * SP_PER_BINADE + 1; }
 __device__ __forceinline__ int sp_bin_m(const SpArgs &a, const SpRule &rule) { // last bin with weights of m or more

@@ -334,3 +334,17 @@ def test_the_least_weight_counts_with_and_without_rules(ks):
             for rule in (dict(), dict(k=3), dict(m=1e-30), dict(k=3, m=1e-30)):
                 ids, _ = check(ks, z, 0.0, T=T, **rule)
                 assert ids.item() == 1, (T, C, rule)
+
+
+@pytest.mark.parametrize("C", [2, 40, 5_000, 40_000])
+def test_logits_far_apart_at_large_and_at_small_temperatures(ks, C):
+    """Differences beyond the largest 32-bit number weigh something at a large temperature, differences below the least normal one at a small one."""
+    rules = (dict(), dict(p=0.99), dict(m=0.1), dict(m=0.2), dict(k=C - 1), dict(k=max(C // 2, 1), p=0.9), dict(p=0.6, m=0.01), dict(p=0.05))
+    for T, scale in ((2e38, 2e38), (3e38, 1e38), (1e37, 3e38), (3e38, 3.4e38), (1e-38, 1e-38), (2e-45, 3e-45), (1e-42, 4e-42), (1.3e-37, 3e-37)):
+        z = torch.linspace(1.0, -1.0, C, dtype=torch.float64).mul_(scale).float().repeat(6, 1)
+        z[1] = z[1].flip(0)
+        z[2, :: 3] = -INF
+        z[2, 1] = scale
+        for rule in rules:
+            print(T, scale, rule, flush=True)
+            check(ks, z.cuda(), [0.0, 0.3, 0.7, LAST, 0.9, 0.95], T=T, **rule)
