@@ -4,7 +4,7 @@
 // With l = log2(e) / T and m the row's largest logit, p_c = 2^(l (z_c - m)) / S, S the sum of those powers over the row, and
 //     loss = T^2 (A + m / T + ln S),  A = sum_k q_k (ln q_k - z_k / T),
 // since the q_k add up to 1: A needs neither m nor S, so that the first pass computes it beside them and the second overwrites the logits
-// where that is asked for.
+// where that is asked for.  A and m / T are as large as the logits, whatever is left of them: what the q_k add up to has to be 1 in fp64.
 #include "../../include/class_distill.h"
 #include "ks_common.h"
 
@@ -102,14 +102,23 @@ __device__ __forceinline__ void ds_join(float &m, float &s, float m2, float s2, 
     m = top;
 }
 
-struct DsTeacher { // of a row: q_k = exp((t - top) / T) / sum; none: sum == 0
-    float top, sum;
+struct DsTeacher { // of a row: q_k = exp((t - top) / T) / sum, fp32 powers and their sum in fp64; none: sum == 0
+    float top;
+    double sum;
 };
 __device__ __forceinline__ float ds_t_logit(const DsArgs &a, int64_t at) {
     return a.t_bf16 ? ks_bf2f(((const uint16_t *)a.t_logits)[at]) : ((const float *)a.t_logits)[at];
 }
 __device__ __forceinline__ float ds_block_sum(float v, float *sh) { // fixed order
     v = ks_wave_sum(v);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return sh[0] + sh[1] + sh[2] + sh[3];
+}
+__device__ __forceinline__ double ds_block_sum(double v, double *sh) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -123,7 +132,7 @@ __device__ __forceinline__ float ds_block_max(float v, float *sh) {
     return fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
 }
 // the row's entries into LDS (ids, -1: empty, and weights), and their sum
-__device__ __forceinline__ DsTeacher ds_teacher(const DsArgs &a, int row, int32_t *s_id, float *s_q, float *sh) {
+__device__ __forceinline__ DsTeacher ds_teacher(const DsArgs &a, int row, int32_t *s_id, float *s_q, float *sh, double *shd) {
     float top = -INFINITY;
     for (int k = threadIdx.x; k < a.K; k += DS_NT) {
         int id = a.t_ids[(int64_t)row * a.K + k];
@@ -137,13 +146,13 @@ __device__ __forceinline__ DsTeacher ds_teacher(const DsArgs &a, int row, int32_
         top = fmaxf(top, t);
     }
     top = ds_block_max(top, sh);
-    float sum = 0.f;
+    double sum = 0.0;
     for (int k = threadIdx.x; k < a.K; k += DS_NT) {
         const float t = s_q[k], q = t == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(a.l * (t - top));
         s_q[k] = q;
-        sum += q;
+        sum += (double)q;
     }
-    return DsTeacher{top, ds_block_sum(sum, sh)};
+    return DsTeacher{top, ds_block_sum(sum, shd)};
 }
 
 // First pass: every slice's largest logit and sum of powers; the first slice also the row's A.  1,024 x 390,625 bf16 144 us: HBM at 5.5 TB/s.
@@ -154,7 +163,7 @@ ds_stats_kernel(DsArgs a) {
     float *const s_q = (float *)(s_id + a.K);
     __shared__ float sh[4];
     __shared__ double shd[4];
-    const int row = a.row0 + blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int row = a.row0 + blockIdx.y;
     const T *const z = (const T *)a.logits + (int64_t)row * a.ldl;
     const DsSlice<T, true> sl(a, z, blockIdx.x);
     typedef DsVec<T> V;
@@ -189,22 +198,19 @@ ds_stats_kernel(DsArgs a) {
     s = ds_block_sum(s * (m == base ? 1.f : __builtin_amdgcn_exp2f(a.l * (m - base))), sh);
     if (threadIdx.x == 0) a.part[(int64_t)row * a.parts + blockIdx.x] = make_float2(top, s);
     if (blockIdx.x) return;
-    const DsTeacher t = ds_teacher(a, row, s_id, s_q, sh);
-    if (threadIdx.x == 0) a.t[row] = make_float2(t.top, t.sum);
+    const DsTeacher t = ds_teacher(a, row, s_id, s_q, sh, shd);
+    if (threadIdx.x == 0) a.t[row] = make_float2(t.top, (float)t.sum);
     double sum = 0.0;
-    const double inv_T = 1.0 / (double)a.T, log_sum = log((double)t.sum);
+    const double inv_T = 1.0 / (double)a.T, log_sum = log(t.sum);
     for (int k = threadIdx.x; k < a.K; k += DS_NT) {
         const float q = s_q[k];
         if (s_id[k] >= 0 && q != 0.f) {
             const double log_q = ((double)ds_t_logit(a, (int64_t)row * a.K + k) - (double)t.top) * inv_T - log_sum;
-            sum += (double)q / (double)t.sum * (log_q - (double)V::one(z + s_id[k]) * inv_T);
+            sum += (double)q / t.sum * (log_q - (double)V::one(z + s_id[k]) * inv_T);
         }
     }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-    if (lane == 0) shd[wave] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) a.a[row] = shd[0] + shd[1] + shd[2] + shd[3];
+    sum = ds_block_sum(sum, shd);
+    if (threadIdx.x == 0) a.a[row] = sum;
 }
 
 __device__ __forceinline__ uint32_t ds_pad(int K) { return (uint32_t)(K + 3) & ~3u; }

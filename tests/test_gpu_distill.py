@@ -319,3 +319,43 @@ def test_refusals_of_tensors(ks):
     with pytest.raises(ks.KsError) as e:
         ks.class_distill_fwd_bwd(z, torch.zeros((3, 4_097), dtype=torch.int32, device="cuda"), torch.zeros((3, 4_097), device="cuda"))
     assert e.value.code == ks.KS_UNSUPPORTED
+
+
+def loss_rounding(z, ids, t, T):
+    """What the loss is off by at most, whatever is added to all logits of a row.  A power of x = (z - m) / T: three roundings of x, and the
+    power itself (two); a sum of them: 64 one after the other and 30 on the way up.  With them the row's sum, the teacher's sum and each q."""
+    z, t = z.double() / T, t.double() / T
+    p, depth = torch.softmax(z, 1), (z - z.amax(1, keepdim=True)).abs().clamp(max=120.0)
+    q, depth_t = torch.softmax(t, 1), (t - t.amax(1, keepdim=True)).abs().clamp(max=120.0)
+    of_sum = 96 + 3 * (p * depth).sum(1)
+    of_t = 2 + 3 * (q * depth_t).sum(1)
+    log_ratio = torch.log_softmax(t, 1) - torch.log_softmax(z, 1).gather(1, ids.long())
+    of_q = (q * (2 + 3 * depth_t + of_t[:, None]) * log_ratio.abs()).sum(1)
+    loss = (q * log_ratio).sum(1)
+    return T * T * loss, T * T * (1.05 * U32 * (of_sum + of_t + of_q + loss.abs()) + 2.0 ** -50 * (z.abs().amax(1) + 50))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_number_added_to_all_logits_changes_no_loss(ks, dtype):
+    gen = torch.Generator("cuda").manual_seed(21)
+    for C, K, T in ((1_000, 128, 1.0), (20_000, 60, 2.0), (300, 300, 1.0), (50, 1, 0.7)):
+        z, ids, t = inputs(gen, 16, C, K, dtype)
+        for add in (0.0, 30.0, -1e3, 1e4, 3e5):
+            shifted = (z.float() + add).to(dtype)
+            want, off = loss_rounding(shifted, ids, t, T)
+            got = ks.class_distill_fwd_bwd(shifted, ids, t, temperature=T)["loss_per_sample"].double()
+            worst = ((got - want).abs() - off).max().item()
+            assert worst <= 0, (C, K, T, add, (got - want).abs().max().item(), off.max().item())
+
+
+def test_a_student_that_matches_its_teacher(ks):
+    """The teacher names every class with the student's own logits: no loss, wherever they lie."""
+    gen = torch.Generator("cuda").manual_seed(22)
+    for C, add, T in ((128, 0.0, 1.0), (128, 30.0, 1.0), (1_000, -1e3, 2.0), (4_096, 1e4, 1.0)):
+        z = (2 * torch.randn((8, C), generator=gen, device="cuda") + add)
+        ids = torch.rand((8, C), generator=gen, device="cuda").argsort(1).to(torch.int32)
+        t = z.gather(1, ids.long())
+        want, off = loss_rounding(z, ids, t, T)
+        o = ks.class_distill_fwd_bwd(z, ids, t, temperature=T)
+        assert ((o["loss_per_sample"].double() - want).abs() <= off).all(), (C, add, o["loss_per_sample"].abs().max().item(), off.max().item())
+        assert want.abs().max().item() <= 1e-12 * (1 + abs(add))
