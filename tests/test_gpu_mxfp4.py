@@ -280,3 +280,61 @@ def test_refusals_of_tensors(ks):
         ks.class_quantize_mxfp4(torch.ones((3, 64), device="cuda"), codes=torch.empty(7, dtype=torch.uint8, device="cuda"))
     with pytest.raises(ValueError):
         ks.class_dequantize_mxfp4(c, 33, 64)
+
+
+def test_every_middle_at_every_exponent(ks):
+    """The middles of two values, their neighbours in 32 bits and the values themselves, for every exponent that a block can have."""
+    at = np.concatenate([GRID, (GRID[1:] + GRID[:-1]) / 2]).astype(np.float32)
+    rows = []
+    for e in range(-130, 126):
+        for f in (at, np.nextafter(at, np.float32(INF)), np.nextafter(at, np.float32(-INF))):
+            for sign in (1, -1):
+                rows.append(np.pad(np.concatenate([[4.0], f]) * sign, (0, 32 - 1 - len(at))).astype(np.float64) * 2.0 ** e)
+    V = torch.from_numpy(np.stack(rows).astype(np.float32)).cuda()  # below 2^-126 the neighbours fall on the middles or on multiples of 2^-149
+    for classes in (False, True):
+        codes = ks.class_quantize_mxfp4(V, classes=classes)
+        check_codes(codes, V, classes)
+    assert sorted(set(plain_codes(V.double().cpu().numpy())[1][:, 0].tolist())) == list(range(0, 253))
+    want = plain_values(*plain_codes(V.double().cpu().numpy()))
+    for t in (torch.float32, torch.bfloat16):
+        assert np.array_equal(ks.class_dequantize_mxfp4(codes, len(rows), 32, classes=True, dtype=t).double().cpu().numpy(), want)
+
+
+# The ways of the product: wavefronts of their own; samples in LDS, for up to 256 and up to 512 elements, where there are many groups of 64 classes and
+# products; chunks of depth through LDS for more.  The sizes lie well inside each, or on both sides of where one begins.
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,C,D", [
+    # samples in LDS, 257 to 512 elements: whole ones and ragged ones, even and odd numbers of classes, more than eight tiles of samples
+    (1_024, 16_389, 512), (1_024, 16_391, 333), (1_040, 24_000, 448), (2_049, 20_001, 257), (4_200, 10_500, 512), (8_300, 10_303, 400),
+    # up to 256 elements, 1 to 4 pieces
+    (1_024, 20_001, 200), (1_030, 20_002, 150), (1_024, 51_300, 100), (1_024, 51_301, 64), (2_050, 60_000, 33), (9_000, 11_003, 256),
+    # on both sides of 160 groups of classes, 3,800 and 1,280 wavefronts
+    (4_096, 10_240, 512), (4_096, 10_241, 512), (1_024, 15_168, 512), (1_024, 15_233, 512), (640, 8_192, 576), (640, 8_193, 576),
+    # chunks of depth: more than 32 tiles of samples, few tiles of classes, ragged depths
+    (4_200, 5_000, 640), (20_000, 500, 576), (20_001, 513, 1_000), (9_000, 1_001, 520), (1_024, 16_391, 1_025)])
+def test_every_way_of_the_product(ks, B, C, D, dtype):
+    same_logits(ks, B, C, D, dtype, bias=(B + C + D) % 2 == 0)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,C,D,pad,shift", [(300, 30_011, 800, 0, 0), (300, 30_010, 800, 1, 1), (300, 30_010, 800, 2, 1), (1_024, 20_001, 200, 1, 0), (1_024, 20_000, 200, 6, 2),
+                                             (1_024, 20_002, 512, 0, 1), (1_030, 20_003, 512, 3, 0)])
+def test_rows_beside_the_lines_on_every_way(ks, B, C, D, pad, shift, dtype):
+    same_logits(ks, B, C, D, dtype, bias=True, pad=pad, shift=shift)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_that_lie_far_apart(ks, dtype):
+    """64 MB from row to row and more, offsets beyond 32 bits: stored element by element."""
+    ld = (1 << 26) // dtype.itemsize + 2
+    same_logits(ks, 70, 101, 96, dtype, bias=True, pad=ld - 101)
+
+
+def test_a_matrix_of_more_than_2_31_elements(ks):
+    gen = torch.Generator("cuda").manual_seed(12)
+    B, C, D = 5_600, 390_625, 64
+    x, w = few_bits(gen, B, D), few_bits(gen, C, D)
+    z = ks.class_logits_mxfp4(ks.class_quantize_mxfp4(x), ks.class_quantize_mxfp4(w, classes=True), B, C, D, 0.25, dtype=torch.bfloat16)
+    assert B * z.stride(0) > 1 << 31
+    for first in range(0, B, 700):
+        assert torch.equal(z[first:first + 700], (product(x[first:first + 700], w) * 0.25).to(torch.bfloat16)), first

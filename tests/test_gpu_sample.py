@@ -348,3 +348,59 @@ def test_logits_far_apart_at_large_and_at_small_temperatures(ks, C):
         for rule in rules:
             print(T, scale, rule, flush=True)
             check(ks, z.cuda(), [0.0, 0.3, 0.7, LAST, 0.9, 0.95], T=T, **rule)
+
+
+# ---------------------------------------------------------------------------------------------------- rows that share what a call has
+def test_more_rows_that_keep_much_than_places_for_their_candidates(ks):
+    """Places for the classes around a border are there for 256 rows; rows beyond take another way, whichever they are, to the same class."""
+    gen = torch.Generator("cuda").manual_seed(31)
+    B, C = 320, 40_000
+    z = (0.0625 * torch.randint(-160, 161, (B, C), generator=gen, device="cuda")).to(torch.bfloat16)  # 321 values, some 3,700 classes in a bin at T = 85
+    z[5], z[77] = 1.5, -INF
+    u = torch.rand(B, generator=gen, device="cuda").tolist()
+    for rule in (dict(k=C // 2, T=85.0), dict(p=0.6, T=85.0)):
+        ids, lp = check(ks, z, u, **rule)
+        again = check_again(ks, z, u, **rule)
+        assert torch.equal(ids, again[0]) and torch.equal(lp, again[1])
+        for b in (0, 5, 200, B - 1):
+            one, one_lp = check(ks, z[b:b + 1], u[b], **rule)
+            assert torch.equal(one, ids[b:b + 1]) and torch.equal(one_lp, lp[b:b + 1])
+
+
+def check_again(ks, z, u, T, k=0, p=1.0):
+    B = z.shape[0]
+
+    def column(v, dtype):
+        return torch.full((B,), v, dtype=dtype, device="cuda")
+    return ks.class_sample(z, torch.tensor(u, device="cuda"), temperature=column(T, torch.float32), top_k=column(k, torch.int32), top_p=column(p, torch.float32))
+
+
+def test_more_rows_than_a_launch_takes(ks):
+    gen = torch.Generator("cuda").manual_seed(32)
+    B, C = 33_000, 24
+    z = logits_of(gen, B, C, torch.float32)
+    u = torch.rand(B, generator=gen, device="cuda").tolist()
+    check(ks, z, u, T=1.5, k=9, p=0.9)
+    # the rows of the second launch that keep more than LDS holds: the same as by themselves
+    C = 6_000
+    z = logits_of(gen, 8, C, torch.bfloat16, spread=0.3).repeat(4_200, 1)
+    u = torch.rand(z.shape[0], generator=gen, device="cuda")
+    ids, lp = ks.class_sample(z, u, top_p=torch.full((z.shape[0],), 0.97, device="cuda"))
+    for first in (0, 32_760, 33_592):
+        part = slice(first, first + 8)
+        own = check(ks, z[part], u[part].tolist(), p=0.97)
+        assert torch.equal(own[0], ids[part]) and torch.equal(own[1], lp[part])
+
+
+def test_many_classes_of_few_logits_in_long_parts(ks):
+    """Parts of 1,024 classes and bins of a million equal logits."""
+    C = 2_500_000
+    gen = torch.Generator("cuda").manual_seed(33)
+    equal = torch.full((1, C), -0.75, dtype=torch.bfloat16, device="cuda")
+    five = torch.randint(-2, 3, (1, C), generator=gen, device="cuda").to(torch.bfloat16)
+    near = 0.01 * torch.randint(0, 3, (1, C), generator=gen, device="cuda").to(torch.float32)
+    for z in (equal, five, near, five[:, 3:C - 2]):
+        for rule in (dict(k=C // 3), dict(p=0.37), dict(k=C // 2, p=0.5), dict(m=0.3)):
+            print(rule, flush=True)
+            check(ks, z, 0.618, **rule)
+    check(ks, torch.cat([equal, five]), [0.0, LAST], k=C // 3, p=0.9)
