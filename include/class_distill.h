@@ -26,9 +26,9 @@ extern "C" {
  *     loss_i = T^2 sum_c q_c (log q_c - log p_c)           (entries with q = 0 count nothing; each entry by itself where a class is
  *                                                           named more than once),      loss_mean = mean_i loss_i
  *     dlogits[i, c] = grad_scale * T / B * (p_c - q_c)     (the gradient of grad_scale * loss_mean)
- * Powers and the sum of a row's are fp32, the rest of the loss is fp64: a loss is off by about T^2 / 10^6 at most (T^2 times the roundings of
- * ln sum_c exp(z_c / T)) and by one rounding to fp32, whatever number is added to all logits of the row; it may come out below 0 by as much.
- * p_c and q_c are off by as many roundings of their own; dlogits is rounded to its type once.
+ * Powers and a row's sum of them are fp32, the rest of the loss is fp64: a loss is off by at most T^2 / 50,000 (the roundings of
+ * ln sum_c exp(z_c / T), up to some 200 of 2^-24) and a like share of itself, whatever number is added to all logits of the row, and may be
+ * below 0 by as much.  p_c and q_c have as many roundings; dlogits is rounded to its type once.
  *
  *   logits [B, C]     in, dtype KS_DTYPE_FP32 or KS_DTYPE_BF16, row i at element i * ldl (ldl >= C; aligned to its elements is enough; reads and
  *                     writes are fastest where rows of logits and dlogits begin equally many bytes beside a multiple of 16)
