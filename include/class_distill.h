@@ -1,7 +1,9 @@
 /*
  * class_distill.h -- C ABI of learning from a teacher's top logits on one MI355X (gfx950): loss and gradient of a batch of logits against
  * every class, where the teacher says for each sample which classes it holds likely and how much (a larger layer's answer: class_logits.h,
- * class_mxfp4.h).  It stands beside full_softmax_fwd_bwd (knnsoftmax.h), whose teacher names one class.
+ * class_mxfp4.h).  It stands beside full_softmax_fwd_bwd (knnsoftmax.h), whose teacher names one class and which takes W and X: this call
+ * takes the logits and gives their gradient, the products before and behind it are the caller's.  A row holds all classes of the layer:
+ * where the layer is sharded, the shards' logits have to be gathered first (ids count from 0 to C - 1 in the row).
  *
  * Part of the same shared library; the conventions of knnsoftmax.h hold here too (device pointers, caller-owned memory and workspace,
  * nothing allocated, calls only enqueue work on `stream`, ks_status return values, KS_DEV_* bits in *dev_status, no floating-point

@@ -1,6 +1,7 @@
 /*
  * class_sample.h -- C ABI of drawing one class per request from a matrix of logits on one MI355X (gfx950), what a serving loop does after
- * class_logits_adjust (class_logits.h): temperature, top-k, top-p and min-p, by random numbers that the caller brings.
+ * class_logits_adjust (class_logits.h): temperature, top-k, top-p and min-p, by random numbers that the caller brings.  A row holds all
+ * classes that a request can get: where the layer is sharded, the shards' logits have to be gathered first.
  *
  * Part of the same shared library as knnsoftmax.h; the conventions stated there hold here too (device pointers, caller-owned memory and
  * workspace, nothing allocated, calls only enqueue work on `stream`, ks_status return values).  The call may be captured into a graph.

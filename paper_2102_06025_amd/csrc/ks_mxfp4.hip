@@ -541,7 +541,9 @@ __device__ __forceinline__ void m4_barrier() {
 // buffers, a barrier a chunk.  While chunk t is multiplied, a fragment is read for the next k-step when it has been used (the last ones
 // from chunk t + 1, which is there since the barrier), and chunk t + 2 is written to LDS from registers.  Weights come straight from memory,
 // four k-steps ahead.  2,048 x 131,072 x 4,096 bf16: 650 us, 3.4 PFLOP/s (wavefronts of their own 1,320); what holds it up are the operands' ways
-// into the registers, 32 KB from LDS and 18 KB through the caches for 64 matrix instructions.  The chunks run on from one tile of 512 classes by 128 samples to the next; what lies beyond the depth is loaded as 0.
+// into the registers, 32 KB from LDS and 18 KB through the caches for 64 matrix instructions: the matrix pipes are busy 40 % of the cycles, at 2.0 GHz
+// (92 %, at 1.7 GHz and 6.1 PFLOP/s, with operands in registers).  The chunks run on from one tile of 512 classes by 128 samples to the next;
+// what lies beyond the depth is loaded as 0 and multiplied (2,048 x 131,072 x 576 184 us, x 1,024 212).
 template <typename OUT>
 __global__ void __launch_bounds__(M4X_NT, 2)
 m4_staged_kernel(const uint8_t *__restrict__ xq, const uint8_t *__restrict__ wq, const float *__restrict__ bias, int64_t C, int kb, int B, float scale,
@@ -708,9 +710,11 @@ static void m4_logits(const uint8_t *xq, const uint8_t *wq, const float *bias, i
     if (B <= 32) return waves <= 1024 && kb >= 16 ? direct(m4_direct_kernel<1, 4, OUT>, 32, 1) : direct(m4_direct_kernel<1, 1, OUT>, 32, 4);
     // Few samples: the codes of the weights are what moves, and every wavefront reads its own (1 x 390,625 x 512 bf16: 24 us with the features'
     // codes); where there are few wavefronts and rows are deep, four of them divide a group's depth.  Few wavefronts, or few groups of classes
-    // for the 256 workgroups that keep samples, likewise (10,000 classes, batch 1,024: x 128 8.7 us, 19.6 with samples kept; x 512 10.4 and 15.6;
-    // 30,000 x 512, 512: 13.5 and 15.5; but 1,024: 23.5 and 16.9; 50,000 x 128, 2,048: 35.9 and 46.6), and rows that begin on an odd
-    // element, which are stored element by element.
+    // for the 256 workgroups that keep samples, likewise, and rows that begin on an odd element, which are stored element by element.  In us, of wavefronts
+    // of their own and with samples kept: 10,000 classes (157 groups), batch 1,024, x 128 8.6 and 19.6, x 512 10.5 and 15.8; 2,048 x 512 14.9 and 16.6;
+    // 4,096 x 512 25.7 and 24.4; 16,000 (250 groups) 2,048 x 512 28 and 20, x 256 15.0 and 18.9; 30,000, 512 x 512 (3,752 wavefronts) 13.8 and 15.4, 1,024
+    // 23.7 and 18.7; x 128, 2,048: 50,000 (782 groups) 34 and 47, 60,000 56 and 54.  Deeper rows: 10,000 x 576, 512 (1,256 wavefronts) 7.9 and 13.6, 1,024
+    // 11.2 and 14.1; 131,072 x 576, 2,048 249 and 184; but 1,000 x 1,024, 8,192 11 and 25: a few tiles of 512 classes leave XCDs without work.
     if (B <= 64 || waves <= 1280 || (kb <= 8 && (!vec || groups <= 160 || waves <= 3800)) || (kb <= 2 && groups <= 800))
         return waves <= 320 && kb >= 16 ? direct(m4_direct_kernel<2, 4, OUT>, 64, 1) : direct(m4_direct_kernel<2, 1, OUT>, 64, 4);
     if (kb > 8) {

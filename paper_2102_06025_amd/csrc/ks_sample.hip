@@ -173,7 +173,7 @@ template <int LG, typename V, typename OP> __device__ __forceinline__ V sp_lanes
     return v;
 }
 
-// A wavefront per 512 classes, or per granule of more.  256 x 390,625 bf16: 47 us (200 MB at 4.3 TB/s), 73 where a third of the rows needs the
+// A wavefront per 512 classes, or per granule of more.  256 x 390,625 bf16: 47 to 52 us (200 MB at 3.8 to 4.3 TB/s), 72 where a third of the rows needs the
 // granules' weights: fp64 powers.
 template <int LG, typename T>
 __global__ void __launch_bounds__(256)
@@ -492,7 +492,7 @@ template <int NT> __device__ __forceinline__ void sp_order(uint64_t *p, uint64_t
 }
 
 __device__ __forceinline__ void sp_share_row(const SpArgs &a, int row, float top, int b0, uint64_t target_p);
-// What bounds it is the way through its short steps: 1 x 10,000 fp32, k = 50 13 us; 256 x 390,625 bf16, k = 500 44.
+// What bounds it is the way through its short steps: 1 x 10,000 fp32, k = 50 13 us; 256 x 390,625 bf16, k = 500 44 to 47.
 struct SpShared {
     SpScan scan;
     float top[SP_GRANULES]; // of the granules
@@ -599,6 +599,8 @@ sp_draw_kernel(SpArgs a) {
         if (!rule.use_k) target_p = sp_share(rule.p, sp_total<NT>(sh.scan, sum));
         sp_find<NT>(sh.scan, sh.n, sh.w, rule.use_k, rule.use_k ? (uint64_t)rule.k : target_p, w_all, n_all);
         const int found = sh.scan.found < 0 ? limit - 1 : sh.scan.found;
+        // A share is looked for half a binade beyond where the granules' own weights reach it, and then two binades on at a time (256 x 390,625 bf16, spread 4,
+        // p = 0.9: 416 us; from the granules' bin on 433, two binades beyond it 425; 16 x 30,000 fp32 81, 76 and 54, and by one binade at a time 73)
         b0 = rule.use_k ? (rule.use_p ? found : sp_min(found, bin_m)) : sp_min(found + SP_PER_BINADE / 2, bin_m);
     }
     // 2  the classes down to there in order, and their running weight; more of them while a share of the weight is not reached
@@ -607,6 +609,8 @@ sp_draw_kernel(SpArgs a) {
         uint32_t listed = 0;
         for (int g = g0; g < g1; ++g) listed += sp_bin(sh.top[g], top, c32) <= b0;
         sp_scan<NT>(sh.scan, 0, listed, w0, n0, w_all, n_all);
+        // Rows that list more than a span of classes are shared.  With top-k four of them: candidates are found by one read, what it costs to share
+        // them is more (256 x 390,625 bf16, k = 500: 101 us, with two spans 177, with one 225; 64 rows, k = 3,000: 124 with one to eight, 297 with sixteen)
         if (n_all > SP_CAND || (rule.use_k && rule.k > SP_CAND) || n_all * a.gran > (rule.use_k ? 4 * a.most : a.most)) n = SP_CAND + 1; // a class of each granule is in
         else {
             if (threadIdx.x == 0) sh.fill = 0;
