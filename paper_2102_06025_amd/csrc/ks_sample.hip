@@ -306,11 +306,12 @@ __device__ __forceinline__ uint64_t sp_mass(const SpArgs &a, int row, int g, flo
 __device__ __forceinline__ float sp_c32(const SpRule &rule) { return fminf((float)(rule.c * SP_PER_BINADE), SP_MOST); }
 // from this bin on weights are 0: half of 2^-bits lies at the end of bin (bits + 1) * SP_PER_BINADE - 1, and bins are found with roundings
 __device__ __forceinline__ int sp_limit(const SpArgs &a) { return (a.bits + 1) * SP_PER_BINADE + 1; }
-__device__ __forceinline__ int sp_bin_m(const SpArgs &a, const SpRule &rule) { // last bin with weights of m or more
-    return rule.use_m ? (int)fminf(-log2f(rule.m) * SP_PER_BINADE + 2.f, (float)(sp_limit(a) - 1)) : sp_limit(a) - 1;
-}
 __device__ __forceinline__ uint64_t sp_floor(const SpArgs &a, const SpRule &rule) { // least weight that is kept
     return rule.use_m ? sp_max((uint64_t)ceil((double)rule.m * (double)((uint64_t)1 << a.bits)), (uint64_t)1) : 1;
+}
+// last bin with weights of m or more: whole ones, which half of 2^-bits less is rounded up to
+__device__ __forceinline__ int sp_bin_m(const SpArgs &a, const SpRule &rule) {
+    return rule.use_m ? (int)fminf(((float)a.bits - log2f((float)sp_floor(a, rule) - 0.5f)) * SP_PER_BINADE + 2.f, (float)(sp_limit(a) - 1)) : sp_limit(a) - 1;
 }
 __device__ __forceinline__ uint64_t sp_share(double p, uint64_t w) { return sp_max((uint64_t)ceil(p * (double)w), (uint64_t)1); } // the weight that is p of w
 __device__ __forceinline__ uint64_t sp_target(const SpArgs &a, int row, uint64_t w) { // the running weight that the drawn class exceeds: u of w

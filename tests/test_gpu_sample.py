@@ -404,3 +404,15 @@ def test_many_classes_of_few_logits_in_long_parts(ks):
             print(rule, flush=True)
             check(ks, z, 0.618, **rule)
     check(ks, torch.cat([equal, five]), [0.0, LAST], k=C // 3, p=0.9)
+
+
+@pytest.mark.parametrize("C", [8, 5_000, 40_000])
+def test_the_least_weights_and_min_p(ks, C):
+    """Whole weights are compared with m: one of 0.6 of 2^-s is 1 and stays for m = 0.7 of 2^-s, 2.6 is 3 and stays for 2.9, 1.4 is 1 and goes for 1.2."""
+    s = min(48, 62 - math.ceil(math.log2(C)))
+    for weight, m, stays in ((0.6, 0.7, True), (0.55, 1.0, True), (2.6, 2.9, True), (1.4, 1.2, False), (0.4, 0.3, False), (9.6, 9.99, True)):
+        z = torch.full((1, C), -200.0, device="cuda")
+        z[0, 1], z[0, 5], z[0, C - 1] = math.log(weight) - s * math.log(2.0), 0.0, -1.0
+        for rule in (dict(), dict(k=3), dict(k=4), dict(p=1 - 2.0 ** -24)):
+            ids, _ = check(ks, z, 0.0, m=m * 2.0 ** -s, **rule)
+            assert ids.item() == (1 if stays and "p" not in rule else 5), (weight, m, rule)
