@@ -30,7 +30,7 @@ extern "C" {
  *     dlogits[i, c] = grad_scale * T / B * (p_c - q_c)     (the gradient of grad_scale * loss_mean)
  * Powers and a row's sum of them are fp32, the rest of the loss is fp64: a loss is off by at most T^2 / 50,000 (the roundings of
  * ln sum_c exp(z_c / T), up to some 200 of 2^-24) and a like share of itself, whatever number is added to all logits of the row, and may be
- * below 0 by as much.  p_c and q_c have as many roundings; dlogits is rounded to its type once.
+ * below 0 by as much.  p_c and q_c have as many roundings, powers below 2^-126 are 0; dlogits is rounded to its type once.
  *
  *   logits [B, C]     in, dtype KS_DTYPE_FP32 or KS_DTYPE_BF16, row i at element i * ldl (ldl >= C; aligned to its elements is enough; reads and
  *                     writes are fastest where rows of logits and dlogits begin equally many bytes beside a multiple of 16)
